@@ -10,7 +10,9 @@
  *     tiles, with their per-token discrepancy (Sec. 3.1, Sec. 3.4, Eq. 9-12);
  *   - the running sums of the least-squares absorption (Sec. 3.2, Eq. 5) and
  *     the closed-form solve with its feasibility score (Eq. 5-6);
- *   - appending a finished chunk's K/V into a ring-buffer cache.
+ *   - appending a finished chunk's K/V into a ring-buffer cache;
+ *   - the rest of a DiT layer's attention block: its norms with modulation, gate and
+ *     residual, and the rotary positions of q and k.
  *
  * Conventions (all entry points)
  *   - Every tensor argument is a DEVICE pointer owned by the caller, unless
@@ -32,7 +34,7 @@
  *     1: an empty call is an argument error (ISPA_ERR_INVALID_ARG) and
  *     enqueues nothing, so callers skip empty work themselves.
  *   - CUDA graphs: after one eager call on a device, the attention, append, LS
- *     accumulate / reset, quantisation and W8A8 entry points enqueue only
+ *     accumulate / reset, quantisation, norm, rotary and W8A8 entry points enqueue only
  *     kernel launches and memsets on `stream` and can be captured.  A replay reuses what the call
  *     saw at capture time: pointers, and the ring's frames_written and hence its
  *     key sets (an append advances frames_written on the host when it is
@@ -671,6 +673,158 @@ ISPA_API ispa_status ispa_quantize_weight_e4m3(const float* W, const float* dW, 
 ISPA_API ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, const uint8_t* w_q,
                                       const float* w_scale, int64_t T, int32_t D, int32_t D_out, void* out,
                                       ispa_stream stream);
+
+/* ------------------------------------------------------------ norms, gate and residual */
+/*
+ * What stands between a transformer block's products in a DiT layer around the chunk attention:
+ * the norm before the block with the modulation of its frame (adaptive norm), and after it the
+ * norm of its output, the gate, the residual scale and the next block's norm, in one pass.
+ *
+ *   rms(v)   = v / sqrt(mean(v^2) + eps) * weight + bias
+ *   layer(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias
+ *   none(v)  = v * weight + bias
+ *
+ * Rows are dense [rows][dim].  dim a multiple of 8 up to 32768, rows below 2^31 (else
+ * ISPA_ERR_UNSUPPORTED).
+ * Statistics and all arithmetic between load and store in fp32.
+ */
+#define ISPA_NORM_NONE 0
+#define ISPA_NORM_RMS 1
+#define ISPA_NORM_LAYER 2
+
+typedef struct {
+  int32_t kind;        /* ISPA_NORM_* */
+  float eps;           /* finite, >= 0 */
+  const float* weight; /* fp32 [dim], NULL: ones */
+  const float* bias;   /* fp32 [dim], NULL: zeros */
+} ispa_norm;
+
+/* Modulation vectors: row r takes group r / rows_per_group, whose vectors of dim values stand at
+ * scale + group * stride (and so on).  The caller holds ceil(rows / rows_per_group) groups.
+ * stride in values, a multiple of 4 (the vectors of all groups may be rows of one projection of
+ * the time embedding, [groups][6][dim]: stride 6 * dim); 0: one vector for every group. */
+typedef struct {
+  const float* scale; /* h = norm(x) * (1 + scale) + shift; NULL: 0 */
+  const float* shift; /* NULL: 0 */
+  const float* gate;  /* of the residual; NULL: 1 */
+  int64_t stride;
+  int64_t rows_per_group; /* >= 1 */
+} ispa_modulation;
+
+/* Type of the residual stream x. */
+#define ISPA_BF16 0
+#define ISPA_FP32 1
+
+/* Where normed rows go: bf16, or 8-bit codes with one fp32 scale per row (value ~ code * scale):
+ *   amax = max |h| of the row (fp32, before any rounding to bf16);
+ *   E4M3: scale = amax / 448, code = e4m3(h * (448 / amax)), as ispa_quantize_rows_e4m3 does;
+ *   I8:   scale = amax / 127, code = round(h * (127 / amax)) to nearest even, in [-127, 127];
+ *   an all-zero row has scale 1.  A row with an infinity or a NaN has an infinite or NaN scale (its
+ *   codes say nothing), so that what is computed from it is no finite number. */
+#define ISPA_ROWS_BF16 0
+#define ISPA_ROWS_E4M3 1
+#define ISPA_ROWS_I8 2
+
+typedef struct {
+  void* data;     /* bf16, uint8 or int8 [rows][dim] */
+  float* scale;   /* fp32 [rows]; unused for ISPA_ROWS_BF16 */
+  int32_t format; /* ISPA_ROWS_* */
+  int32_t reserved;
+} ispa_rows_out;
+
+/* out = norm(x) * (1 + scale_g) + shift_g.  mod: NULL for no modulation (its gate is not used).
+ * out->data must not overlap x. */
+ISPA_API ispa_status ispa_norm_modulate(const void* x, int32_t x_type, int64_t rows, int32_t dim,
+                                        const ispa_norm* norm, const ispa_modulation* mod, const ispa_rows_out* out,
+                                        ispa_stream stream);
+
+/* x_out = x_scale * x + y_scale * gate_g * post(y), then, with pre not NULL,
+ * out = pre(x_out) * (1 + scale_g) + shift_g of x_out as it is stored.
+ *   x, x_out : [rows][dim] of x_type; x_out may be x itself (nothing else may overlap)
+ *   y        : bf16 [rows][dim], the block's output
+ *   post, mod: NULL for none;  pre, out: both or neither */
+ISPA_API ispa_status ispa_gate_residual(const void* x, int32_t x_type, const void* y, int64_t rows, int32_t dim,
+                                        const ispa_norm* post, float x_scale, float y_scale,
+                                        const ispa_modulation* mod, void* x_out, const ispa_norm* pre,
+                                        const ispa_rows_out* out, ispa_stream stream);
+
+/* ------------------------------------------------------------ rotary positions */
+/*
+ * Rotary positions of a chunk's queries and keys on their way from the projection to the attention
+ * and the ring, with the RMS norm of q and k where the model has one, for q and k in one launch.
+ * Pair i of every head turns by pos * w_i radians at its axis's position:
+ *   (u, v) -> factor * (u cos - v sin, u sin + v cos)
+ * Features of a head past 2 * pairs pass unturned (but normed).  Negative positions turn back.
+ */
+#define ISPA_ROPE_INTERLEAVED 0 /* pair i: features 2 i and 2 i + 1 */
+#define ISPA_ROPE_HALF 1        /* pair i: features i and i + pairs */
+#define ISPA_ROPE_MAX_AXES 3
+
+typedef struct {
+  int32_t layout;                         /* ISPA_ROPE_* */
+  int32_t head_dim;                       /* a multiple of 8, at most 256 (else ISPA_ERR_UNSUPPORTED) */
+  int32_t n_axes;                         /* 1 to 3 (say: frame, row, column) */
+  int32_t axis_pairs[ISPA_ROPE_MAX_AXES]; /* pairs of each axis, in order; their sum is the number of pairs: at
+                                             most head_dim / 2, and a multiple of 8 for ISPA_ROPE_HALF (else
+                                             ISPA_ERR_UNSUPPORTED) */
+  float factor;                           /* on the rotated features (1 but for some long-context scalings) */
+  int32_t reserved;
+  const uint64_t* steps;                  /* DEVICE [pairs]: turns per position as fractions of 2^64
+                                             (ispa_rope_steps, once per model) */
+} ispa_rope;
+
+/* RMS norm in front of the rotation: none, over each head (weight [head_dim]), or over all heads
+ * of the token (weight [heads * head_dim]). */
+#define ISPA_QK_NORM_NONE 0
+#define ISPA_QK_NORM_HEAD 1
+#define ISPA_QK_NORM_TOKEN 2
+
+/* One of the tensors to turn: bf16, token t's heads at x + t * x_stride, [heads][head_dim] dense.
+ * Strides in values, at least heads * head_dim and multiples of 8 (16 bytes): q and k may be columns of
+ * a fused projection.  out may be x with the same stride; else they must not overlap. */
+typedef struct {
+  const void* x;
+  void* out;
+  int64_t x_stride, out_stride;
+  const float* norm_weight; /* fp32, NULL: ones */
+  float eps;
+  int32_t norm;             /* ISPA_QK_NORM_* */
+  int32_t heads;
+  int32_t reserved;
+} ispa_rope_rows;
+
+/* rows: host array of n_rows (1 or 2: queries and keys, whose heads may differ in number);
+ * pos: device int32 [n_axes][n]; pos0 is added to the positions of axis 0 (the chunk's first frame).
+ * The angle is reduced to a fraction of a turn in 64-bit integers, so far positions lose nothing.
+ * n below 2^31 (else ISPA_ERR_UNSUPPORTED). */
+ISPA_API ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows,
+                                     const int32_t* pos, int64_t pos0, int64_t n, ispa_stream stream);
+
+/* Frequencies of one axis: w_i = base^(-i / n_pairs) radians per position, i = 0 .. n_pairs - 1, scaled for
+ * contexts `scale` times as long as the trained one:
+ *   NONE    as they are
+ *   LINEAR  w_i / scale (positions interpolated)
+ *   BASE    base * scale^(n_pairs / (n_pairs - 1)) in base's place: the slowest pair gets the whole scale, the
+ *           fastest none (one pair: LINEAR)
+ *   PARTS   pairs that turn at least `high` times over the trained length stay, those that turn at most `low` times
+ *           are divided by scale, a linear ramp in the turns between; factor = 0.1 ln(scale) + 1 */
+#define ISPA_ROPE_SCALE_NONE 0
+#define ISPA_ROPE_SCALE_LINEAR 1
+#define ISPA_ROPE_SCALE_BASE 2
+#define ISPA_ROPE_SCALE_PARTS 3
+
+typedef struct {
+  double base;           /* >= 1 */
+  double scale;          /* >= 1; unused for NONE */
+  double trained_length; /* PARTS: positions the model was trained on, > 0 */
+  double low, high;      /* PARTS: 0 <= low < high (1 and 32, say) */
+  int32_t scaling;       /* ISPA_ROPE_SCALE_* */
+  int32_t reserved;
+} ispa_rope_frequencies;
+
+/* Host-only: steps[i] = round(w_i / (2 pi) * 2^64) of one axis (host array of n_pairs, to be copied to the
+ * device next to the other axes'), and *factor (nullable) for ispa_rope. */
+ISPA_API ispa_status ispa_rope_steps(const ispa_rope_frequencies* f, int32_t n_pairs, uint64_t* steps, float* factor);
 
 #ifdef __cplusplus
 }

@@ -30,6 +30,12 @@ ISPA_KV_BF16 = 0             # ring k_format values
 ISPA_KV_K_E4M3 = 1
 ISPA_KV_KV_E4M3 = 2
 MAX_RANGES = 4
+ISPA_NORM_NONE, ISPA_NORM_RMS, ISPA_NORM_LAYER = 0, 1, 2
+ISPA_BF16, ISPA_FP32 = 0, 1                                     # types of the residual stream
+ISPA_ROWS_BF16, ISPA_ROWS_E4M3, ISPA_ROWS_I8 = 0, 1, 2
+ISPA_ROPE_INTERLEAVED, ISPA_ROPE_HALF = 0, 1
+ISPA_QK_NORM_NONE, ISPA_QK_NORM_HEAD, ISPA_QK_NORM_TOKEN = 0, 1, 2
+ISPA_ROPE_SCALE_NONE, ISPA_ROPE_SCALE_LINEAR, ISPA_ROPE_SCALE_BASE, ISPA_ROPE_SCALE_PARTS = 0, 1, 2, 3
 
 
 class KVRing(Structure):
@@ -59,6 +65,35 @@ class KeySets(Structure):
 
 class LSState(Structure):
     _fields_ = [("dim", c_int32), ("reserved", c_int32), ("n_tokens", c_int64), ("gram", c_void_p)]
+
+
+class Norm(Structure):
+    _fields_ = [("kind", c_int32), ("eps", c_float), ("weight", c_void_p), ("bias", c_void_p)]
+
+
+class Modulation(Structure):
+    _fields_ = [("scale", c_void_p), ("shift", c_void_p), ("gate", c_void_p), ("stride", c_int64),
+                ("rows_per_group", c_int64)]
+
+
+class RowsOut(Structure):
+    _fields_ = [("data", c_void_p), ("scale", c_void_p), ("format", c_int32), ("reserved", c_int32)]
+
+
+class Rope(Structure):
+    _fields_ = [("layout", c_int32), ("head_dim", c_int32), ("n_axes", c_int32), ("axis_pairs", c_int32 * 3),
+                ("factor", c_float), ("reserved", c_int32), ("steps", c_void_p)]
+
+
+class RopeRows(Structure):
+    _fields_ = [("x", c_void_p), ("out", c_void_p), ("x_stride", c_int64), ("out_stride", c_int64),
+                ("norm_weight", c_void_p), ("eps", c_float), ("norm", c_int32), ("heads", c_int32),
+                ("reserved", c_int32)]
+
+
+class RopeFrequencies(Structure):
+    _fields_ = [("base", c_double), ("scale", c_double), ("trained_length", c_double), ("low", c_double),
+                ("high", c_double), ("scaling", c_int32), ("reserved", c_int32)]
 
 
 class IspaError(RuntimeError):
@@ -144,6 +179,12 @@ _SIGS = {
     "ispa_quantize_weight_e4m3": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
     "ispa_linear_w8a8": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_void_p,
                                    c_void_p]),
+    "ispa_norm_modulate": (c_int32, [c_void_p, c_int32, c_int64, c_int32, POINTER(Norm), POINTER(Modulation),
+                                     POINTER(RowsOut), c_void_p]),
+    "ispa_gate_residual": (c_int32, [c_void_p, c_int32, c_void_p, c_int64, c_int32, POINTER(Norm), c_float, c_float,
+                                     POINTER(Modulation), c_void_p, POINTER(Norm), POINTER(RowsOut), c_void_p]),
+    "ispa_rope_apply": (c_int32, [POINTER(Rope), POINTER(RopeRows), c_int32, c_void_p, c_int64, c_int64, c_void_p]),
+    "ispa_rope_steps": (c_int32, [POINTER(RopeFrequencies), c_int32, POINTER(c_uint64), POINTER(c_float)]),
     "ispa_ls_solve": (c_int32, [POINTER(LSState), c_void_p, c_int32, c_double, c_void_p, POINTER(c_double),
                                 c_void_p, c_size_t, c_void_p]),
 }
@@ -478,3 +519,66 @@ def ispa_attn_dual_qk8(ring: KVRing, k_ring_scale, win: Window, q8, q_scale, k8_
                                     _ptr(a_loc), _ptr(disc), _ptr(disc_sq_sum), _ptr(lse_full), _ptr(lse_loc),
                                     _ptr(workspace), ws_bytes, _stream(stream)), "ispa_attn_dual_qk8")
 
+
+# ---------------------------------------------------------------- norms, gate and residual
+def _holding(s, *tensors):
+    """A struct of pointers that keeps the tensors it points into alive."""
+    s.tensors = tensors
+    return s
+
+
+def norm(kind: int, eps: float = 1e-6, weight=None, bias=None) -> Norm:
+    return _holding(Norm(kind, eps, _ptr(weight), _ptr(bias)), weight, bias)
+
+
+def modulation(scale=None, shift=None, gate=None, stride: int = 0, rows_per_group: int = 1) -> Modulation:
+    return _holding(Modulation(_ptr(scale), _ptr(shift), _ptr(gate), stride, rows_per_group), scale, shift, gate)
+
+
+def rows_out(data, format: int = ISPA_ROWS_BF16, scale=None) -> RowsOut:
+    return _holding(RowsOut(_ptr(data), _ptr(scale), format, 0), data, scale)
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def ispa_norm_modulate(x, x_type: int, rows: int, dim: int, norm: Norm, mod: Modulation | None, out: RowsOut,
+                       stream=None) -> None:
+    _check(lib().ispa_norm_modulate(_ptr(x), x_type, rows, dim, _ref(norm), _ref(mod), _ref(out), _stream(stream)),
+           "ispa_norm_modulate")
+
+
+def ispa_gate_residual(x, x_type: int, y, rows: int, dim: int, post: Norm | None, x_scale: float, y_scale: float,
+                       mod: Modulation | None, x_out, pre: Norm | None = None, out: RowsOut | None = None,
+                       stream=None) -> None:
+    _check(lib().ispa_gate_residual(_ptr(x), x_type, _ptr(y), rows, dim, _ref(post), x_scale, y_scale, _ref(mod),
+                                    _ptr(x_out), _ref(pre), _ref(out), _stream(stream)), "ispa_gate_residual")
+
+
+# ---------------------------------------------------------------- rotary positions
+def rope(layout: int, head_dim: int, axis_pairs, steps, factor: float = 1.0) -> Rope:
+    """axis_pairs: pairs of each axis; steps: device int64 / uint64 tensor of all pairs (ispa_rope_steps)."""
+    n = len(axis_pairs)
+    return _holding(Rope(layout, head_dim, n, (c_int32 * 3)(*list(axis_pairs)[:3]), factor, 0, _ptr(steps)), steps)
+
+
+def rope_rows(x, out, heads: int, x_stride: int, out_stride: int, norm: int = ISPA_QK_NORM_NONE, norm_weight=None,
+              eps: float = 1e-6) -> RopeRows:
+    return _holding(RopeRows(_ptr(x), _ptr(out), x_stride, out_stride, _ptr(norm_weight), eps, norm, heads, 0),
+                    x, out, norm_weight)
+
+
+def ispa_rope_apply(rope: Rope, rows: list, pos, pos0: int, n: int, stream=None) -> None:
+    arr = (RopeRows * len(rows))(*rows)
+    _check(lib().ispa_rope_apply(ctypes.byref(rope), arr, len(rows), _ptr(pos), pos0, n, _stream(stream)),
+           "ispa_rope_apply")
+
+
+def ispa_rope_steps(n_pairs: int, base: float = 10000.0, scaling: int = ISPA_ROPE_SCALE_NONE, scale: float = 1.0,
+                    trained_length: float = 1.0, low: float = 1.0, high: float = 32.0) -> tuple[list[int], float]:
+    """(turns per position of one axis as fractions of 2^64, factor on the rotated features)."""
+    f = RopeFrequencies(base, scale, trained_length, low, high, scaling, 0)
+    steps, factor = (c_uint64 * max(n_pairs, 1))(), c_float(0.0)
+    _check(lib().ispa_rope_steps(ctypes.byref(f), n_pairs, steps, ctypes.byref(factor)), "ispa_rope_steps")
+    return list(steps), factor.value

@@ -510,6 +510,47 @@ __global__ void wait_probe_kernel(uint64_t limit_ns, int* status) {
   }
 }
 
+bool aligned16_or_null(const void* p) { return !p || aligned16(p); }
+
+bool good_norm(const ispa_norm* n) {
+  return n->kind >= ISPA_NORM_NONE && n->kind <= ISPA_NORM_LAYER && n->eps >= 0.f && isfinite(n->eps) &&
+         aligned16_or_null(n->weight) && aligned16_or_null(n->bias);
+}
+
+// Checks and parameters that the two norm entry points share; null norms and a null `out` are allowed here.
+ispa_status norm_params(NormParams& p, const void* x, int32_t x_type, int64_t rows, int32_t dim,
+                        const ispa_norm* post, const ispa_norm* pre, const ispa_modulation* mod,
+                        const ispa_rows_out* out) {
+  if (!aligned16(x) || (x_type != ISPA_BF16 && x_type != ISPA_FP32) || rows <= 0 || dim <= 0 ||
+      (post && !good_norm(post)) || (pre && !good_norm(pre)))
+    return ISPA_ERR_INVALID_ARG;
+  if (mod && (mod->rows_per_group < 1 || mod->stride < 0 || mod->stride % 4 != 0 || !aligned16_or_null(mod->scale) ||
+              !aligned16_or_null(mod->shift) || !aligned16_or_null(mod->gate)))
+    return ISPA_ERR_INVALID_ARG;
+  if (out && (!aligned16(out->data) || out->format < ISPA_ROWS_BF16 || out->format > ISPA_ROWS_I8 ||
+              (out->format != ISPA_ROWS_BF16 && !out->scale)))
+    return ISPA_ERR_INVALID_ARG;
+  if (dim % 8 != 0 || dim > kMaxNormDim || rows > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
+  const ispa_norm none{ISPA_NORM_NONE, 0.f, nullptr, nullptr};
+  p.x = x;
+  p.rows = rows;
+  p.dim = dim;
+  p.post = post ? *post : none;
+  p.pre = pre ? *pre : none;
+  if (mod) {
+    p.scale = mod->scale;
+    p.shift = mod->shift;
+    p.mod_stride = mod->stride;
+  }
+  p.rows_per_group = mod ? mod->rows_per_group : 1;
+  if (out) {
+    p.out = out->data;
+    p.out_scale = out->scale;
+    p.format = out->format;
+  }
+  return ISPA_OK;
+}
+
 }  // namespace
 }  // namespace ispa
 
@@ -810,6 +851,88 @@ ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, const uin
   return ISPA_OK;
 }
 
+
+// ------------------------------------------------------------ norms, gate and residual
+
+ispa_status ispa_norm_modulate(const void* x, int32_t x_type, int64_t rows, int32_t dim, const ispa_norm* norm,
+                               const ispa_modulation* mod, const ispa_rows_out* out, ispa_stream stream) {
+  if (!norm || !out) return ISPA_ERR_INVALID_ARG;
+  NormParams p = {};
+  const ispa_status st = norm_params(p, x, x_type, rows, dim, nullptr, norm, mod, out);
+  if (st != ISPA_OK) return st;
+  return launch_norm(p, x_type == ISPA_FP32, false, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+ispa_status ispa_gate_residual(const void* x, int32_t x_type, const void* y, int64_t rows, int32_t dim,
+                               const ispa_norm* post, float x_scale, float y_scale, const ispa_modulation* mod,
+                               void* x_out, const ispa_norm* pre, const ispa_rows_out* out, ispa_stream stream) {
+  if (!aligned16(y) || !aligned16(x_out) || !pre != !out || !isfinite(x_scale) || !isfinite(y_scale))
+    return ISPA_ERR_INVALID_ARG;
+  NormParams p = {};
+  const ispa_status st = norm_params(p, x, x_type, rows, dim, post, pre, mod, out);
+  if (st != ISPA_OK) return st;
+  p.y = static_cast<const __nv_bfloat16*>(y);
+  p.x_out = x_out;
+  p.x_scale = x_scale;
+  p.y_scale = y_scale;
+  p.gate = mod ? mod->gate : nullptr;
+  return launch_norm(p, x_type == ISPA_FP32, true, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+// ------------------------------------------------------------ rotary positions
+
+ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows, const int32_t* pos,
+                            int64_t pos0, int64_t n, ispa_stream stream) {
+  if (!rope || !rows || !rope->steps || !pos || n_rows < 1 || n_rows > 2 || n <= 0 || rope->n_axes < 1 ||
+      rope->n_axes > ISPA_ROPE_MAX_AXES || rope->head_dim <= 0 || !isfinite(rope->factor) ||
+      (rope->layout != ISPA_ROPE_INTERLEAVED && rope->layout != ISPA_ROPE_HALF) ||
+      (reinterpret_cast<uintptr_t>(rope->steps) & 7u) || (reinterpret_cast<uintptr_t>(pos) & 3u))
+    return ISPA_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < rope->n_axes; ++a) {
+    if (rope->axis_pairs[a] < 0) return ISPA_ERR_INVALID_ARG;
+    pairs += rope->axis_pairs[a];
+  }
+  if (pairs < 1) return ISPA_ERR_INVALID_ARG;
+  for (int i = 0; i < n_rows; ++i) {
+    const ispa_rope_rows& r = rows[i];
+    if (!aligned16(r.x) || !aligned16(r.out) || r.heads <= 0 || r.norm < ISPA_QK_NORM_NONE ||
+        r.norm > ISPA_QK_NORM_TOKEN)
+      return ISPA_ERR_INVALID_ARG;
+    const int64_t width = static_cast<int64_t>(r.heads) * rope->head_dim;
+    if (r.x_stride < width || r.out_stride < width || r.x_stride % 8 != 0 || r.out_stride % 8 != 0 ||
+        (r.x == r.out && r.x_stride != r.out_stride))
+      return ISPA_ERR_INVALID_ARG;
+    if (r.norm != ISPA_QK_NORM_NONE &&
+        ((r.norm_weight && !aligned16(r.norm_weight)) || !(r.eps >= 0.f) || !isfinite(r.eps)))
+      return ISPA_ERR_INVALID_ARG;
+    if (width > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
+  }
+  if (rope->head_dim % 8 != 0 || rope->head_dim > 256 || 2 * pairs > rope->head_dim ||
+      (rope->layout == ISPA_ROPE_HALF && pairs % 8 != 0) || n > INT32_MAX)
+    return ISPA_ERR_UNSUPPORTED;
+  RopeParams p = {};
+  for (int i = 0; i < n_rows; ++i)
+    p.rows[i] = {rows[i].x, rows[i].out, rows[i].x_stride, rows[i].out_stride, rows[i].norm_weight, rows[i].eps,
+                 rows[i].heads, rows[i].norm};
+  p.n = n;
+  p.pos0 = pos0;
+  p.pos = pos;
+  p.steps = rope->steps;
+  p.head_dim = rope->head_dim;
+  p.pairs = static_cast<int32_t>(pairs);
+  p.lanes_per_head = 1;
+  while (8 * p.lanes_per_head < rope->head_dim) p.lanes_per_head *= 2;
+  p.axis_end[0] = rope->axis_pairs[0];
+  p.axis_end[1] = p.axis_end[0] + (rope->n_axes > 1 ? rope->axis_pairs[1] : 0);
+  p.factor = rope->factor;
+  return launch_rope(p, n_rows, rope->layout == ISPA_ROPE_HALF, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+ispa_status ispa_rope_steps(const ispa_rope_frequencies* f, int32_t n_pairs, uint64_t* steps, float* factor) {
+  if (!f || !steps || n_pairs < 1 || !rope_steps(*f, n_pairs, steps, factor)) return ISPA_ERR_INVALID_ARG;
+  return ISPA_OK;
+}
 
 // ------------------------------------------------------------ 8-bit Q K^T attention
 

@@ -115,6 +115,49 @@ cudaError_t launch_w8a8_gemm(const uint8_t* a_q, const float* a_scale, const uin
                              int32_t T, int32_t D, int32_t Dout, void* out, int* status, uint64_t wait_limit_ns,
                              cudaStream_t s);
 
+// ------------------------------------------------------------ norms, gate and residual
+struct NormParams {
+  const void* x;            // [rows][dim], bf16 or fp32
+  void* x_out;              // residual part: the new x (may be x)
+  const __nv_bfloat16* y;   // residual part: the block's output
+  int64_t rows;
+  int32_t dim;
+  float x_scale, y_scale;
+  ispa_norm post, pre;
+  const float* gate;        // modulation vectors of group 0, or null
+  const float* scale;
+  const float* shift;
+  int64_t mod_stride, rows_per_group;
+  void* out;                // null: the residual part alone
+  float* out_scale;
+  int32_t format;           // ISPA_ROWS_*
+};
+constexpr int kMaxNormDim = 32768;   // 512 threads of eight vectors of eight values
+cudaError_t launch_norm(const NormParams& p, bool x_fp32, bool residual, cudaStream_t s);
+
+// ------------------------------------------------------------ rotary positions
+struct RopeRowsParams {
+  const void* x;
+  void* out;
+  int64_t x_stride, out_stride;
+  const float* weight;
+  float eps;
+  int32_t heads, norm;
+};
+struct RopeParams {
+  RopeRowsParams rows[2];
+  int64_t n, pos0;
+  const int32_t* pos;       // [axes][n]
+  const uint64_t* steps;    // [pairs]
+  int32_t head_dim, pairs;
+  int32_t lanes_per_head;   // the power of two of 16-byte words that a head's lanes are dealt in
+  int32_t axis_end[2];      // pairs before axis 1 and before axis 2
+  float factor;
+};
+cudaError_t launch_rope(const RopeParams& p, int n_ops, bool half, cudaStream_t s);
+// Turns per position of n_pairs pairs (64-bit fractions) and the factor on the rotated features; false: bad arguments.
+bool rope_steps(const ispa_rope_frequencies& f, int32_t n_pairs, uint64_t* steps, float* factor);
+
 // ------------------------------------------------------------ 8-bit Q K^T
 cudaError_t launch_quant_heads(const void* x, int64_t n, int32_t H, int32_t d, uint8_t* q, float* scale,
                                cudaStream_t s);

@@ -1,0 +1,70 @@
+// Pieces shared by the kernels that work row by row (norm.cu, rope.cu): rows as vectors of eight
+// values a thread, in fp32 once loaded, and sums over a warp or over the warps of a block.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include "ptx.cuh"
+
+namespace ispa {
+
+// Eight bf16 values (one 16-byte word) as fp32, and back (round to nearest even).
+__device__ __forceinline__ void unpack8(const uint4& w, float* f) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = __uint_as_float(u[e] << 16);
+    f[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                    pack_bf16x2(f[6], f[7]));
+}
+// Eight consecutive fp32 values of a read-only array (16-byte aligned).
+__device__ __forceinline__ void load8(const float* __restrict__ p, float* f) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+}
+
+// The larger of two values; NaN if one of them is NaN, so that a row that holds one cannot pass for a finite row.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+struct SumOp {
+  static __device__ __forceinline__ float of(float a, float b) { return a + b; }
+};
+struct MaxOp {
+  static __device__ __forceinline__ float of(float a, float b) { return max_nan(a, b); }
+};
+
+// Op over the lanes of a group of `lanes` (a power of two) neighbouring lanes; every lane gets it.
+template <typename Op>
+__device__ __forceinline__ float group_reduce(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <typename Op>
+__device__ __forceinline__ float warp_reduce(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+// Op over the block's `warps` warps (at most 32); every thread gets it.  `slot` (0 or 1) alternates from one call of
+// a kernel to the next, so that one barrier a call is enough: a slot is written again only after the barrier of the
+// call in between, which every thread reaches after its reads.
+template <typename Op>
+__device__ __forceinline__ float block_reduce(float v, int warps, float (*red)[32], int slot) {
+  v = warp_reduce<Op>(v);
+  if ((threadIdx.x & 31) == 0) red[slot][threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = red[slot][0];
+  for (int i = 1; i < warps; ++i) v = Op::of(v, red[slot][i]);
+  return v;
+}
+
+}  // namespace ispa
