@@ -674,6 +674,39 @@ ISPA_API ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, 
                                       const float* w_scale, int64_t T, int32_t D, int32_t D_out, void* out,
                                       ispa_stream stream);
 
+/* ------------------------------------------------------------ projection in 8-bit integers */
+/*
+ * W8A8 with int8 codes (Sec. 4 names no 8-bit format; checkpoints quantised after training mostly hold
+ * integers), one fp32 scale per token for activations and one per output channel for weights:
+ *   amax = max |x| over the group; inv = 127 / amax and scale = amax / 127 in fp32 (both 1 for an all-zero
+ *   group); code = x * inv rounded to nearest even, in [-127, 127].
+ * A group with an infinity or a NaN has an infinite or NaN scale (its codes say nothing), so that what is
+ * computed from it is no finite number.
+ */
+
+/* Activations x: bf16 [rows][cols] -> codes q [rows][cols], scale fp32 [rows].  cols % 16 == 0 (else
+ * ISPA_ERR_UNSUPPORTED); x and q 16-byte aligned. */
+ISPA_API ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale,
+                                           ispa_stream stream);
+
+/* Weight W (+ dW, nullable): fp32 [D][D_out] (row-vector convention y = a W) -> codes q_t [D_out][D] (K-major)
+ * and scale fp32 [D_out], one per output channel of W + dW (summed in fp32).  D % 16 == 0.  Three launches;
+ * once per weight update, not per step. */
+ISPA_API ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
+                                             float* scale, ispa_stream stream);
+
+/* Largest D of ispa_linear_i8: D * 128 * 128 stays below 2^31. */
+#define ISPA_LINEAR_I8_MAX_D 131056
+
+/* out: bf16 [T][D_out] = sum_k a_q[t][k] * w_q[n][k] * a_scale[t] * w_scale[n] + bias[n].  The sum is the exact
+ * integer whatever T, for any codes in [-128, 127]; then, in fp32, each step rounded to nearest: the integer, times
+ * a_scale, times w_scale, plus bias (fp32 [D_out], NULL: none), and last to bf16.
+ * a_q [T][D], w_q [D_out][D].  D % 16 == 0, D <= ISPA_LINEAR_I8_MAX_D and D_out % 8 == 0 (else
+ * ISPA_ERR_UNSUPPORTED); a_q, w_q and out 16-byte aligned. */
+ISPA_API ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
+                                    const float* bias, int64_t T, int32_t D, int32_t D_out, void* out,
+                                    ispa_stream stream);
+
 /* ------------------------------------------------------------ norms, gate and residual */
 /*
  * What stands between a transformer block's products in a DiT layer around the chunk attention:

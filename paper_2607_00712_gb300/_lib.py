@@ -179,6 +179,10 @@ _SIGS = {
     "ispa_quantize_weight_e4m3": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
     "ispa_linear_w8a8": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_void_p,
                                    c_void_p]),
+    "ispa_quantize_rows_i8": (c_int32, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "ispa_quantize_weight_i8": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
+    "ispa_linear_i8": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_void_p,
+                                 c_void_p]),
     "ispa_norm_modulate": (c_int32, [c_void_p, c_int32, c_int64, c_int32, POINTER(Norm), POINTER(Modulation),
                                      POINTER(RowsOut), c_void_p]),
     "ispa_gate_residual": (c_int32, [c_void_p, c_int32, c_void_p, c_int64, c_int32, POINTER(Norm), c_float, c_float,
@@ -518,6 +522,22 @@ def ispa_attn_dual_qk8(ring: KVRing, k_ring_scale, win: Window, q8, q_scale, k8_
                                     _ptr(k8_cur), _ptr(k_cur_scale), _ptr(v_cur), n_q, scale, _ptr(a_full),
                                     _ptr(a_loc), _ptr(disc), _ptr(disc_sq_sum), _ptr(lse_full), _ptr(lse_loc),
                                     _ptr(workspace), ws_bytes, _stream(stream)), "ispa_attn_dual_qk8")
+
+
+# ---------------------------------------------------------------- projection in 8-bit integers
+def ispa_quantize_rows_i8(x, rows: int, cols: int, q, scale, stream=None) -> None:
+    _check(lib().ispa_quantize_rows_i8(_ptr(x), rows, cols, _ptr(q), _ptr(scale), _stream(stream)),
+           "ispa_quantize_rows_i8")
+
+
+def ispa_quantize_weight_i8(W, dW, D: int, D_out: int, q_t, scale, stream=None) -> None:
+    _check(lib().ispa_quantize_weight_i8(_ptr(W), _ptr(dW), D, D_out, _ptr(q_t), _ptr(scale), _stream(stream)),
+           "ispa_quantize_weight_i8")
+
+
+def ispa_linear_i8(a_q, a_scale, w_q, w_scale, bias, T: int, D: int, D_out: int, out, stream=None) -> None:
+    _check(lib().ispa_linear_i8(_ptr(a_q), _ptr(a_scale), _ptr(w_q), _ptr(w_scale), _ptr(bias), T, D, D_out,
+                                _ptr(out), _stream(stream)), "ispa_linear_i8")
 
 
 # ---------------------------------------------------------------- norms, gate and residual

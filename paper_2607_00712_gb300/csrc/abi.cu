@@ -225,6 +225,20 @@ bool encode_tmap_2d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_tmap_2d_u8_plain(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
+                             uint32_t b0, uint32_t b1) {
+  ensure_context();
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {d0, d1};
+  cuuint64_t strides[1] = {stride1_bytes};
+  cuuint32_t box[2] = {b0, b1};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_tmap_2d(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1,
                     uint64_t stride1_bytes, uint32_t b0, uint32_t b1) {
   ensure_context();
@@ -851,6 +865,38 @@ ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, const uin
   return ISPA_OK;
 }
 
+
+// ------------------------------------------------------------ projection in 8-bit integers
+
+ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale,
+                                  ispa_stream stream) {
+  if (!x || !q || !scale || rows <= 0 || cols <= 0 || !aligned16(x) || !aligned16(q)) return ISPA_ERR_INVALID_ARG;
+  if (cols % 16 != 0) return ISPA_ERR_UNSUPPORTED;
+  if (launch_quant_rows_i8(x, rows, cols, q, scale, stream) != cudaSuccess) return ISPA_ERR_CUDA;
+  return ISPA_OK;
+}
+
+ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
+                                    float* scale, ispa_stream stream) {
+  if (!W || !q_t || !scale || D <= 0 || D_out <= 0 || !aligned16(q_t)) return ISPA_ERR_INVALID_ARG;
+  if (D % 16 != 0) return ISPA_ERR_UNSUPPORTED;
+  if (launch_quant_weight_i8(W, dW, D, D_out, q_t, scale, stream) != cudaSuccess) return ISPA_ERR_CUDA;
+  return ISPA_OK;
+}
+
+ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
+                           const float* bias, int64_t T, int32_t D, int32_t D_out, void* out, ispa_stream stream) {
+  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || T <= 0 || T > INT32_MAX || D <= 0 || D_out <= 0 ||
+      !aligned16(out))
+    return ISPA_ERR_INVALID_ARG;
+  if (D % 16 != 0 || D > ISPA_LINEAR_I8_MAX_D || D_out % 8 != 0) return ISPA_ERR_UNSUPPORTED;
+  int* status = device_status_ptr();
+  if (!status) return ISPA_ERR_CUDA;
+  if (launch_linear_i8(a_q, a_scale, w_q, w_scale, bias, static_cast<int32_t>(T), D, D_out, out, status,
+                       g_wait_limit.load(), stream) != cudaSuccess)
+    return ISPA_ERR_CUDA;
+  return ISPA_OK;
+}
 
 // ------------------------------------------------------------ norms, gate and residual
 

@@ -115,6 +115,14 @@ cudaError_t launch_w8a8_gemm(const uint8_t* a_q, const float* a_scale, const uin
                              int32_t T, int32_t D, int32_t Dout, void* out, int* status, uint64_t wait_limit_ns,
                              cudaStream_t s);
 
+// ------------------------------------------------------------ projection in 8-bit integers
+cudaError_t launch_quant_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale, cudaStream_t s);
+cudaError_t launch_quant_weight_i8(const float* W, const float* dW, int32_t D, int32_t Dout, int8_t* q_t, float* scale,
+                                   cudaStream_t s);
+cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
+                             const float* bias, int32_t T, int32_t D, int32_t Dout, void* out, int* status,
+                             uint64_t wait_limit_ns, cudaStream_t s);
+
 // ------------------------------------------------------------ norms, gate and residual
 struct NormParams {
   const void* x;            // [rows][dim], bf16 or fp32
@@ -196,6 +204,9 @@ bool encode_tmap_2d_f32(CUtensorMap* m, const void* base, uint64_t d0, uint64_t 
 // uint8 (d0 inner, d1, d2) with 128-byte swizzle
 bool encode_tmap_3d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
                        uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t b0, uint32_t b1, uint32_t b2);
+// uint8 elements, rank 2, rows of b0 bytes one after another (no swizzle)
+bool encode_tmap_2d_u8_plain(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
+                             uint32_t b0, uint32_t b1);
 // uint8 elements, 128-byte swizzle, rank 2
 bool encode_tmap_2d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
                        uint32_t b0, uint32_t b1);

@@ -1,0 +1,513 @@
+// Projection in 8-bit integers (W8A8, Sec. 4): out[t][n] = bf16(float(sum_k a[t][k] w[n][k]) a_scale[t] w_scale[n] +
+// bias[n]) with the sum an exact 32-bit integer.
+//
+//   gemm_i8_kernel   many tokens: tensor cores
+//   gemv_i8_kernel   few tokens: dp4a, bound by the weights' way from HBM
+//
+// The tensor cores of sm_103a have no integer form (tcgen05 kind::i8 does not exist there), and mma.sync's integer
+// rate is a fraction of theirs.  But codes are exact in fp16, their products are integers up to 2^14, and the sum of
+// 1024 of them stays within 2^24, where every integer is exact in the fp32 accumulator.  So codes go through
+// kind::f16, and every 1024 of the contraction the accumulator is read back and added up in int32: the result is the
+// integer sum, bit for bit, whatever the tile shape.  Against fp8 digits (two e4m3 digits a code, three or four products
+// at twice the rate) this is the cheapest exact form: one product at the fp16 rate.
+//
+// GEMM: persistent CTAs over 128 x BN tiles, or pairs over 256 x BN tiles (cta_group::2).  Per 64 codes of the
+// contraction: TMA brings the bytes as they are (warp 0); eight warps turn them into fp16 in the 128-byte swizzle
+// that the tensor cores read (byte u = code + 128 beside 0x64 is the fp16 number 1024 + u, less 1152 the code: a
+// permute and a subtraction for two codes); warp 1 issues the UMMAs; eight warps read the accumulators back, two
+// sets in TMEM in turn.  These hold up to 128 int32 sums each thread, so the warpgroups share the registers out anew
+// (setmaxnreg).  Shared memory bounds it: a block's bytes are written by TMA, read and written as fp16 by the
+// converters and read by the UMMAs; in a pair each CTA does that for half of B.  Every wait is bounded.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "internal.h"
+#include "pdl.cuh"
+#include "ptx.cuh"
+
+namespace ispa {
+
+namespace {
+
+// ------------------------------------------------------------ few tokens
+// out[t][n] of the sum: the documented fp32 steps.
+__device__ __forceinline__ float scaled(int32_t s, float sa, float sw, float b) {
+  return __fadd_rn(__fmul_rn(__fmul_rn(__int2float_rn(s), sa), sw), b);
+}
+
+// One warp: NC output channels and up to TT tokens.  Lane l takes the 16-byte words l, l + 32, ... of the rows.
+// Block 8 warps; grid (ceil(Dout / (8 * NC)), ceil(T / TT)).
+template <int TT, int NC>
+__global__ void __launch_bounds__(256)
+    gemv_i8_kernel(const int8_t* __restrict__ a, const float* __restrict__ a_scale, const int8_t* __restrict__ w,
+                   const float* __restrict__ w_scale, const float* __restrict__ bias, int T, int D, int Dout,
+                   __nv_bfloat16* __restrict__ out) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int n0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * NC, t0 = blockIdx.y * TT;
+  if (n0 >= Dout) return;
+  const int words = D / 16;
+  int32_t acc[TT][NC] = {};
+  for (int i = lane; i < words; i += 32) {
+    int4 wv[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      wv[c] = n0 + c < Dout ? __ldg(reinterpret_cast<const int4*>(w + static_cast<int64_t>(n0 + c) * D) + i)
+                            : make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int4 av = t0 + t < T ? __ldg(reinterpret_cast<const int4*>(a + static_cast<int64_t>(t0 + t) * D) + i)
+                                 : make_int4(0, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        acc[t][c] = __dp4a(av.x, wv[c].x, __dp4a(av.y, wv[c].y, __dp4a(av.z, wv[c].z, __dp4a(av.w, wv[c].w, acc[t][c]))));
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      int32_t s = __reduce_add_sync(0xffffffffu, acc[t][c]);
+      if (lane == (t * NC + c) % 32 && t0 + t < T && n0 + c < Dout)
+        out[static_cast<int64_t>(t0 + t) * Dout + n0 + c] =
+            __float2bfloat16_rn(scaled(s, a_scale[t0 + t], w_scale[n0 + c], bias ? bias[n0 + c] : 0.f));
+    }
+}
+
+// ------------------------------------------------------------ many tokens
+constexpr int IM = 128;          // rows (tokens) of a CTA's part of a tile
+constexpr int IK = 64;           // contraction codes per block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
+constexpr int I_EXACT = 1024 / IK;   // blocks whose sums the fp32 accumulator holds exactly
+constexpr int I_CONV = 8, I_EPI = 8;   // converter and read-back warps
+constexpr int I_THREADS = 32 * (4 + I_CONV + I_EPI);
+constexpr int I_OUT_BLOCK = 32 * 64;
+constexpr uint64_t I_DRAIN_NS = 200ull * 1000 * 1000;
+// Registers a thread after the split: the first four warps, converters, read-back warps.  Their sum over the five
+// warpgroups must not exceed five times what the kernel is launched with (checked at the launch).
+constexpr int I_REGS_FIRST = 40, I_REGS_CONV = 48, I_REGS_EPI = 168;
+constexpr int I_REGS_SUM = I_REGS_FIRST + 2 * I_REGS_CONV + 2 * I_REGS_EPI;
+
+template <int BN, bool PAIR>
+struct ICfg {
+  static constexpr int CTAS = PAIR ? 2 : 1;
+  static constexpr int BR = BN / CTAS;              // this CTA's rows of B
+  static constexpr int ROWS = IM + BR;              // rows of A and B that this CTA loads and converts
+  static constexpr int RAW = ROWS * IK;             // bytes of a block as codes
+  static constexpr int F16 = ROWS * 2 * IK;         // and as fp16
+  static constexpr int ST = BR == 128 ? 4 : 5;      // stages of each kind
+  static constexpr int OFF_RAW = ST * F16;
+  static constexpr int OFF_OUT = OFF_RAW + ST * RAW;
+  static constexpr int OFF_BAR = OFF_OUT + I_EPI * 2 * I_OUT_BLOCK;
+  static constexpr int N_BAR = 4 * ST + 4 + 1;      // raw and fp16 full / empty, set full / empty, drain
+  static constexpr int SMEM = OFF_BAR + N_BAR * 8 + 16;
+  static_assert(SMEM > 116 * 1024 && SMEM <= 232448, "one CTA per SM");
+  static_assert(F16 % 1024 == 0 && RAW % 128 == 0 && OFF_OUT % 128 == 0, "shared memory layout");
+  static_assert(BN % 64 == 0 && 2 * BN <= 512, "two accumulator sets fit in TMEM");
+  // fp16 operands (format 0), fp32 accumulator
+  static constexpr uint32_t IDESC = (1u << 4) | (static_cast<uint32_t>(BN >> 3) << 17) |
+                                    (static_cast<uint32_t>((IM * CTAS) >> 4) << 24);
+};
+
+struct LinearParams {
+  int32_t T, Dout, n_kb;
+  int32_t n_mt, n_tiles;   // row tiles; all tiles (tile t: rows (t % n_mt), columns (t / n_mt))
+  int32_t split;           // CTAs that share a tile's blocks (SPLIT)
+  const float* a_scale;
+  const float* w_scale;
+  const float* bias;
+  __nv_bfloat16* out;
+  int* status;
+  uint64_t wait_limit_ns;
+};
+
+// mbar_wait (CLUSTER: for arrivals from the pair's other CTA) with its polling loop in line: a kernel that shares its
+// registers out anew cannot call functions.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const WaitCtx& w, int site, int detail) {
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if ((i & 63) == 0) {
+      if (*w.abort) return false;
+      if (globaltimer_ns() - t0 > w.limit_ns) {
+        *w.abort = 1;
+        record_error(w.status, DEVERR_TIMEOUT, site, bar, parity, detail);
+        return false;
+      }
+    }
+  }
+}
+
+// Four codes as four fp16 numbers.
+__device__ __forceinline__ uint2 f16_of(uint32_t w) {
+  const uint32_t u = w ^ 0x80808080u;   // code + 128
+  uint32_t lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+  const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+  __half2 l = __hsub2(*reinterpret_cast<__half2*>(&lo), off), h = __hsub2(*reinterpret_cast<__half2*>(&hi), off);
+  return make_uint2(*reinterpret_cast<uint32_t*>(&l), *reinterpret_cast<uint32_t*>(&h));
+}
+
+template <int BN, bool PAIR, bool SPLIT>
+__global__ void __launch_bounds__(I_THREADS, 1)
+    gemm_i8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
+                   const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ LinearParams p) {
+  using C = ICfg<BN, PAIR>;
+  constexpr int ST = C::ST;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = smem_raw;
+  const uint32_t sbase = smem_u32(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::N_BAR);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const uint32_t rawf0 = smem_u32(bars), rawe0 = rawf0 + 8 * ST, f16f0 = rawe0 + 8 * ST, f16e0 = f16f0 + 8 * ST,
+                 accf0 = f16e0 + 8 * ST, acce0 = accf0 + 16, drain_bar = acce0 + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
+  const int ctas = SPLIT ? p.split : C::CTAS, unit = blockIdx.x / ctas, units = gridDim.x / ctas;
+  const int part = SPLIT ? static_cast<int>(cluster_ctarank()) : 0;
+  const int kb0 = SPLIT ? p.n_kb * part / p.split : 0, kb1 = SPLIT ? p.n_kb * (part + 1) / p.split : p.n_kb;
+  if (sbase & 1023u) {   // the same for every CTA of a launch
+    if (threadIdx.x == 0) record_error(p.status, DEVERR_LAYOUT, 0, sbase, 0, 2);
+    return;
+  }
+  // A pair's rank 0 issues the UMMAs: its fp16-full and set-empty barriers count both CTAs' warps.  Loads count on
+  // their own CTA's barriers alone.  The fp16-empty, set-full and drain barriers are each CTA's own, arrived at by
+  // commits that go to both.
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(rawf0 + 8 * i, 1);
+      mbar_init(rawe0 + 8 * i, I_CONV);
+      mbar_init(f16f0 + 8 * i, I_CONV * C::CTAS);
+      mbar_init(f16e0 + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(accf0 + 8 * i, 1);
+      mbar_init(acce0 + 8 * i, I_EPI * C::CTAS);
+    }
+    mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if constexpr (PAIR) cluster_sync();   // both CTAs run and their barriers exist
+  if (warp == 1) {
+    if constexpr (PAIR) {
+      tmem_alloc_pair(smem_u32(tmem_slot), 512);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(tmem_slot), 512);
+      tmem_relinquish();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (PAIR) cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();   // the codes and scales may come from the kernel before this one
+  pdl_trigger();
+  const WaitCtx wc{abort_flag, p.status, p.wait_limit_ns};
+
+  if (warp < 4) {
+    regs_dec<I_REGS_FIRST>();
+    if (warp == 0) {
+      // ---------------------------------------------------------- TMA producer
+      if (lane == 0) {
+        int g = 0;   // blocks issued over all tiles of this CTA
+        bool ok = true;
+        for (int t = unit; ok && t < p.n_tiles; t += units) {
+          const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + rank * C::BR;
+          for (int kb = kb0; kb < kb1; ++kb, ++g) {
+            const int st = g % ST;
+            if (!wait_for(rawe0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 41, g)) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(rawf0 + 8 * st, C::RAW);
+            const uint32_t dst = sbase + C::OFF_RAW + st * C::RAW;
+            tma_load_2d(dst, &tm_a, rawf0 + 8 * st, kb * IK, m0);
+            tma_load_2d(dst + IM * IK, &tm_w, rawf0 + 8 * st, kb * IK, n0);
+          }
+        }
+        for (int i = g > ST ? g - ST : 0; i < g; ++i)
+          mbar_wait_drain(rawf0 + 8 * (i % ST), (i / ST) & 1, I_DRAIN_NS);
+      }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- UMMA issuer
+      if (lane == 0 && rank == 0) {
+        int g = 0, i = 0;   // blocks; accumulator sets filled
+        bool ok = true;
+        for (int t = unit; ok && t < p.n_tiles; t += units) {
+          for (int c0 = kb0; ok && c0 < kb1; c0 += I_EXACT, ++i) {
+            const int set = i & 1, c1 = min(c0 + I_EXACT, kb1);
+            if (!wait_for<PAIR>(acce0 + 8 * set, ((i >> 1) & 1) ^ 1, wc, 44, i)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t acc = tmem + set * BN;
+            for (int kb = c0; kb < c1; ++kb, ++g) {
+              const int st = g % ST;
+              if (!wait_for<PAIR>(f16f0 + 8 * st, (g / ST) & 1, wc, 42, g)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              const uint32_t sa = sbase + st * C::F16, sb = sa + IM * 2 * IK;
+#pragma unroll
+              for (int k = 0; k < IK / 16; ++k) {   // 16 fp16 = 32 bytes inside the swizzle row
+                const uint64_t da = sw128_desc(sa + 32 * k, 16, 1024), db = sw128_desc(sb + 32 * k, 16, 1024);
+                const uint32_t more = kb > c0 || k > 0 ? 1u : 0u;
+                if constexpr (PAIR) umma_ss_pair(acc, da, db, C::IDESC, more);
+                else umma_ss(acc, da, db, C::IDESC, more);
+              }
+              if constexpr (PAIR) tc_commit_pair(f16e0 + 8 * st);
+              else tc_commit(f16e0 + 8 * st);
+            }
+            if (!ok) break;
+            if constexpr (PAIR) tc_commit_pair(accf0 + 8 * set);
+            else tc_commit(accf0 + 8 * set);
+          }
+        }
+        if constexpr (PAIR) tc_commit_pair(drain_bar);
+        else tc_commit(drain_bar);
+      }
+      if (lane == 0) mbar_wait_drain(drain_bar, 0, rank == 0 ? I_DRAIN_NS : p.wait_limit_ns + 2 * I_DRAIN_NS);
+    }
+    __syncwarp();
+  } else if (warp < 4 + I_CONV) {
+    // ------------------------------------------------------------ converters
+    regs_dec<I_REGS_CONV>();
+    const int w = warp - 4;
+    int g = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < p.n_tiles; t += units) {
+      for (int kb = kb0; kb < kb1; ++kb, ++g) {
+        const int st = g % ST;
+        if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * st, (g / ST) & 1, wc, 45, g) &&
+                                         wait_for(f16e0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 46, g))) {
+          ok = false;
+          break;
+        }
+        const uint8_t* src = smem + C::OFF_RAW + st * C::RAW;
+        uint8_t* dst = smem + st * C::F16;
+        // A warp takes eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and
+        // write, of two neighbouring rows, the even (then the odd) 16-byte words, which the swizzle puts into
+        // eight different bank groups.
+#pragma unroll
+        for (int j = 0; j < (C::ROWS / 8 + I_CONV - 1) / I_CONV; ++j) {
+          const int r = (j * I_CONV + w) * 8 + (lane >> 2), q = lane & 3;
+          if (r < C::ROWS) {   // uniform over the warp
+            const uint4 v = *reinterpret_cast<const uint4*>(src + r * IK + q * 16);
+            const uint2 x0 = f16_of(v.x), x1 = f16_of(v.y), x2 = f16_of(v.z), x3 = f16_of(v.w);
+            uint8_t* row = dst + r * 2 * IK;
+            *reinterpret_cast<uint4*>(row + (((2 * q) ^ (r & 7)) * 16)) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+            *reinterpret_cast<uint4*>(row + (((2 * q + 1) ^ (r & 7)) * 16)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+          }
+        }
+        fence_proxy_async_smem();   // each lane's own stores, before the UMMAs read them
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(rawe0 + 8 * st);
+          if constexpr (PAIR) mbar_arrive_cluster(cluster_map(f16f0 + 8 * st, 0));
+          else mbar_arrive(f16f0 + 8 * st);
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ read-back
+    regs_inc<I_REGS_EPI>();
+    constexpr int HC = BN / 64;   // 32-column chunks of this warp's half
+    const int quarter = warp & 3, half = (warp - 4 - I_CONV) >> 2;
+    uint8_t* block = smem + C::OFF_OUT + (warp - 4 - I_CONV) * 2 * I_OUT_BLOCK;
+    int i = 0, stores = 0;   // sets read; blocks stored (they alternate on across tiles, wherever one ends)
+    bool ok = true;
+    for (int t = unit; ok && t < p.n_tiles; t += units) {
+      const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + half * (BN / 2);
+      int32_t sum[HC * 32];
+#pragma unroll
+      for (int e = 0; e < HC * 32; ++e) sum[e] = 0;
+      for (int c0 = kb0; c0 < kb1; c0 += I_EXACT, ++i) {
+        const int set = i & 1;
+        if (!__all_sync(0xffffffffu, wait_for(accf0 + 8 * set, (i >> 1) & 1, wc, 43, i))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + set * BN + half * (BN / 2);
+#pragma unroll
+        for (int c = 0; c < 2 * HC; ++c) {
+          uint32_t v[16];
+          tmem_ld16(taddr + 16 * c, v);
+          tmem_wait_ld16(v);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[16 * c + e] += __float2int_rn(__uint_as_float(v[e]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) mbar_arrive_cluster(cluster_map(acce0 + 8 * set, 0));
+          else mbar_arrive(acce0 + 8 * set);
+        }
+      }
+      if (!ok) break;
+      if constexpr (SPLIT) {
+        // the partial sums into the fp16 stages, which have been read: 16-byte word q of row r at q ^ (r & 7)
+        int4* x = reinterpret_cast<int4*>(smem) + (quarter * 32 + lane) * (BN / 4);
+#pragma unroll
+        for (int q = 0; q < HC * 8; ++q)
+          x[(half * (BN / 8) + q) ^ (lane & 7)] =
+              make_int4(sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]);
+        break;   // a split tile's CTA has no other
+      }
+      if (m0 + quarter * 32 >= p.T) continue;   // uniform over the warp; rows past T inside the block are clipped
+      const float sa = m0 + quarter * 32 + lane < p.T ? p.a_scale[m0 + quarter * 32 + lane] : 0.f;
+#pragma unroll
+      for (int c = 0; c < HC; ++c) {
+        if (n0 + 32 * c >= p.Dout) break;       // uniform
+        const int n = n0 + 32 * c + lane;
+        const float sw = n < p.Dout ? p.w_scale[n] : 0.f, bi = p.bias && n < p.Dout ? p.bias[n] : 0.f;
+        uint8_t* b = block + (stores++ & 1) * I_OUT_BLOCK;
+        if (lane == 0) bulk_wait_read<1>();     // the store before last, this block's last, has read it
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int o = 8 * q + 2 * e;
+            pk[e] = pack_bf16x2(
+                scaled(sum[32 * c + o], sa, __shfl_sync(0xffffffffu, sw, o), __shfl_sync(0xffffffffu, bi, o)),
+                scaled(sum[32 * c + o + 1], sa, __shfl_sync(0xffffffffu, sw, o + 1), __shfl_sync(0xffffffffu, bi, o + 1)));
+          }
+          // 64-byte swizzle: 16-byte word q of row r at word q ^ (r / 2 mod 4)
+          *reinterpret_cast<uint4*>(b + lane * 64 + (q ^ ((lane >> 1) & 3)) * 16) =
+              make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(&tm_out, smem_u32(b), n0 + 32 * c, m0 + quarter * 32);
+          bulk_commit_group();
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (SPLIT) {
+    static_assert(!SPLIT || BN == 128, "a row is four columns a lane");
+    cluster_sync();   // every CTA's partial sums are in its shared memory
+    if (warp >= 4 + I_CONV) {
+      const int m0 = unit % p.n_mt * IM, n0 = unit / p.n_mt * BN + 4 * lane;
+      float sw[4], bi[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sw[e] = n0 + e < p.Dout ? p.w_scale[n0 + e] : 0.f;
+        bi[e] = p.bias && n0 + e < p.Dout ? p.bias[n0 + e] : 0.f;
+      }
+      // one warp per row of this CTA's share; Dout is a multiple of 8, so a lane's four columns are all in or all out
+      for (int r = IM * part / p.split + warp - 4 - I_CONV; r < IM * (part + 1) / p.split && m0 + r < p.T; r += I_EPI) {
+        const uint32_t x = sbase + (r * (BN / 4) + (lane ^ (r & 7))) * 16;
+        int4 o = make_int4(0, 0, 0, 0);
+        for (int i = 0; i < p.split; ++i) {
+          const float4 v = cluster_ld4(cluster_map(x, i));
+          o.x += __float_as_int(v.x);
+          o.y += __float_as_int(v.y);
+          o.z += __float_as_int(v.z);
+          o.w += __float_as_int(v.w);
+        }
+        const float sa = p.a_scale[m0 + r];
+        if (n0 < p.Dout)
+          *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(m0 + r) * p.Dout + n0) =
+              make_uint2(pack_bf16x2(scaled(o.x, sa, sw[0], bi[0]), scaled(o.y, sa, sw[1], bi[1])),
+                         pack_bf16x2(scaled(o.z, sa, sw[2], bi[2]), scaled(o.w, sa, sw[3], bi[3])));
+      }
+    }
+    cluster_sync();   // no CTA leaves while another still reads its shared memory
+  }
+  if constexpr (PAIR) cluster_sync();   // neither CTA's TMEM, barriers or shared memory is used by the other any more
+  if (warp == 1) {
+    tc_fence_after();
+    if constexpr (PAIR) tmem_dealloc_pair(tmem, 512);
+    else tmem_dealloc(tmem, 512);
+  }
+}
+
+// The register split of gemm_i8_kernel fits into what its blocks are launched with.
+cudaError_t check_registers(const void* func) {
+  cudaFuncAttributes attr;
+  const cudaError_t e = cudaFuncGetAttributes(&attr, func);
+  if (e != cudaSuccess) return e;
+  return attr.numRegs * 5 >= I_REGS_SUM ? cudaSuccess : cudaErrorInvalidConfiguration;
+}
+
+template <int BN, bool PAIR, bool SPLIT = false>
+cudaError_t launch_gemm(int split, const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
+                        const float* bias, int32_t T, int32_t D, int32_t Dout, __nv_bfloat16* out, int* status,
+                        uint64_t wait_limit_ns, int sms, cudaStream_t s) {
+  using C = ICfg<BN, PAIR>;
+  const void* func = reinterpret_cast<const void*>(gemm_i8_kernel<BN, PAIR, SPLIT>);
+  static const cudaError_t registers = check_registers(func);   // of the code, the same on every device
+  if (registers != cudaSuccess) return registers;
+  const cudaError_t e = set_smem_limit_once(func, C::SMEM);
+  if (e != cudaSuccess) return e;
+  CUtensorMap ta, tw, to;
+  if (!encode_tmap_2d_u8_plain(&ta, a_q, D, T, D, IK, IM) || !encode_tmap_2d_u8_plain(&tw, w_q, D, Dout, D, IK, C::BR) ||
+      !encode_tmap_2d_sw64(&to, out, Dout, T, 2 * static_cast<uint64_t>(Dout), 32, 32))
+    return cudaErrorInvalidValue;
+  LinearParams p;
+  p.T = T;
+  p.Dout = Dout;
+  p.n_kb = (D + IK - 1) / IK;   // past D the loads fill with zeros
+  p.n_mt = (T + IM * C::CTAS - 1) / (IM * C::CTAS);
+  p.n_tiles = p.n_mt * ((Dout + BN - 1) / BN);
+  p.split = split;
+  p.a_scale = a_scale;
+  p.w_scale = w_scale;
+  p.bias = bias;
+  p.out = out;
+  p.status = status;
+  p.wait_limit_ns = wait_limit_ns;
+  const int ctas = SPLIT ? split : C::CTAS, units = SPLIT ? p.n_tiles : std::min(p.n_tiles, sms / ctas);
+  return launch_pdl_cluster(gemm_i8_kernel<BN, PAIR, SPLIT>, dim3(units * ctas), dim3(I_THREADS), C::SMEM, ctas, s, ta,
+                            tw, to, p);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
+                             const float* bias, int32_t T, int32_t D, int32_t Dout, void* out, int* status,
+                             uint64_t wait_limit_ns, cudaStream_t s) {
+  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out);
+  int dev = 0, sms = 152;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (T <= 8) {
+    const auto go = [&](auto kernel, int tt, int nc) {
+      return launch_pdl(kernel, dim3((Dout + 8 * nc - 1) / (8 * nc), (T + tt - 1) / tt), dim3(256), 0, s, a_q, a_scale, w_q,
+                        w_scale, bias, static_cast<int>(T), static_cast<int>(D), static_cast<int>(Dout), o);
+    };
+    return T == 1 ? go(gemv_i8_kernel<1, 1>, 1, 1) : T <= 4 ? go(gemv_i8_kernel<4, 2>, 4, 2) : go(gemv_i8_kernel<8, 2>, 8, 2);
+  }
+  const int64_t m_tiles = (static_cast<int64_t>(T) + IM - 1) / IM, n_kb = (D + IK - 1) / IK;
+  const int64_t tiles = m_tiles * ((Dout + 127) / 128);
+  int split = 1;
+  for (const int c : {2, 4, 8})
+    if (n_kb >= 2 * c && tiles * c <= sms) split = c;
+  if (split > 1)
+    return launch_gemm<128, false, true>(split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
+                                         sms, s);
+  if (tiles <= sms)
+    return launch_gemm<128, false>(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
+  return launch_gemm<256, true>(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
+}
+
+}  // namespace ispa

@@ -10,7 +10,8 @@
 //
 // Quantisation arithmetic (fp32, rounded to nearest at every step, identical to the
 // oracle's): amax = max |x|; inv = 448 / amax, scale = amax / 448 (both 1 for an all-zero
-// group); code = e4m3(x * inv), round to nearest even with saturation at +-448.
+// group); code = e4m3(x * inv), round to nearest even with saturation at +-448.  The same kernels
+// make the int8 codes of linear_i8.cu (127 in 448's place, rounded to the nearest even integer).
 //
 // GEMM: persistent, one CTA per SM looping over 128 x BN output tiles (BN = 256, 192 or 128), or one pair of
 // CTAs over 256 x 256 tiles (cta_group::2), whichever gives the shortest estimated run; both operands
@@ -33,12 +34,15 @@
 #include "internal.h"
 #include "pdl.cuh"
 #include "ptx.cuh"
+#include "rows.cuh"
 
 namespace ispa {
 
 namespace {
 
-constexpr float kE4M3Max = 448.f;
+// Largest magnitude of a code: e4m3, or (I8) int8 used symmetrically.
+template <bool I8>
+constexpr float kCodeMax = I8 ? 127.f : 448.f;
 
 // Two fp32 values -> two e4m3 codes (round to nearest even, saturating), x0 in the low byte.
 __device__ __forceinline__ uint16_t e4m3x2(float x0, float x1) {
@@ -47,10 +51,23 @@ __device__ __forceinline__ uint16_t e4m3x2(float x0, float x1) {
   return r;
 }
 
+// The larger magnitude; of int8 groups NaN if there is one (their codes have none).
+template <bool I8>
+__device__ __forceinline__ float amax_of(float a, float b) {
+  return I8 ? max_nan(a, b) : fmaxf(a, b);
+}
+
+// Two fp32 values -> two codes, x0 in the low byte.
+template <bool I8>
+__device__ __forceinline__ uint16_t code2(float x0, float x1) {
+  if constexpr (I8) return static_cast<uint16_t>((__float2int_rn(x0) & 0xFF) | (__float2int_rn(x1) & 0xFF) << 8);
+  else return e4m3x2(x0, x1);
+}
+
 // One warp per row (grid-stride over rows); cols % 8 == 0.  Rows of up to 32 * CACHE
 // 16-byte words (8 bf16 each) stay in registers between the max and the quantisation pass;
 // of longer rows the rest is read twice.
-template <int CACHE>
+template <int CACHE, bool I8>
 __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <= 8 ? 3 : 2)
     quant_rows_kernel(const __nv_bfloat16* __restrict__ x, int64_t rows, int cols, uint8_t* __restrict__ q,
                       float* __restrict__ scale) {
@@ -73,28 +90,30 @@ __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xFFFF0000u))));
+        amax = amax_of<I8>(amax, amax_of<I8>(fabsf(__uint_as_float(w[e] << 16)),
+                                             fabsf(__uint_as_float(w[e] & 0xFFFF0000u))));
     }
 #pragma unroll
     for (int c = 0; c < CACHE; ++c) {
       const uint32_t w[4] = {cache[c].x, cache[c].y, cache[c].z, cache[c].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xFFFF0000u))));
+        amax = amax_of<I8>(amax, amax_of<I8>(fabsf(__uint_as_float(w[e] << 16)),
+                                             fabsf(__uint_as_float(w[e] & 0xFFFF0000u))));
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const float inv = amax == 0.f ? 1.f : __fdiv_rn(kE4M3Max, amax);
+    for (int o = 16; o > 0; o >>= 1) amax = amax_of<I8>(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const float inv = amax == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, amax);
     uint2* qr = reinterpret_cast<uint2*>(q + r * cols);
     auto quant8 = [&](const uint4& v) {
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
       uint32_t out[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint16_t lo = e4m3x2(__fmul_rn(__uint_as_float(w[2 * h] << 16), inv),
-                                   __fmul_rn(__uint_as_float(w[2 * h] & 0xFFFF0000u), inv));
-        const uint16_t hi = e4m3x2(__fmul_rn(__uint_as_float(w[2 * h + 1] << 16), inv),
-                                   __fmul_rn(__uint_as_float(w[2 * h + 1] & 0xFFFF0000u), inv));
+        const uint16_t lo = code2<I8>(__fmul_rn(__uint_as_float(w[2 * h] << 16), inv),
+                                      __fmul_rn(__uint_as_float(w[2 * h] & 0xFFFF0000u), inv));
+        const uint16_t hi = code2<I8>(__fmul_rn(__uint_as_float(w[2 * h + 1] << 16), inv),
+                                      __fmul_rn(__uint_as_float(w[2 * h + 1] & 0xFFFF0000u), inv));
         out[h] = static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
       }
       return make_uint2(out[0], out[1]);
@@ -105,7 +124,7 @@ __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <
       if (i < nw) qr[i] = quant8(cache[c]);
     }
     for (int i = lane + 32 * CACHE; i < nw; i += 32) qr[i] = quant8(xr[i]);
-    if (lane == 0) scale[r] = amax == 0.f ? 1.f : __fdiv_rn(amax, kE4M3Max);
+    if (lane == 0) scale[r] = amax == 0.f ? 1.f : __fdiv_rn(amax, kCodeMax<I8>);
   }
 }
 
@@ -114,37 +133,39 @@ __device__ __forceinline__ float w_plus_dw(const float* W, const float* dW, int6
 }
 
 // Per-column max |W + dW| into amax[D_out].  Block (32, 8) per 32 columns.
+template <bool I8>
 __global__ void col_amax_kernel(const float* __restrict__ W, const float* __restrict__ dW, int D, int Dout,
                                 float* __restrict__ amax) {
   __shared__ float red[8][33];
   const int n = blockIdx.x * 32 + threadIdx.x;
   float m = 0.f;
   if (n < Dout)
-    for (int k = threadIdx.y; k < D; k += 8) m = fmaxf(m, fabsf(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n)));
+    for (int k = threadIdx.y; k < D; k += 8) m = amax_of<I8>(m, fabsf(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n)));
   red[threadIdx.y][threadIdx.x] = m;
   __syncthreads();
   if (threadIdx.y == 0 && n < Dout) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = fmaxf(m, red[i][threadIdx.x]);
+    for (int i = 1; i < 8; ++i) m = amax_of<I8>(m, red[i][threadIdx.x]);
     amax[n] = m;
   }
 }
 
-// codes[n][k] = e4m3((W + dW)[k][n] * inv_n) through a 32 x 32 shared-memory transpose.
+// codes[n][k] = code((W + dW)[k][n] * inv_n) through a 32 x 32 shared-memory transpose.
 // Block (32, 8); grid (ceil(D / 32), ceil(Dout / 32)).
+template <bool I8>
 __global__ void quant_wt_kernel(const float* __restrict__ W, const float* __restrict__ dW, int D, int Dout,
                                 const float* __restrict__ amax, uint8_t* __restrict__ q_t) {
   __shared__ uint8_t tile[32][36];
   const int k0 = blockIdx.x * 32, n0 = blockIdx.y * 32;
   const int n = n0 + threadIdx.x;
   const float am = n < Dout ? amax[n] : 0.f;
-  const float inv = am == 0.f ? 1.f : __fdiv_rn(kE4M3Max, am);
+  const float inv = am == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, am);
   for (int j = threadIdx.y; j < 32; j += 8) {
     const int k = k0 + j;
     uint8_t c = 0;
     if (k < D && n < Dout) {
       const float v = __fmul_rn(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n), inv);
-      c = static_cast<uint8_t>(e4m3x2(v, 0.f) & 0xFF);
+      c = static_cast<uint8_t>(code2<I8>(v, 0.f) & 0xFF);
     }
     tile[j][threadIdx.x] = c;   // [k][n]
   }
@@ -155,9 +176,10 @@ __global__ void quant_wt_kernel(const float* __restrict__ W, const float* __rest
   }
 }
 
+template <bool I8>
 __global__ void col_scale_kernel(float* __restrict__ s, int Dout) {
   const int n = blockIdx.x * blockDim.x + threadIdx.x;
-  if (n < Dout) s[n] = s[n] == 0.f ? 1.f : __fdiv_rn(s[n], kE4M3Max);
+  if (n < Dout) s[n] = s[n] == 0.f ? 1.f : __fdiv_rn(s[n], kCodeMax<I8>);
 }
 
 // ------------------------------------------------------------ GEMM
@@ -519,7 +541,10 @@ cudaError_t launch_gemm_bn(int split, const uint8_t* a_q, const float* a_scale, 
 
 }  // namespace
 
-cudaError_t launch_quant_rows(const void* x, int64_t rows, int32_t cols, uint8_t* q, float* scale, cudaStream_t s) {
+namespace {
+
+template <bool I8>
+cudaError_t launch_rows(const void* x, int64_t rows, int32_t cols, uint8_t* q, float* scale, cudaStream_t s) {
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -529,20 +554,38 @@ cudaError_t launch_quant_rows(const void* x, int64_t rows, int32_t cols, uint8_t
   // at once.  4680 x 1536: 4.4 -> 3.2 us, 9400 x 1024: 7.0 -> 4.0 (against 12 words a lane for every row).  Rows of
   // more than 3072 values keep 12 and read the rest twice: with 20 only 8 warps a SM fit, 8.1 -> 10.2 us at 5120.
   const int words = (cols / 8 + 31) / 32;
-  const auto kernel = words <= 4   ? quant_rows_kernel<4>
-                      : words <= 6 ? quant_rows_kernel<6>
-                      : words <= 8 ? quant_rows_kernel<8>
-                                   : quant_rows_kernel<12>;
+  const auto kernel = words <= 4   ? quant_rows_kernel<4, I8>
+                      : words <= 6 ? quant_rows_kernel<6, I8>
+                      : words <= 8 ? quant_rows_kernel<8, I8>
+                                   : quant_rows_kernel<12, I8>;
   return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s,
                     static_cast<const __nv_bfloat16*>(x), rows, static_cast<int>(cols), q, scale);
 }
 
+template <bool I8>
+cudaError_t launch_weight(const float* W, const float* dW, int32_t D, int32_t Dout, uint8_t* q_t, float* scale,
+                          cudaStream_t s) {
+  col_amax_kernel<I8><<<(Dout + 31) / 32, dim3(32, 8), 0, s>>>(W, dW, D, Dout, scale);
+  quant_wt_kernel<I8><<<dim3((D + 31) / 32, (Dout + 31) / 32), dim3(32, 8), 0, s>>>(W, dW, D, Dout, scale, q_t);
+  col_scale_kernel<I8><<<(Dout + 255) / 256, 256, 0, s>>>(scale, Dout);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_quant_rows(const void* x, int64_t rows, int32_t cols, uint8_t* q, float* scale, cudaStream_t s) {
+  return launch_rows<false>(x, rows, cols, q, scale, s);
+}
+cudaError_t launch_quant_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale, cudaStream_t s) {
+  return launch_rows<true>(x, rows, cols, reinterpret_cast<uint8_t*>(q), scale, s);
+}
 cudaError_t launch_quant_weight(const float* W, const float* dW, int32_t D, int32_t Dout, uint8_t* q_t, float* scale,
                                 cudaStream_t s) {
-  col_amax_kernel<<<(Dout + 31) / 32, dim3(32, 8), 0, s>>>(W, dW, D, Dout, scale);
-  quant_wt_kernel<<<dim3((D + 31) / 32, (Dout + 31) / 32), dim3(32, 8), 0, s>>>(W, dW, D, Dout, scale, q_t);
-  col_scale_kernel<<<(Dout + 255) / 256, 256, 0, s>>>(scale, Dout);
-  return cudaGetLastError();
+  return launch_weight<false>(W, dW, D, Dout, q_t, scale, s);
+}
+cudaError_t launch_quant_weight_i8(const float* W, const float* dW, int32_t D, int32_t Dout, int8_t* q_t, float* scale,
+                                   cudaStream_t s) {
+  return launch_weight<true>(W, dW, D, Dout, reinterpret_cast<uint8_t*>(q_t), scale, s);
 }
 
 cudaError_t launch_w8a8_gemm(const uint8_t* a_q, const float* a_scale, const uint8_t* w_q, const float* w_scale,

@@ -89,6 +89,21 @@ def test_residual_refusals():
     assert call(post=abi.norm(7)) == BAD
 
 
+def test_linear_i8_refusals():
+    def call(a=16, sa=16, w=16, sw=16, bias=None, T=10, D=64, N=64, out=16):
+        return _status(lambda: abi.ispa_linear_i8(a, sa, w, sw, bias, T, D, N, out))
+
+    assert call(a=None) == BAD and call(a=24) == BAD and call(w=None) == BAD and call(w=8) == BAD
+    assert call(sa=None) == BAD and call(sw=None) == BAD and call(out=None) == BAD and call(out=24) == BAD
+    assert call(T=0) == BAD and call(T=2 ** 31) == BAD and call(D=0) == BAD and call(N=0) == BAD
+    assert call(D=72) == UNSUP and call(N=36) == UNSUP and call(D=131072) == UNSUP
+    assert _status(lambda: abi.ispa_quantize_rows_i8(16, 10, 24, 16, 16)) == UNSUP
+    assert _status(lambda: abi.ispa_quantize_rows_i8(None, 10, 32, 16, 16)) == BAD
+    assert _status(lambda: abi.ispa_quantize_rows_i8(16, 0, 32, 16, 16)) == BAD
+    assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 24, 32, 16, 16)) == UNSUP
+    assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 32, 0, 16, 16)) == BAD
+
+
 def test_rope_refusals():
     rope = abi.rope(0, 64, [32], 16)
     rows = abi.rope_rows(16, 16, 2, 128, 128)
