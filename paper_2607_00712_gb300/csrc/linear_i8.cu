@@ -84,6 +84,7 @@ constexpr int IM = 128;          // rows (tokens) of a CTA's part of a tile
 constexpr int IK = 64;           // contraction codes per block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
 constexpr int I_EXACT = 1024 / IK;   // blocks whose sums the fp32 accumulator holds exactly
 constexpr int I_CONV = 8, I_EPI = 8;   // converter and read-back warps
+constexpr int I_PER = 2;               // converter warps that share a block
 constexpr int I_THREADS = 32 * (4 + I_CONV + I_EPI);
 constexpr int I_OUT_BLOCK = 32 * 64;
 constexpr uint64_t I_DRAIN_NS = 200ull * 1000 * 1000;
@@ -181,8 +182,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < ST; ++i) {
       mbar_init(rawf0 + 8 * i, 1);
-      mbar_init(rawe0 + 8 * i, I_CONV);
-      mbar_init(f16f0 + 8 * i, I_CONV * C::CTAS);
+      mbar_init(rawe0 + 8 * i, I_PER);
+      mbar_init(f16f0 + 8 * i, I_PER * C::CTAS);
       mbar_init(f16e0 + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -282,40 +283,43 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   } else if (warp < 4 + I_CONV) {
     // ------------------------------------------------------------ converters
     regs_dec<I_REGS_CONV>();
-    const int w = warp - 4;
-    int g = 0;
-    bool ok = true;
-    for (int t = unit; ok && t < p.n_tiles; t += units) {
-      for (int kb = kb0; kb < kb1; ++kb, ++g) {
-        const int st = g % ST;
-        if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * st, (g / ST) & 1, wc, 45, g) &&
-                                         wait_for(f16e0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 46, g))) {
-          ok = false;
-          break;
-        }
-        const uint8_t* src = smem + C::OFF_RAW + st * C::RAW;
-        uint8_t* dst = smem + st * C::F16;
-        // A warp takes eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and
-        // write, of two neighbouring rows, the even (then the odd) 16-byte words, which the swizzle puts into
-        // eight different bank groups.
+    // I_PER warps a block, each team its own blocks: the waits, the fence and the arrivals of one block hide behind the
+    // other teams' work.
+    const int w = (warp - 4) % I_PER, rows_step = 8 * I_PER;
+    const int n = (unit < p.n_tiles ? (p.n_tiles - 1 - unit) / units + 1 : 0) * (kb1 - kb0);   // this CTA's blocks
+    // A warp takes eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and
+    // write, of two neighbouring rows, the even (then the odd) 16-byte words, which the swizzle puts into eight
+    // different bank groups.
+    const int r = 8 * w + (lane >> 2), q = lane & 3;
+    const uint32_t even = ((2 * q) ^ (r & 7)) * 16, odd = ((2 * q + 1) ^ (r & 7)) * 16;
+    for (int g = (warp - 4) / I_PER; g < n; g += I_CONV / I_PER) {
+      const int st = g % ST;
+      if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * st, (g / ST) & 1, wc, 45, g) &&
+                                       wait_for(f16e0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 46, g)))
+        break;
+      const uint8_t* src = smem + C::OFF_RAW + st * C::RAW + r * IK + q * 16;
+      uint8_t* dst = smem + st * C::F16 + r * 2 * IK;
+      constexpr int STEPS = C::ROWS / (8 * I_PER);
+      static_assert(C::ROWS % (8 * I_PER) == 0 && STEPS % 2 == 0, "rows of a team");
 #pragma unroll
-        for (int j = 0; j < (C::ROWS / 8 + I_CONV - 1) / I_CONV; ++j) {
-          const int r = (j * I_CONV + w) * 8 + (lane >> 2), q = lane & 3;
-          if (r < C::ROWS) {   // uniform over the warp
-            const uint4 v = *reinterpret_cast<const uint4*>(src + r * IK + q * 16);
-            const uint2 x0 = f16_of(v.x), x1 = f16_of(v.y), x2 = f16_of(v.z), x3 = f16_of(v.w);
-            uint8_t* row = dst + r * 2 * IK;
-            *reinterpret_cast<uint4*>(row + (((2 * q) ^ (r & 7)) * 16)) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-            *reinterpret_cast<uint4*>(row + (((2 * q + 1) ^ (r & 7)) * 16)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-          }
+      for (int j = 0; j < STEPS; j += 2) {
+        const uint4 v0 = *reinterpret_cast<const uint4*>(src + j * rows_step * IK);
+        const uint4 v1 = *reinterpret_cast<const uint4*>(src + (j + 1) * rows_step * IK);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint4 v = k ? v1 : v0;
+          const uint2 x0 = f16_of(v.x), x1 = f16_of(v.y), x2 = f16_of(v.z), x3 = f16_of(v.w);
+          uint8_t* row = dst + (j + k) * rows_step * 2 * IK;
+          *reinterpret_cast<uint4*>(row + even) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+          *reinterpret_cast<uint4*>(row + odd) = make_uint4(x2.x, x2.y, x3.x, x3.y);
         }
-        fence_proxy_async_smem();   // each lane's own stores, before the UMMAs read them
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(rawe0 + 8 * st);
-          if constexpr (PAIR) mbar_arrive_cluster(cluster_map(f16f0 + 8 * st, 0));
-          else mbar_arrive(f16f0 + 8 * st);
-        }
+      }
+      fence_proxy_async_smem();   // each lane's own stores, before the UMMAs read them
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(rawe0 + 8 * st);
+        if constexpr (PAIR) mbar_arrive_cluster(cluster_map(f16f0 + 8 * st, 0));
+        else mbar_arrive(f16f0 + 8 * st);
       }
     }
   } else {
