@@ -90,7 +90,7 @@ constexpr int I_OUT_BLOCK = 32 * 64;
 constexpr uint64_t I_DRAIN_NS = 200ull * 1000 * 1000;
 // Registers a thread after the split: the first four warps, converters, read-back warps.  Their sum over the five
 // warpgroups must not exceed five times what the kernel is launched with (checked at the launch).
-constexpr int I_REGS_FIRST = 40, I_REGS_CONV = 48, I_REGS_EPI = 168;
+constexpr int I_REGS_FIRST = 32, I_REGS_CONV = 56, I_REGS_EPI = 168;
 constexpr int I_REGS_SUM = I_REGS_FIRST + 2 * I_REGS_CONV + 2 * I_REGS_EPI;
 
 template <int BN, bool PAIR>
@@ -100,11 +100,15 @@ struct ICfg {
   static constexpr int ROWS = IM + BR;              // rows of A and B that this CTA loads and converts
   static constexpr int RAW = ROWS * IK;             // bytes of a block as codes
   static constexpr int F16 = ROWS * 2 * IK;         // and as fp16
-  static constexpr int ST = BR == 128 ? 4 : 5;      // stages of each kind
-  static constexpr int OFF_RAW = ST * F16;
-  static constexpr int OFF_OUT = OFF_RAW + ST * RAW;
-  static constexpr int OFF_BAR = OFF_OUT + I_EPI * 2 * I_OUT_BLOCK;
-  static constexpr int N_BAR = 4 * ST + 4 + 1;      // raw and fp16 full / empty, set full / empty, drain
+  static constexpr int FST = 4, RST = 4;            // stages of fp16 and of codes
+  // A team waits for a stage of codes knowing that its own last block has landed, and for an fp16 stage knowing that the
+  // UMMAs have read all blocks up to its own last one less FST.  Parities tell two uses of a stage apart, not three: the
+  // stage's use before must be one that the team knows of.
+  static_assert(RST % (I_CONV / I_PER) == 0 && FST >= I_CONV / I_PER, "parities stay unambiguous");
+  static constexpr int OFF_RAW = FST * F16;
+  static constexpr int OFF_OUT = OFF_RAW + RST * RAW;
+  static constexpr int OFF_BAR = OFF_OUT + I_EPI * I_OUT_BLOCK;
+  static constexpr int N_BAR = 2 * RST + 2 * FST + 4 + 1;   // codes and fp16 full / empty, set full / empty, drain
   static constexpr int SMEM = OFF_BAR + N_BAR * 8 + 16;
   static_assert(SMEM > 116 * 1024 && SMEM <= 232448, "one CTA per SM");
   static_assert(F16 % 1024 == 0 && RAW % 128 == 0 && OFF_OUT % 128 == 0, "shared memory layout");
@@ -158,15 +162,15 @@ __global__ void __launch_bounds__(I_THREADS, 1)
     gemm_i8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
                    const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ LinearParams p) {
   using C = ICfg<BN, PAIR>;
-  constexpr int ST = C::ST;
+  constexpr int RST = C::RST, FST = C::FST;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw;
   const uint32_t sbase = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::N_BAR);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  const uint32_t rawf0 = smem_u32(bars), rawe0 = rawf0 + 8 * ST, f16f0 = rawe0 + 8 * ST, f16e0 = f16f0 + 8 * ST,
-                 accf0 = f16e0 + 8 * ST, acce0 = accf0 + 16, drain_bar = acce0 + 16;
+  const uint32_t rawf0 = smem_u32(bars), rawe0 = rawf0 + 8 * RST, f16f0 = rawe0 + 8 * RST, f16e0 = f16f0 + 8 * FST,
+                 accf0 = f16e0 + 8 * FST, acce0 = accf0 + 16, drain_bar = acce0 + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
   const int ctas = SPLIT ? p.split : C::CTAS, unit = blockIdx.x / ctas, units = gridDim.x / ctas;
@@ -180,9 +184,11 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   // their own CTA's barriers alone.  The fp16-empty, set-full and drain barriers are each CTA's own, arrived at by
   // commits that go to both.
   if (threadIdx.x == 0) {
-    for (int i = 0; i < ST; ++i) {
+    for (int i = 0; i < RST; ++i) {
       mbar_init(rawf0 + 8 * i, 1);
       mbar_init(rawe0 + 8 * i, I_PER);
+    }
+    for (int i = 0; i < FST; ++i) {
       mbar_init(f16f0 + 8 * i, I_PER * C::CTAS);
       mbar_init(f16e0 + 8 * i, 1);
     }
@@ -223,8 +229,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         for (int t = unit; ok && t < p.n_tiles; t += units) {
           const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + rank * C::BR;
           for (int kb = kb0; kb < kb1; ++kb, ++g) {
-            const int st = g % ST;
-            if (!wait_for(rawe0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 41, g)) {
+            const int st = g % RST;
+            if (!wait_for(rawe0 + 8 * st, ((g / RST) & 1) ^ 1, wc, 41, g)) {
               ok = false;
               break;
             }
@@ -234,8 +240,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
             tma_load_2d(dst + IM * IK, &tm_w, rawf0 + 8 * st, kb * IK, n0);
           }
         }
-        for (int i = g > ST ? g - ST : 0; i < g; ++i)
-          mbar_wait_drain(rawf0 + 8 * (i % ST), (i / ST) & 1, I_DRAIN_NS);
+        for (int i = g > RST ? g - RST : 0; i < g; ++i)
+          mbar_wait_drain(rawf0 + 8 * (i % RST), (i / RST) & 1, I_DRAIN_NS);
       }
     } else if (warp == 1) {
       // ---------------------------------------------------------- UMMA issuer
@@ -252,8 +258,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
             tc_fence_after();
             const uint32_t acc = tmem + set * BN;
             for (int kb = c0; kb < c1; ++kb, ++g) {
-              const int st = g % ST;
-              if (!wait_for<PAIR>(f16f0 + 8 * st, (g / ST) & 1, wc, 42, g)) {
+              const int st = g % FST;
+              if (!wait_for<PAIR>(f16f0 + 8 * st, (g / FST) & 1, wc, 42, g)) {
                 ok = false;
                 break;
               }
@@ -293,33 +299,40 @@ __global__ void __launch_bounds__(I_THREADS, 1)
     const int r = 8 * w + (lane >> 2), q = lane & 3;
     const uint32_t even = ((2 * q) ^ (r & 7)) * 16, odd = ((2 * q + 1) ^ (r & 7)) * 16;
     for (int g = (warp - 4) / I_PER; g < n; g += I_CONV / I_PER) {
-      const int st = g % ST;
-      if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * st, (g / ST) & 1, wc, 45, g) &&
-                                       wait_for(f16e0 + 8 * st, ((g / ST) & 1) ^ 1, wc, 46, g)))
-        break;
-      const uint8_t* src = smem + C::OFF_RAW + st * C::RAW + r * IK + q * 16;
-      uint8_t* dst = smem + st * C::F16 + r * 2 * IK;
-      constexpr int STEPS = C::ROWS / (8 * I_PER);
-      static_assert(C::ROWS % (8 * I_PER) == 0 && STEPS % 2 == 0, "rows of a team");
+      const int rs = g % RST, fs = g % FST;
+      if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * rs, (g / RST) & 1, wc, 45, g))) break;
+      const uint8_t* src = smem + C::OFF_RAW + rs * C::RAW + r * IK + q * 16;
+      uint8_t* dst = smem + fs * C::F16 + r * 2 * IK;
+      constexpr int STEPS = C::ROWS / (8 * I_PER), BATCH = STEPS % 4 == 0 ? 4 : STEPS % 2 == 0 ? 2 : STEPS;
+      static_assert(C::ROWS % (8 * I_PER) == 0 && STEPS % BATCH == 0, "rows of a team");
+      bool free = false;
 #pragma unroll
-      for (int j = 0; j < STEPS; j += 2) {
-        const uint4 v0 = *reinterpret_cast<const uint4*>(src + j * rows_step * IK);
-        const uint4 v1 = *reinterpret_cast<const uint4*>(src + (j + 1) * rows_step * IK);
+      for (int j0 = 0; j0 < STEPS; j0 += BATCH) {
+        uint4 v[BATCH];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint4 v = k ? v1 : v0;
-          const uint2 x0 = f16_of(v.x), x1 = f16_of(v.y), x2 = f16_of(v.z), x3 = f16_of(v.w);
-          uint8_t* row = dst + (j + k) * rows_step * 2 * IK;
+        for (int j = 0; j < BATCH; ++j) v[j] = *reinterpret_cast<const uint4*>(src + (j0 + j) * rows_step * IK);
+        if (j0 == 0) {
+          free = __all_sync(0xffffffffu, wait_for(f16e0 + 8 * fs, ((g / FST) & 1) ^ 1, wc, 46, g));
+          if (!free) break;
+        }
+        if (j0 + BATCH == STEPS) {
+          __syncwarp();   // every lane has its codes
+          if (lane == 0) mbar_arrive(rawe0 + 8 * rs);
+        }
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+          const uint2 x0 = f16_of(v[j].x), x1 = f16_of(v[j].y), x2 = f16_of(v[j].z), x3 = f16_of(v[j].w);
+          uint8_t* row = dst + (j0 + j) * rows_step * 2 * IK;
           *reinterpret_cast<uint4*>(row + even) = make_uint4(x0.x, x0.y, x1.x, x1.y);
           *reinterpret_cast<uint4*>(row + odd) = make_uint4(x2.x, x2.y, x3.x, x3.y);
         }
       }
+      if (!free) break;
       fence_proxy_async_smem();   // each lane's own stores, before the UMMAs read them
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(rawe0 + 8 * st);
-        if constexpr (PAIR) mbar_arrive_cluster(cluster_map(f16f0 + 8 * st, 0));
-        else mbar_arrive(f16f0 + 8 * st);
+        if constexpr (PAIR) mbar_arrive_cluster_own(cluster_map(f16f0 + 8 * fs, 0));
+        else mbar_arrive(f16f0 + 8 * fs);
       }
     }
   } else {
@@ -327,8 +340,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
     regs_inc<I_REGS_EPI>();
     constexpr int HC = BN / 64;   // 32-column chunks of this warp's half
     const int quarter = warp & 3, half = (warp - 4 - I_CONV) >> 2;
-    uint8_t* block = smem + C::OFF_OUT + (warp - 4 - I_CONV) * 2 * I_OUT_BLOCK;
-    int i = 0, stores = 0;   // sets read; blocks stored (they alternate on across tiles, wherever one ends)
+    uint8_t* block = smem + C::OFF_OUT + (warp - 4 - I_CONV) * I_OUT_BLOCK;
+    int i = 0;   // sets read
     bool ok = true;
     for (int t = unit; ok && t < p.n_tiles; t += units) {
       const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + half * (BN / 2);
@@ -375,8 +388,7 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         if (n0 + 32 * c >= p.Dout) break;       // uniform
         const int n = n0 + 32 * c + lane;
         const float sw = n < p.Dout ? p.w_scale[n] : 0.f, bi = p.bias && n < p.Dout ? p.bias[n] : 0.f;
-        uint8_t* b = block + (stores++ & 1) * I_OUT_BLOCK;
-        if (lane == 0) bulk_wait_read<1>();     // the store before last, this block's last, has read it
+        if (lane == 0) bulk_wait_read_all();    // the store before has read the block
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -389,13 +401,13 @@ __global__ void __launch_bounds__(I_THREADS, 1)
                 scaled(sum[32 * c + o + 1], sa, __shfl_sync(0xffffffffu, sw, o + 1), __shfl_sync(0xffffffffu, bi, o + 1)));
           }
           // 64-byte swizzle: 16-byte word q of row r at word q ^ (r / 2 mod 4)
-          *reinterpret_cast<uint4*>(b + lane * 64 + (q ^ ((lane >> 1) & 3)) * 16) =
+          *reinterpret_cast<uint4*>(block + lane * 64 + (q ^ ((lane >> 1) & 3)) * 16) =
               make_uint4(pk[0], pk[1], pk[2], pk[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          tma_store_2d(&tm_out, smem_u32(b), n0 + 32 * c, m0 + quarter * 32);
+          tma_store_2d(&tm_out, smem_u32(block), n0 + 32 * c, m0 + quarter * 32);
           bulk_commit_group();
         }
       }
@@ -485,6 +497,42 @@ cudaError_t launch_gemm(int split, const int8_t* a_q, const float* a_scale, cons
                             tw, to, p);
 }
 
+struct GemmChoice {
+  int bn;
+  bool pair;
+  int split;
+};
+
+GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms) {
+  struct Shape {
+    int bn, ctas, block_ns, start_ns;
+  };
+  static constexpr Shape kShapes[4] = {{256, 2, 400, 4800}, {192, 2, 340, 4800}, {128, 2, 300, 4800}, {128, 1, 400, 3000}};
+  const int64_t n_kb = (D + IK - 1) / IK;
+  GemmChoice best{128, false, 1};
+  int64_t best_cost = INT64_MAX;
+  for (const Shape& f : kShapes) {
+    if (sms < f.ctas) continue;
+    const int64_t rows = IM * f.ctas, units = sms / f.ctas;
+    const int64_t tiles = (T + rows - 1) / rows * ((Dout + f.bn - 1) / f.bn);
+    const int64_t cost = (tiles + units - 1) / units * (n_kb * f.block_ns + 360) + f.start_ns;
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = {f.bn, f.ctas == 2, 1};
+    }
+  }
+  for (const int c : {2, 4, 8}) {
+    const int64_t tiles = (T + IM - 1) / IM * ((Dout + 127) / 128);
+    if (n_kb < c || tiles * c * (c > 2 ? 5 : 4) > 4 * static_cast<int64_t>(sms)) break;
+    const int64_t cost = (n_kb + c - 1) / c * 400 + 360 + 3000 + 2500 + 50 * c;
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = {128, false, c};
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
@@ -501,17 +549,13 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
     };
     return T == 1 ? go(gemv_i8_kernel<1, 1>, 1, 1) : T <= 4 ? go(gemv_i8_kernel<4, 2>, 4, 2) : go(gemv_i8_kernel<8, 2>, 8, 2);
   }
-  const int64_t m_tiles = (static_cast<int64_t>(T) + IM - 1) / IM, n_kb = (D + IK - 1) / IK;
-  const int64_t tiles = m_tiles * ((Dout + 127) / 128);
-  int split = 1;
-  for (const int c : {2, 4, 8})
-    if (n_kb >= 2 * c && tiles * c <= sms) split = c;
-  if (split > 1)
-    return launch_gemm<128, false, true>(split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
+  const GemmChoice g = choose_gemm(T, D, Dout, sms);
+  if (g.split > 1)
+    return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
                                          sms, s);
-  if (tiles <= sms)
-    return launch_gemm<128, false>(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
-  return launch_gemm<256, true>(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
+  const auto run = !g.pair ? launch_gemm<128, false>
+                   : g.bn == 256 ? launch_gemm<256, true> : g.bn == 192 ? launch_gemm<192, true> : launch_gemm<128, true>;
+  return run(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
 }
 
 }  // namespace ispa

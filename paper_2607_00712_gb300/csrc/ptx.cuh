@@ -473,6 +473,13 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The same where what it releases is the arriving CTA's own shared memory, written through the generic proxy, fenced
+// (fence_proxy_async_smem) and read by that same SM's tensor core when the pair's UMMA runs: ordering within the
+// arriving CTA is enough, and the wider release is a memory barrier that waits about a microsecond.
+__device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // ---------------------------------------------------------------- descriptors
 // UMMA shared-memory matrix descriptor, 128-byte swizzle (the layout TMA writes
 // with CU_TENSOR_MAP_SWIZZLE_128B).  Fields: start address >> 4 (bits 0-13),
