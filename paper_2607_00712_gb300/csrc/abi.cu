@@ -225,8 +225,8 @@ bool encode_tmap_2d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool encode_tmap_2d_u8_plain(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
-                             uint32_t b0, uint32_t b1) {
+bool encode_tmap_2d_u8_rows(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
+                            uint32_t b0, uint32_t b1, bool sw64) {
   ensure_context();
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
@@ -235,7 +235,7 @@ bool encode_tmap_2d_u8_plain(CUtensorMap* m, const void* base, uint64_t d0, uint
   cuuint32_t box[2] = {b0, b1};
   cuuint32_t estr[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, sw64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -204,9 +204,9 @@ bool encode_tmap_2d_f32(CUtensorMap* m, const void* base, uint64_t d0, uint64_t 
 // uint8 (d0 inner, d1, d2) with 128-byte swizzle
 bool encode_tmap_3d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
                        uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t b0, uint32_t b1, uint32_t b2);
-// uint8 elements, rank 2, rows of b0 bytes one after another (no swizzle)
-bool encode_tmap_2d_u8_plain(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
-                             uint32_t b0, uint32_t b1);
+// uint8 elements, rank 2, rows of b0 bytes one after another: no swizzle, or 64-byte swizzle (b0 = 64)
+bool encode_tmap_2d_u8_rows(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
+                            uint32_t b0, uint32_t b1, bool sw64);
 // uint8 elements, 128-byte swizzle, rank 2
 bool encode_tmap_2d_u8(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t stride1_bytes,
                        uint32_t b0, uint32_t b1);

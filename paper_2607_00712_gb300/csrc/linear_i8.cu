@@ -83,39 +83,39 @@ __global__ void __launch_bounds__(256)
 constexpr int IM = 128;          // rows (tokens) of a CTA's part of a tile
 constexpr int IK = 64;           // contraction codes per block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
 constexpr int I_EXACT = 1024 / IK;   // blocks whose sums the fp32 accumulator holds exactly
-constexpr int I_CONV = 8, I_EPI = 8;   // converter and read-back warps
-constexpr int I_PER = 2;               // converter warps that share a block
+constexpr int I_CONV = 12, I_EPI = 8;   // converter and read-back warps
+constexpr int I_TEAMS = I_CONV / 4;    // four converter warps, one per TMEM lane quarter, share a block
 constexpr int I_THREADS = 32 * (4 + I_CONV + I_EPI);
 constexpr int I_OUT_BLOCK = 32 * 64;
 constexpr uint64_t I_DRAIN_NS = 200ull * 1000 * 1000;
-// Registers a thread after the split: the first four warps, converters, read-back warps.  Their sum over the five
-// warpgroups must not exceed five times what the kernel is launched with (checked at the launch).
-constexpr int I_REGS_FIRST = 32, I_REGS_CONV = 56, I_REGS_EPI = 168;
-constexpr int I_REGS_SUM = I_REGS_FIRST + 2 * I_REGS_CONV + 2 * I_REGS_EPI;
 
 template <int BN, bool PAIR>
 struct ICfg {
   static constexpr int CTAS = PAIR ? 2 : 1;
   static constexpr int BR = BN / CTAS;              // this CTA's rows of B
-  static constexpr int ROWS = IM + BR;              // rows of A and B that this CTA loads and converts
-  static constexpr int RAW = ROWS * IK;             // bytes of a block as codes
-  static constexpr int F16 = ROWS * 2 * IK;         // and as fp16
-  static constexpr int FST = 4, RST = 4;            // stages of fp16 and of codes
+  static constexpr int RAW = (IM + BR) * IK;        // bytes of a block as codes
+  static constexpr int B16 = BR * 2 * IK;           // of its part of B as fp16
+  static constexpr int FST = 4, RST = BR == 128 ? 6 : 9;   // stages of fp16 (A in TMEM, B in shared memory) and of codes
   // A team waits for a stage of codes knowing that its own last block has landed, and for an fp16 stage knowing that the
   // UMMAs have read all blocks up to its own last one less FST.  Parities tell two uses of a stage apart, not three: the
   // stage's use before must be one that the team knows of.
-  static_assert(RST % (I_CONV / I_PER) == 0 && FST >= I_CONV / I_PER, "parities stay unambiguous");
-  static constexpr int OFF_RAW = FST * F16;
+  static_assert(RST % I_TEAMS == 0 && FST >= I_TEAMS, "parities stay unambiguous");
+  static constexpr int A_COL = 512 - FST * IK / 2;  // TMEM columns of A's stages: two fp16 a column
+  static_assert(2 * BN <= A_COL, "two accumulator sets and A fit in TMEM");
+  static constexpr int OFF_RAW = FST * B16;
   static constexpr int OFF_OUT = OFF_RAW + RST * RAW;
   static constexpr int OFF_BAR = OFF_OUT + I_EPI * I_OUT_BLOCK;
   static constexpr int N_BAR = 2 * RST + 2 * FST + 4 + 1;   // codes and fp16 full / empty, set full / empty, drain
   static constexpr int SMEM = OFF_BAR + N_BAR * 8 + 16;
   static_assert(SMEM > 116 * 1024 && SMEM <= 232448, "one CTA per SM");
-  static_assert(F16 % 1024 == 0 && RAW % 128 == 0 && OFF_OUT % 128 == 0, "shared memory layout");
-  static_assert(BN % 64 == 0 && 2 * BN <= 512, "two accumulator sets fit in TMEM");
+  static_assert(B16 % 1024 == 0 && RAW % 512 == 0 && OFF_OUT % 512 == 0 && BR % 32 == 0, "shared memory layout");
   // fp16 operands (format 0), fp32 accumulator
   static constexpr uint32_t IDESC = (1u << 4) | (static_cast<uint32_t>(BN >> 3) << 17) |
                                     (static_cast<uint32_t>((IM * CTAS) >> 4) << 24);
+  // Registers a thread after the split: the first four warps, converters, read-back warps (BN / 2 of theirs are sums).
+  // Their sum over the warpgroups must not exceed what the kernel is launched with (checked at the launch).
+  static constexpr int REGS_FIRST = 40, REGS_CONV = 56, REGS_EPI = 136;
+  static constexpr int REGS_SUM = REGS_FIRST + I_CONV / 4 * REGS_CONV + I_EPI / 4 * REGS_EPI;
 };
 
 struct LinearParams {
@@ -130,22 +130,36 @@ struct LinearParams {
   uint64_t wait_limit_ns;
 };
 
-// mbar_wait (CLUSTER: for arrivals from the pair's other CTA) with its polling loop in line: a kernel that shares its
-// registers out anew cannot call functions.
+// A converged warp's test of a barrier (CLUSTER: that the pair's other CTA arrives at too), the same answer in every
+// lane, and its bounded wait (as mbar_wait, with the polling loop in line: a kernel that shares its registers out anew
+// cannot call functions).  The test never suspends the warp; the wait's polls do, for up to microseconds.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const WaitCtx& w, int site, int detail) {
-  const uint64_t t0 = globaltimer_ns();
-  for (uint32_t i = 1;; ++i) {
-    if (CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, CLUSTER ? mbar_test_wait_cluster(bar, parity) : mbar_test_wait(bar, parity));
+}
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& w, int site, int detail) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;
+       !__all_sync(0xffffffffu, CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)); ++i) {
     if ((i & 63) == 0) {
-      if (*w.abort) return false;
-      if (globaltimer_ns() - t0 > w.limit_ns) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      const bool late = now - t0 > w.limit_ns;
+      if (late && (threadIdx.x & 31) == 0) {
         *w.abort = 1;
         record_error(w.status, DEVERR_TIMEOUT, site, bar, parity, detail);
-        return false;
       }
+      if (__any_sync(0xffffffffu, late || *w.abort != 0)) return false;
     }
   }
+  return true;
+}
+
+// mbar_wait_drain by a converged warp; the timer, hundreds of cycles a reading, only for what has not landed yet.
+__device__ __forceinline__ void warp_drain(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+  if (!warp_test(bar, parity) && (threadIdx.x & 31) == 0) mbar_wait_drain(bar, parity, limit_ns);
+  __syncwarp();
 }
 
 // Four codes as four fp16 numbers.
@@ -186,10 +200,10 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < RST; ++i) {
       mbar_init(rawf0 + 8 * i, 1);
-      mbar_init(rawe0 + 8 * i, I_PER);
+      mbar_init(rawe0 + 8 * i, 4);
     }
     for (int i = 0; i < FST; ++i) {
-      mbar_init(f16f0 + 8 * i, I_PER * C::CTAS);
+      mbar_init(f16f0 + 8 * i, 4 * C::CTAS);
       mbar_init(f16e0 + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -220,124 +234,148 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   const WaitCtx wc{abort_flag, p.status, p.wait_limit_ns};
 
   if (warp < 4) {
-    regs_dec<I_REGS_FIRST>();
+    regs_dec<C::REGS_FIRST>();
     if (warp == 0) {
       // ---------------------------------------------------------- TMA producer
-      if (lane == 0) {
-        int g = 0;   // blocks issued over all tiles of this CTA
-        bool ok = true;
-        for (int t = unit; ok && t < p.n_tiles; t += units) {
-          const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + rank * C::BR;
-          for (int kb = kb0; kb < kb1; ++kb, ++g) {
-            const int st = g % RST;
-            if (!wait_for(rawe0 + 8 * st, ((g / RST) & 1) ^ 1, wc, 41, g)) {
-              ok = false;
-              break;
-            }
+      const bool leader = elect_one();
+      int g = 0;   // blocks issued over all tiles of this CTA
+      bool ok = true;
+      for (int t = unit; ok && t < p.n_tiles; t += units) {
+        const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + rank * C::BR;
+        for (int kb = kb0; kb < kb1; ++kb, ++g) {
+          const int st = g % RST;
+          if (!warp_wait(rawe0 + 8 * st, ((g / RST) & 1) ^ 1, wc, 41, g)) {
+            ok = false;
+            break;
+          }
+          const uint32_t dst = sbase + C::OFF_RAW + st * C::RAW;
+          if (leader) {
             mbar_arrive_expect_tx(rawf0 + 8 * st, C::RAW);
-            const uint32_t dst = sbase + C::OFF_RAW + st * C::RAW;
             tma_load_2d(dst, &tm_a, rawf0 + 8 * st, kb * IK, m0);
             tma_load_2d(dst + IM * IK, &tm_w, rawf0 + 8 * st, kb * IK, n0);
           }
+          __syncwarp();
         }
-        for (int i = g > RST ? g - RST : 0; i < g; ++i)
-          mbar_wait_drain(rawf0 + 8 * (i % RST), (i / RST) & 1, I_DRAIN_NS);
       }
+      for (int i = g > RST ? g - RST : 0; i < g; ++i)
+        warp_drain(rawf0 + 8 * (i % RST), (i / RST) & 1, I_DRAIN_NS);
     } else if (warp == 1) {
       // ---------------------------------------------------------- UMMA issuer
-      if (lane == 0 && rank == 0) {
-        int g = 0, i = 0;   // blocks; accumulator sets filled
-        bool ok = true;
+      if (rank == 0) {
+        const bool leader = elect_one();
+        const uint64_t desc0 = sw128_desc(sbase, 16, 1024);   // + bytes / 16 inside the 256 KB window
+        int g = 0, i = 0;      // blocks; accumulator sets filled
+        bool ok = true, next = false;   // next: the next block is known to be there
         for (int t = unit; ok && t < p.n_tiles; t += units) {
           for (int c0 = kb0; ok && c0 < kb1; c0 += I_EXACT, ++i) {
             const int set = i & 1, c1 = min(c0 + I_EXACT, kb1);
-            if (!wait_for<PAIR>(acce0 + 8 * set, ((i >> 1) & 1) ^ 1, wc, 44, i)) {
+            if (!warp_wait<PAIR>(acce0 + 8 * set, ((i >> 1) & 1) ^ 1, wc, 44, i)) {
               ok = false;
               break;
             }
-            tc_fence_after();
             const uint32_t acc = tmem + set * BN;
             for (int kb = c0; kb < c1; ++kb, ++g) {
               const int st = g % FST;
-              if (!wait_for<PAIR>(f16f0 + 8 * st, (g / FST) & 1, wc, 42, g)) {
+              if (!next && !warp_wait<PAIR>(f16f0 + 8 * st, (g / FST) & 1, wc, 42, g)) {
                 ok = false;
                 break;
               }
               tc_fence_after();
-              const uint32_t sa = sbase + st * C::F16, sb = sa + IM * 2 * IK;
+              const uint32_t ta = tmem + C::A_COL + st * (IK / 2);
+              const uint64_t db = desc0 + static_cast<uint64_t>(st * C::B16 / 16);
+              if (leader) {
 #pragma unroll
-              for (int k = 0; k < IK / 16; ++k) {   // 16 fp16 = 32 bytes inside the swizzle row
-                const uint64_t da = sw128_desc(sa + 32 * k, 16, 1024), db = sw128_desc(sb + 32 * k, 16, 1024);
-                const uint32_t more = kb > c0 || k > 0 ? 1u : 0u;
-                if constexpr (PAIR) umma_ss_pair(acc, da, db, C::IDESC, more);
-                else umma_ss(acc, da, db, C::IDESC, more);
+                for (int k = 0; k < IK / 16; ++k) {   // 16 fp16: 8 TMEM columns of A, 32 bytes inside B's swizzle row
+                  const uint32_t more = kb > c0 || k > 0 ? 1u : 0u;
+                  if constexpr (PAIR) umma_ts_pair(acc, ta + 8 * k, db + 2 * k, C::IDESC, more);
+                  else umma_ts(acc, ta + 8 * k, db + 2 * k, C::IDESC, more);
+                }
+                if constexpr (PAIR) tc_commit_pair(f16e0 + 8 * st);
+                else tc_commit(f16e0 + 8 * st);
               }
-              if constexpr (PAIR) tc_commit_pair(f16e0 + 8 * st);
-              else tc_commit(f16e0 + 8 * st);
+              __syncwarp();
+              next = warp_test<PAIR>(f16f0 + 8 * ((g + 1) % FST), ((g + 1) / FST) & 1);
             }
             if (!ok) break;
-            if constexpr (PAIR) tc_commit_pair(accf0 + 8 * set);
-            else tc_commit(accf0 + 8 * set);
+            if (leader) {
+              if constexpr (PAIR) tc_commit_pair(accf0 + 8 * set);
+              else tc_commit(accf0 + 8 * set);
+            }
+            __syncwarp();
           }
         }
-        if constexpr (PAIR) tc_commit_pair(drain_bar);
-        else tc_commit(drain_bar);
+        if (leader) {
+          if constexpr (PAIR) tc_commit_pair(drain_bar);
+          else tc_commit(drain_bar);
+        }
+        __syncwarp();
       }
-      if (lane == 0) mbar_wait_drain(drain_bar, 0, rank == 0 ? I_DRAIN_NS : p.wait_limit_ns + 2 * I_DRAIN_NS);
+      warp_drain(drain_bar, 0, rank == 0 ? I_DRAIN_NS : p.wait_limit_ns + 2 * I_DRAIN_NS);
     }
     __syncwarp();
   } else if (warp < 4 + I_CONV) {
     // ------------------------------------------------------------ converters
-    regs_dec<I_REGS_CONV>();
-    // I_PER warps a block, each team its own blocks: the waits, the fence and the arrivals of one block hide behind the
-    // other teams' work.
-    const int w = (warp - 4) % I_PER, rows_step = 8 * I_PER;
+    regs_dec<C::REGS_CONV>();
+    // Each team its own blocks: the waits, the fence and the arrivals of one block hide behind the other team's work.
+    const int quarter = warp & 3;
     const int n = (unit < p.n_tiles ? (p.n_tiles - 1 - unit) / units + 1 : 0) * (kb1 - kb0);   // this CTA's blocks
-    // A warp takes eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and
-    // write, of two neighbouring rows, the even (then the odd) 16-byte words, which the swizzle puts into eight
-    // different bank groups.
-    const int r = 8 * w + (lane >> 2), q = lane & 3;
-    const uint32_t even = ((2 * q) ^ (r & 7)) * 16, odd = ((2 * q + 1) ^ (r & 7)) * 16;
-    for (int g = (warp - 4) / I_PER; g < n; g += I_CONV / I_PER) {
+    // A: a lane a row, 64 codes; the 64-byte swizzle puts 16-byte word c of row r at word c ^ (r / 2 mod 4), so that eight
+    // rows' words lie in eight different bank groups.
+    const int ra = quarter * 32 + lane, xa = (ra >> 1) & 3;
+    // B: eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and write, of two
+    // neighbouring rows, the even (then the odd) 16-byte words, which the 128-byte swizzle puts into eight different
+    // bank groups.
+    const int rb = 8 * quarter + (lane >> 2), q = lane & 3;
+    const uint32_t even = ((2 * q) ^ (rb & 7)) * 16, odd = ((2 * q + 1) ^ (rb & 7)) * 16;
+    for (int g = (warp - 4) / 4; g < n; g += I_TEAMS) {
       const int rs = g % RST, fs = g % FST;
-      if (!__all_sync(0xffffffffu, wait_for(rawf0 + 8 * rs, (g / RST) & 1, wc, 45, g))) break;
-      const uint8_t* src = smem + C::OFF_RAW + rs * C::RAW + r * IK + q * 16;
-      uint8_t* dst = smem + fs * C::F16 + r * 2 * IK;
-      constexpr int STEPS = C::ROWS / (8 * I_PER), BATCH = STEPS % 4 == 0 ? 4 : STEPS % 2 == 0 ? 2 : STEPS;
-      static_assert(C::ROWS % (8 * I_PER) == 0 && STEPS % BATCH == 0, "rows of a team");
-      bool free = false;
+      if (!warp_wait(rawf0 + 8 * rs, (g / RST) & 1, wc, 45, g) ||
+          !warp_wait(f16e0 + 8 * fs, ((g / FST) & 1) ^ 1, wc, 46, g))
+        break;
+      tc_fence_after();
+      const uint8_t* src = smem + C::OFF_RAW + rs * C::RAW;
+      const uint32_t ta = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + C::A_COL + fs * (IK / 2);
 #pragma unroll
-      for (int j0 = 0; j0 < STEPS; j0 += BATCH) {
-        uint4 v[BATCH];
+      for (int h = 0; h < 2; ++h) {
+        uint32_t x[16];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) v[j] = *reinterpret_cast<const uint4*>(src + (j0 + j) * rows_step * IK);
-        if (j0 == 0) {
-          free = __all_sync(0xffffffffu, wait_for(f16e0 + 8 * fs, ((g / FST) & 1) ^ 1, wc, 46, g));
-          if (!free) break;
-        }
-        if (j0 + BATCH == STEPS) {
-          __syncwarp();   // every lane has its codes
-          if (lane == 0) mbar_arrive(rawe0 + 8 * rs);
-        }
+        for (int c = 0; c < 2; ++c) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src + ra * IK + ((2 * h + c) ^ xa) * 16);
+          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          const uint2 x0 = f16_of(v[j].x), x1 = f16_of(v[j].y), x2 = f16_of(v[j].z), x3 = f16_of(v[j].w);
-          uint8_t* row = dst + (j0 + j) * rows_step * 2 * IK;
-          *reinterpret_cast<uint4*>(row + even) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-          *reinterpret_cast<uint4*>(row + odd) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+          for (int e = 0; e < 4; ++e) {
+            const uint2 f = f16_of(u[e]);
+            x[8 * c + 2 * e] = f.x;
+            x[8 * c + 2 * e + 1] = f.y;
+          }
         }
+        tmem_st16(ta + 16 * h, x);
       }
-      if (!free) break;
+      src += IM * IK + rb * IK + q * 16;
+      uint8_t* dst = smem + fs * C::B16 + rb * 2 * IK;
+      uint4 v[C::BR / 32];
+#pragma unroll
+      for (int j = 0; j < C::BR / 32; ++j) v[j] = *reinterpret_cast<const uint4*>(src + j * 32 * IK);
+#pragma unroll
+      for (int j = 0; j < C::BR / 32; ++j) {
+        const uint2 x0 = f16_of(v[j].x), x1 = f16_of(v[j].y), x2 = f16_of(v[j].z), x3 = f16_of(v[j].w);
+        uint8_t* row = dst + j * 32 * 2 * IK;
+        *reinterpret_cast<uint4*>(row + even) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+        *reinterpret_cast<uint4*>(row + odd) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+      }
       fence_proxy_async_smem();   // each lane's own stores, before the UMMAs read them
+      tmem_wait_st();
+      tc_fence_before();
       __syncwarp();
       if (lane == 0) {
+        mbar_arrive(rawe0 + 8 * rs);
         if constexpr (PAIR) mbar_arrive_cluster_own(cluster_map(f16f0 + 8 * fs, 0));
         else mbar_arrive(f16f0 + 8 * fs);
       }
     }
   } else {
     // ------------------------------------------------------------ read-back
-    regs_inc<I_REGS_EPI>();
+    regs_inc<C::REGS_EPI>();
     constexpr int HC = BN / 64;   // 32-column chunks of this warp's half
     const int quarter = warp & 3, half = (warp - 4 - I_CONV) >> 2;
     uint8_t* block = smem + C::OFF_OUT + (warp - 4 - I_CONV) * I_OUT_BLOCK;
@@ -350,7 +388,7 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       for (int e = 0; e < HC * 32; ++e) sum[e] = 0;
       for (int c0 = kb0; c0 < kb1; c0 += I_EXACT, ++i) {
         const int set = i & 1;
-        if (!__all_sync(0xffffffffu, wait_for(accf0 + 8 * set, (i >> 1) & 1, wc, 43, i))) {
+        if (!warp_wait(accf0 + 8 * set, (i >> 1) & 1, wc, 43, i)) {
           ok = false;
           break;
         }
@@ -458,11 +496,11 @@ __global__ void __launch_bounds__(I_THREADS, 1)
 }
 
 // The register split of gemm_i8_kernel fits into what its blocks are launched with.
-cudaError_t check_registers(const void* func) {
+cudaError_t check_registers(const void* func, int sum) {
   cudaFuncAttributes attr;
   const cudaError_t e = cudaFuncGetAttributes(&attr, func);
   if (e != cudaSuccess) return e;
-  return attr.numRegs * 5 >= I_REGS_SUM ? cudaSuccess : cudaErrorInvalidConfiguration;
+  return attr.numRegs * (I_THREADS / 128) >= sum ? cudaSuccess : cudaErrorInvalidConfiguration;
 }
 
 template <int BN, bool PAIR, bool SPLIT = false>
@@ -471,12 +509,13 @@ cudaError_t launch_gemm(int split, const int8_t* a_q, const float* a_scale, cons
                         uint64_t wait_limit_ns, int sms, cudaStream_t s) {
   using C = ICfg<BN, PAIR>;
   const void* func = reinterpret_cast<const void*>(gemm_i8_kernel<BN, PAIR, SPLIT>);
-  static const cudaError_t registers = check_registers(func);   // of the code, the same on every device
+  static const cudaError_t registers = check_registers(func, C::REGS_SUM);   // of the code, the same on every device
   if (registers != cudaSuccess) return registers;
   const cudaError_t e = set_smem_limit_once(func, C::SMEM);
   if (e != cudaSuccess) return e;
   CUtensorMap ta, tw, to;
-  if (!encode_tmap_2d_u8_plain(&ta, a_q, D, T, D, IK, IM) || !encode_tmap_2d_u8_plain(&tw, w_q, D, Dout, D, IK, C::BR) ||
+  if (!encode_tmap_2d_u8_rows(&ta, a_q, D, T, D, IK, IM, true) ||
+      !encode_tmap_2d_u8_rows(&tw, w_q, D, Dout, D, IK, C::BR, false) ||
       !encode_tmap_2d_sw64(&to, out, Dout, T, 2 * static_cast<uint64_t>(Dout), 32, 32))
     return cudaErrorInvalidValue;
   LinearParams p;
@@ -507,7 +546,7 @@ GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms) {
   struct Shape {
     int bn, ctas, block_ns, start_ns;
   };
-  static constexpr Shape kShapes[4] = {{256, 2, 400, 4800}, {192, 2, 340, 4800}, {128, 2, 300, 4800}, {128, 1, 400, 3000}};
+  static constexpr Shape kShapes[3] = {{192, 2, 272, 6000}, {128, 2, 260, 4700}, {128, 1, 285, 4000}};
   const int64_t n_kb = (D + IK - 1) / IK;
   GemmChoice best{128, false, 1};
   int64_t best_cost = INT64_MAX;
@@ -554,7 +593,7 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
     return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
                                          sms, s);
   const auto run = !g.pair ? launch_gemm<128, false>
-                   : g.bn == 256 ? launch_gemm<256, true> : g.bn == 192 ? launch_gemm<192, true> : launch_gemm<128, true>;
+                   : g.bn == 192 ? launch_gemm<192, true> : launch_gemm<128, true>;
   return run(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);
 }
 

@@ -127,8 +127,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   return mbar_wait_slow(bar, parity, w, site, detail);
 }
 
-// The same for a barrier that the other CTA of a pair arrives at too: what its threads wrote to their own shared memory
-// before they arrived is ordered before what follows this wait.
+// The same two tests of a barrier that the other CTA of a pair arrives at too: what its threads wrote to their own shared
+// memory before they arrived is ordered before what follows.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -140,6 +140,18 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
       : "memory");
   return ok != 0;
 }
+__device__ __forceinline__ bool mbar_test_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Heartbeat counters in host-visible memory (debug aid): hb[0] += 1 at CTA
 // start, hb[1] after the TMEM allocation, hb[2] at CTA exit.
 __device__ __forceinline__ void heartbeat(uint32_t* hb, int idx) {
@@ -288,6 +300,19 @@ __device__ __forceinline__ void bulk_wait_read() {
   asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// True in one lane of a converged warp, always the same one.  A role whose warp stays together and elects the issuing
+// lane only around the issue keeps its addresses and descriptors in uniform registers, where tcgen05 and TMA
+// instructions take them from; inside `if (lane == 0)` each is moved there one by one.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok));
+  return ok != 0;
+}
 
 // ---------------------------------------------------------------- register shares
 // All four warps of a warpgroup give registers back (down to N a thread) or take free ones (up to N).  Takers wait until
@@ -524,14 +549,15 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
       : "memory");
 }
 
-// D(tmem) (+)= A(smem desc) * B(smem desc) over a pair of CTAs (M = 256), fp16 or bf16 operands, K = 16.
-__device__ __forceinline__ void umma_ss_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+// D(tmem) (+)= A(tmem) * B(smem desc) over a pair of CTAs (M = 256), fp16 or bf16 operands, K = 16: each CTA's rows
+// of A in its own TMEM, at the same columns.
+__device__ __forceinline__ void umma_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                              uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 
