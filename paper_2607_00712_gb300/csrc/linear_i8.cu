@@ -34,9 +34,9 @@ namespace ispa {
 namespace {
 
 // ------------------------------------------------------------ few tokens
-// out[t][n] of the sum: the documented fp32 steps.
-__device__ __forceinline__ float scaled(int32_t s, float sa, float sw, float b) {
-  return __fadd_rn(__fmul_rn(__fmul_rn(__int2float_rn(s), sa), sw), b);
+// out[t][n] of the sum (as fp32, rounded to nearest): the documented fp32 steps.
+__device__ __forceinline__ float scaled(float s, float sa, float sw, float b) {
+  return __fadd_rn(__fmul_rn(__fmul_rn(s, sa), sw), b);
 }
 
 // One warp: NC output channels and up to TT tokens.  Lane l takes the 16-byte words l, l + 32, ... of the rows.
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256)
       int32_t s = __reduce_add_sync(0xffffffffu, acc[t][c]);
       if (lane == (t * NC + c) % 32 && t0 + t < T && n0 + c < Dout)
         out[static_cast<int64_t>(t0 + t) * Dout + n0 + c] =
-            __float2bfloat16_rn(scaled(s, a_scale[t0 + t], w_scale[n0 + c], bias ? bias[n0 + c] : 0.f));
+            __float2bfloat16_rn(scaled(__int2float_rn(s), a_scale[t0 + t], w_scale[n0 + c], bias ? bias[n0 + c] : 0.f));
     }
 }
 
@@ -104,7 +104,8 @@ struct ICfg {
   static_assert(2 * BN <= A_COL, "two accumulator sets and A fit in TMEM");
   static constexpr int OFF_RAW = FST * B16;
   static constexpr int OFF_OUT = OFF_RAW + RST * RAW;
-  static constexpr int OFF_BAR = OFF_OUT + I_EPI * I_OUT_BLOCK;
+  static constexpr int OFF_SCALE = OFF_OUT + I_EPI * 2 * I_OUT_BLOCK;   // two blocks of 32 x 32 bf16 a read-back warp
+  static constexpr int OFF_BAR = OFF_SCALE + I_EPI * BN * 4;           // w_scale and bias of a warp's BN / 2 columns
   static constexpr int N_BAR = 2 * RST + 2 * FST + 4 + 1;   // codes and fp16 full / empty, set full / empty, drain
   static constexpr int SMEM = OFF_BAR + N_BAR * 8 + 16;
   static_assert(SMEM > 116 * 1024 && SMEM <= 232448, "one CTA per SM");
@@ -378,12 +379,27 @@ __global__ void __launch_bounds__(I_THREADS, 1)
     regs_inc<C::REGS_EPI>();
     constexpr int HC = BN / 64;   // 32-column chunks of this warp's half
     const int quarter = warp & 3, half = (warp - 4 - I_CONV) >> 2;
-    uint8_t* block = smem + C::OFF_OUT + (warp - 4 - I_CONV) * I_OUT_BLOCK;
-    int i = 0;   // sets read
+    uint8_t* blocks = smem + C::OFF_OUT + (warp - 4 - I_CONV) * 2 * I_OUT_BLOCK;
+    float* cols = reinterpret_cast<float*>(smem + C::OFF_SCALE) + (warp - 4 - I_CONV) * BN;   // scales, then biases
+    // Up to two runs of 1024: their fp32 sum is the integer's rounding to fp32, so nothing is converted (the
+    // conversions go 16 a clock and SM; 4680 x 1536 -> 4608 took 54 us with them).  A share of a split tile has to stay
+    // exact: one run.
+    const bool in_fp32 = kb1 - kb0 <= (SPLIT ? 1 : 2) * I_EXACT;
+    int i = 0, stores = 0;   // sets read; blocks stored (they alternate on across tiles, wherever one ends)
     bool ok = true;
     for (int t = unit; ok && t < p.n_tiles; t += units) {
       const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + half * (BN / 2);
-      int32_t sum[HC * 32];
+      const int row = m0 + quarter * 32 + lane;
+      // the scales are here before the sums are
+      const float sa = row < p.T ? p.a_scale[row] : 0.f;
+#pragma unroll
+      for (int c = 0; c < HC; ++c) {
+        const int n = n0 + 32 * c + lane;
+        cols[32 * c + lane] = n < p.Dout ? p.w_scale[n] : 0.f;
+        cols[BN / 2 + 32 * c + lane] = p.bias && n < p.Dout ? p.bias[n] : 0.f;
+      }
+      __syncwarp();
+      int32_t sum[HC * 32];   // fp32 bits (in_fp32)
 #pragma unroll
       for (int e = 0; e < HC * 32; ++e) sum[e] = 0;
       for (int c0 = kb0; c0 < kb1; c0 += I_EXACT, ++i) {
@@ -394,13 +410,25 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         }
         tc_fence_after();
         const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + set * BN + half * (BN / 2);
+        if (in_fp32) {
 #pragma unroll
-        for (int c = 0; c < 2 * HC; ++c) {
-          uint32_t v[16];
-          tmem_ld16(taddr + 16 * c, v);
-          tmem_wait_ld16(v);
+          for (int c = 0; c < 2 * HC; ++c) {
+            uint32_t v[16];
+            tmem_ld16(taddr + 16 * c, v);
+            tmem_wait_ld16(v);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum[16 * c + e] += __float2int_rn(__uint_as_float(v[e]));
+            for (int e = 0; e < 16; ++e)
+              sum[16 * c + e] = __float_as_int(__fadd_rn(__int_as_float(sum[16 * c + e]), __uint_as_float(v[e])));
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 2 * HC; ++c) {
+            uint32_t v[16];
+            tmem_ld16(taddr + 16 * c, v);
+            tmem_wait_ld16(v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[16 * c + e] += __float2int_rn(__uint_as_float(v[e]));
+          }
         }
         tc_fence_before();
         __syncwarp();
@@ -411,7 +439,11 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       }
       if (!ok) break;
       if constexpr (SPLIT) {
-        // the partial sums into the fp16 stages, which have been read: 16-byte word q of row r at q ^ (r & 7)
+        // The partial sums, as integers, into the fp16 stages, which have been read: 16-byte word q of row r at q ^ (r & 7).
+        if (in_fp32) {
+#pragma unroll
+          for (int e = 0; e < HC * 32; ++e) sum[e] = __float2int_rn(__int_as_float(sum[e]));
+        }
         int4* x = reinterpret_cast<int4*>(smem) + (quarter * 32 + lane) * (BN / 4);
 #pragma unroll
         for (int q = 0; q < HC * 8; ++q)
@@ -420,23 +452,28 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         break;   // a split tile's CTA has no other
       }
       if (m0 + quarter * 32 >= p.T) continue;   // uniform over the warp; rows past T inside the block are clipped
-      const float sa = m0 + quarter * 32 + lane < p.T ? p.a_scale[m0 + quarter * 32 + lane] : 0.f;
+      if (!in_fp32) {
+#pragma unroll
+        for (int e = 0; e < HC * 32; ++e) sum[e] = __float_as_int(__int2float_rn(sum[e]));
+      }
 #pragma unroll
       for (int c = 0; c < HC; ++c) {
         if (n0 + 32 * c >= p.Dout) break;       // uniform
-        const int n = n0 + 32 * c + lane;
-        const float sw = n < p.Dout ? p.w_scale[n] : 0.f, bi = p.bias && n < p.Dout ? p.bias[n] : 0.f;
-        if (lane == 0) bulk_wait_read_all();    // the store before has read the block
+        uint8_t* block = blocks + (stores++ & 1) * I_OUT_BLOCK;
+        if (lane == 0) bulk_wait_read<1>();     // the store before last, this block's last, has read it
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t pk[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int o = 8 * q + 2 * e;
-            pk[e] = pack_bf16x2(
-                scaled(sum[32 * c + o], sa, __shfl_sync(0xffffffffu, sw, o), __shfl_sync(0xffffffffu, bi, o)),
-                scaled(sum[32 * c + o + 1], sa, __shfl_sync(0xffffffffu, sw, o + 1), __shfl_sync(0xffffffffu, bi, o + 1)));
+          for (int e = 0; e < 2; ++e) {
+            const int o = 32 * c + 8 * q + 4 * e;
+            const float4 sw = *reinterpret_cast<const float4*>(cols + o);
+            const float4 bi = *reinterpret_cast<const float4*>(cols + BN / 2 + o);
+            pk[2 * e] = pack_bf16x2(scaled(__int_as_float(sum[o]), sa, sw.x, bi.x),
+                                    scaled(__int_as_float(sum[o + 1]), sa, sw.y, bi.y));
+            pk[2 * e + 1] = pack_bf16x2(scaled(__int_as_float(sum[o + 2]), sa, sw.z, bi.z),
+                                        scaled(__int_as_float(sum[o + 3]), sa, sw.w, bi.w));
           }
           // 64-byte swizzle: 16-byte word q of row r at word q ^ (r / 2 mod 4)
           *reinterpret_cast<uint4*>(block + lane * 64 + (q ^ ((lane >> 1) & 3)) * 16) =
@@ -481,8 +518,10 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         const float sa = p.a_scale[m0 + r];
         if (n0 < p.Dout)
           *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(m0 + r) * p.Dout + n0) =
-              make_uint2(pack_bf16x2(scaled(o.x, sa, sw[0], bi[0]), scaled(o.y, sa, sw[1], bi[1])),
-                         pack_bf16x2(scaled(o.z, sa, sw[2], bi[2]), scaled(o.w, sa, sw[3], bi[3])));
+              make_uint2(pack_bf16x2(scaled(__int2float_rn(o.x), sa, sw[0], bi[0]),
+                                     scaled(__int2float_rn(o.y), sa, sw[1], bi[1])),
+                         pack_bf16x2(scaled(__int2float_rn(o.z), sa, sw[2], bi[2]),
+                                     scaled(__int2float_rn(o.w), sa, sw[3], bi[3])));
       }
     }
     cluster_sync();   // no CTA leaves while another still reads its shared memory
