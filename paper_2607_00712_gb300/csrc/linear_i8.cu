@@ -240,22 +240,23 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       // ---------------------------------------------------------- TMA producer
       const bool leader = elect_one();
       int g = 0;   // blocks issued over all tiles of this CTA
+      uint32_t st = 0, ph = 1;
       bool ok = true;
       for (int t = unit; ok && t < p.n_tiles; t += units) {
         const int m0 = ((t % p.n_mt) * C::CTAS + rank) * IM, n0 = (t / p.n_mt) * BN + rank * C::BR;
         for (int kb = kb0; kb < kb1; ++kb, ++g) {
-          const int st = g % RST;
-          if (!warp_wait(rawe0 + 8 * st, ((g / RST) & 1) ^ 1, wc, 41, g)) {
+          if (!warp_wait(rawe0 + 8 * st, ph, wc, 41, g)) {
             ok = false;
             break;
           }
-          const uint32_t dst = sbase + C::OFF_RAW + st * C::RAW;
+          const uint32_t dst = sbase + C::OFF_RAW + st * C::RAW, full = rawf0 + 8 * st;
           if (leader) {
-            mbar_arrive_expect_tx(rawf0 + 8 * st, C::RAW);
-            tma_load_2d(dst, &tm_a, rawf0 + 8 * st, kb * IK, m0);
-            tma_load_2d(dst + IM * IK, &tm_w, rawf0 + 8 * st, kb * IK, n0);
+            mbar_arrive_expect_tx(full, C::RAW);
+            tma_load_2d(dst, &tm_a, full, kb * IK, m0);
+            tma_load_2d(dst + IM * IK, &tm_w, full, kb * IK, n0);
           }
           __syncwarp();
+          if (++st == RST) st = 0, ph ^= 1;
         }
       }
       for (int i = g > RST ? g - RST : 0; i < g; ++i)
@@ -265,37 +266,38 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       if (rank == 0) {
         const bool leader = elect_one();
         const uint64_t desc0 = sw128_desc(sbase, 16, 1024);   // + bytes / 16 inside the 256 KB window
-        int g = 0, i = 0;      // blocks; accumulator sets filled
-        bool ok = true, next = false;   // next: the next block is known to be there
+        uint32_t st = 0, ph = 0;   // fp16 stage and its parity
+        int i = 0;                 // accumulator sets filled
+        bool ok = true;
         for (int t = unit; ok && t < p.n_tiles; t += units) {
           for (int c0 = kb0; ok && c0 < kb1; c0 += I_EXACT, ++i) {
-            const int set = i & 1, c1 = min(c0 + I_EXACT, kb1);
+            const int set = i & 1;
             if (!warp_wait<PAIR>(acce0 + 8 * set, ((i >> 1) & 1) ^ 1, wc, 44, i)) {
               ok = false;
               break;
             }
             const uint32_t acc = tmem + set * BN;
-            for (int kb = c0; kb < c1; ++kb, ++g) {
-              const int st = g % FST;
-              if (!next && !warp_wait<PAIR>(f16f0 + 8 * st, (g / FST) & 1, wc, 42, g)) {
+            uint32_t more = 0;
+            for (int left = min(I_EXACT, kb1 - c0); left > 0; --left) {
+              if (!warp_wait<PAIR>(f16f0 + 8 * st, ph, wc, 42, c0)) {
                 ok = false;
                 break;
               }
               tc_fence_after();
               const uint32_t ta = tmem + C::A_COL + st * (IK / 2);
-              const uint64_t db = desc0 + static_cast<uint64_t>(st * C::B16 / 16);
+              const uint64_t db = desc0 + st * (C::B16 / 16);
               if (leader) {
 #pragma unroll
                 for (int k = 0; k < IK / 16; ++k) {   // 16 fp16: 8 TMEM columns of A, 32 bytes inside B's swizzle row
-                  const uint32_t more = kb > c0 || k > 0 ? 1u : 0u;
-                  if constexpr (PAIR) umma_ts_pair(acc, ta + 8 * k, db + 2 * k, C::IDESC, more);
-                  else umma_ts(acc, ta + 8 * k, db + 2 * k, C::IDESC, more);
+                  if constexpr (PAIR) umma_ts_pair(acc, ta + 8 * k, db + 2 * k, C::IDESC, k ? 1u : more);
+                  else umma_ts(acc, ta + 8 * k, db + 2 * k, C::IDESC, k ? 1u : more);
                 }
                 if constexpr (PAIR) tc_commit_pair(f16e0 + 8 * st);
                 else tc_commit(f16e0 + 8 * st);
               }
               __syncwarp();
-              next = warp_test<PAIR>(f16f0 + 8 * ((g + 1) % FST), ((g + 1) / FST) & 1);
+              more = 1;
+              if (++st == FST) st = 0, ph ^= 1;
             }
             if (!ok) break;
             if (leader) {
@@ -496,7 +498,7 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   if constexpr (SPLIT) {
     static_assert(!SPLIT || BN == 128, "a row is four columns a lane");
     cluster_sync();   // every CTA's partial sums are in its shared memory
-    if (warp >= 4 + I_CONV) {
+    if (warp >= 4) {   // not the first four, whose registers are few
       const int m0 = unit % p.n_mt * IM, n0 = unit / p.n_mt * BN + 4 * lane;
       float sw[4], bi[4];
 #pragma unroll
@@ -505,7 +507,7 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         bi[e] = p.bias && n0 + e < p.Dout ? p.bias[n0 + e] : 0.f;
       }
       // one warp per row of this CTA's share; Dout is a multiple of 8, so a lane's four columns are all in or all out
-      for (int r = IM * part / p.split + warp - 4 - I_CONV; r < IM * (part + 1) / p.split && m0 + r < p.T; r += I_EPI) {
+      for (int r = IM * part / p.split + warp - 4; r < IM * (part + 1) / p.split && m0 + r < p.T; r += I_CONV + I_EPI) {
         const uint32_t x = sbase + (r * (BN / 4) + (lane ^ (r & 7))) * 16;
         int4 o = make_int4(0, 0, 0, 0);
         for (int i = 0; i < p.split; ++i) {
@@ -581,30 +583,38 @@ struct GemmChoice {
   int split;
 };
 
-GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms) {
+// The form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in L2) of 9 to 9400
+// tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's fixed part) +
+// launch, fill and the last tile's way out.  A block of a pair of 192 columns costs little more than one of 128, so
+// those win where tiles fill whole waves (4680 x 1536 -> 1536: 19.7 against 22.4 us with pairs of 128 and 23.6 with
+// single CTAs); single CTAs win where there are few tiles (1000 x 1536 -> 1536: 10.0 against 10.9 and 10.3).
+GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms, int64_t* ns) {
   struct Shape {
-    int bn, ctas, block_ns, start_ns;
+    int bn, ctas, block_ns, tile_ns, start_ns;
   };
-  static constexpr Shape kShapes[3] = {{192, 2, 272, 6000}, {128, 2, 260, 4700}, {128, 1, 285, 4000}};
+  static constexpr Shape kShapes[3] = {{192, 2, 250, 500, 4600}, {128, 2, 230, 300, 3750}, {128, 1, 265, 300, 3100}};
   const int64_t n_kb = (D + IK - 1) / IK;
   GemmChoice best{128, false, 1};
-  int64_t best_cost = INT64_MAX;
+  *ns = INT64_MAX;
   for (const Shape& f : kShapes) {
     if (sms < f.ctas) continue;
     const int64_t rows = IM * f.ctas, units = sms / f.ctas;
     const int64_t tiles = (T + rows - 1) / rows * ((Dout + f.bn - 1) / f.bn);
-    const int64_t cost = (tiles + units - 1) / units * (n_kb * f.block_ns + 360) + f.start_ns;
-    if (cost < best_cost) {
-      best_cost = cost;
+    const int64_t cost = (tiles + units - 1) / units * (n_kb * f.block_ns + f.tile_ns) + f.start_ns;
+    if (cost < *ns) {
+      *ns = cost;
       best = {f.bn, f.ctas == 2, 1};
     }
   }
+  // Few tiles and a long contraction: clusters share a tile's blocks and add up through distributed shared memory.
+  // 61 x 5120 -> 640: 24.2 us in pairs of 192, 18.2 / 11.9 / 9.2 with 2 / 4 / 8 CTAs a tile.  As many clusters as run
+  // at once: of four or eight CTAs that is taken as four fifths of the chip.
   for (const int c : {2, 4, 8}) {
     const int64_t tiles = (T + IM - 1) / IM * ((Dout + 127) / 128);
     if (n_kb < c || tiles * c * (c > 2 ? 5 : 4) > 4 * static_cast<int64_t>(sms)) break;
-    const int64_t cost = (n_kb + c - 1) / c * 400 + 360 + 3000 + 2500 + 50 * c;
-    if (cost < best_cost) {
-      best_cost = cost;
+    const int64_t cost = 5100 + (n_kb + c - 1) / c * 265 + 250 * c + 40 * std::min<int64_t>(T, IM) / c;
+    if (cost < *ns) {
+      *ns = cost;
       best = {128, false, c};
     }
   }
@@ -620,14 +630,27 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (T <= 8) {
+  int64_t gemm_ns = 0;
+  const GemmChoice g = choose_gemm(T, D, Dout, sms, &gemm_ns);
+  // Few tokens: the warps' loads and dp4a against the tensor cores' long start.  16 x 1536 -> 1536: 4.5 against 7.7 us;
+  // 16 x 5120 -> 5120: 20.8 against 16.4.
+  if (T <= 32 && 2000 + 55 * (static_cast<int64_t>(T) * D * Dout / 1000000) + D / 2 < gemm_ns) {
     const auto go = [&](auto kernel, int tt, int nc) {
       return launch_pdl(kernel, dim3((Dout + 8 * nc - 1) / (8 * nc), (T + tt - 1) / tt), dim3(256), 0, s, a_q, a_scale, w_q,
                         w_scale, bias, static_cast<int>(T), static_cast<int>(D), static_cast<int>(Dout), o);
     };
-    return T == 1 ? go(gemv_i8_kernel<1, 1>, 1, 1) : T <= 4 ? go(gemv_i8_kernel<4, 2>, 4, 2) : go(gemv_i8_kernel<8, 2>, 8, 2);
+    // Two channels a warp share the tokens' loads, one makes twice the warps: 2 x 1536 -> 1536 2.1 us with one, 2.6 with
+    // two; 2 x 5120 -> 5120 7.7 with one, 5.4 with two; 16 x 1536 -> 1536, two groups of tokens, 5.5 and 4.5.
+    if (Dout <= 16 * sms && T <= 8)
+      return T == 1   ? go(gemv_i8_kernel<1, 1>, 1, 1)
+             : T == 2 ? go(gemv_i8_kernel<2, 1>, 2, 1)
+             : T <= 4 ? go(gemv_i8_kernel<4, 1>, 4, 1)
+                      : go(gemv_i8_kernel<8, 1>, 8, 1);
+    return T == 1   ? go(gemv_i8_kernel<1, 2>, 1, 2)
+           : T == 2 ? go(gemv_i8_kernel<2, 2>, 2, 2)
+           : T <= 4 ? go(gemv_i8_kernel<4, 2>, 4, 2)
+                    : go(gemv_i8_kernel<8, 2>, 8, 2);
   }
-  const GemmChoice g = choose_gemm(T, D, Dout, sms);
   if (g.split > 1)
     return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
                                          sms, s);
