@@ -212,11 +212,7 @@ def lib() -> ctypes.CDLL:
 
 def _ptr(x) -> int | None:
     """Device pointer of a tensor (or an int / None passed through)."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
-    return x.data_ptr()
+    return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
 def _stream(s) -> int | None:
@@ -579,8 +575,7 @@ def ispa_gate_residual(x, x_type: int, y, rows: int, dim: int, post: Norm | None
 # ---------------------------------------------------------------- rotary positions
 def rope(layout: int, head_dim: int, axis_pairs, steps, factor: float = 1.0) -> Rope:
     """axis_pairs: pairs of each axis; steps: device int64 / uint64 tensor of all pairs (ispa_rope_steps)."""
-    n = len(axis_pairs)
-    return _holding(Rope(layout, head_dim, n, (c_int32 * 3)(*list(axis_pairs)[:3]), factor, 0, _ptr(steps)), steps)
+    return _holding(Rope(layout, head_dim, len(axis_pairs), tuple(axis_pairs[:3]), factor, 0, _ptr(steps)), steps)
 
 
 def rope_rows(x, out, heads: int, x_stride: int, out_stride: int, norm: int = ISPA_QK_NORM_NONE, norm_weight=None,

@@ -562,7 +562,9 @@ ispa_status norm_params(NormParams& p, const void* x, int32_t x_type, int64_t ro
     p.out_scale = out->scale;
     p.format = out->format;
   }
-  return ISPA_OK;
+  p.status = device_status_ptr();
+  p.wait_limit_ns = g_wait_limit.load();
+  return p.status ? ISPA_OK : ISPA_ERR_CUDA;
 }
 
 }  // namespace

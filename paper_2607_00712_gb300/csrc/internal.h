@@ -139,6 +139,8 @@ struct NormParams {
   void* out;                // null: the residual part alone
   float* out_scale;
   int32_t format;           // ISPA_ROWS_*
+  int* status;
+  uint64_t wait_limit_ns;
 };
 constexpr int kMaxNormDim = 32768;   // 512 threads of eight vectors of eight values
 cudaError_t launch_norm(const NormParams& p, bool x_fp32, bool residual, cudaStream_t s);

@@ -275,6 +275,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
+// Untiled bulk copy of `bytes` (addresses and size multiples of 16).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 // TMA bulk tensor reduce-add of an fp32 tile from shared memory into global memory: the memory
 // system performs the read-modify-write.  Completion is tracked per issuing thread in bulk
 // async groups (commit, then wait until the source has been read, or until done).
