@@ -798,7 +798,7 @@ typedef struct {
   int32_t head_dim;                       /* a multiple of 8, at most 256 (else ISPA_ERR_UNSUPPORTED) */
   int32_t n_axes;                         /* 1 to 3 (say: frame, row, column) */
   int32_t axis_pairs[ISPA_ROPE_MAX_AXES]; /* pairs of each axis, in order; their sum is the number of pairs: at
-                                             most head_dim / 2, and a multiple of 8 for ISPA_ROPE_HALF (else
+                                             most head_dim / 2, and a multiple of 4 for ISPA_ROPE_HALF (else
                                              ISPA_ERR_UNSUPPORTED) */
   float factor;                           /* on the rotated features (1 but for some long-context scalings) */
   int32_t reserved;
@@ -829,7 +829,7 @@ typedef struct {
 /* rows: host array of n_rows (1 or 2: queries and keys, whose heads may differ in number);
  * pos: device int32 [n_axes][n]; pos0 is added to the positions of axis 0 (the chunk's first frame).
  * The angle is reduced to a fraction of a turn in 64-bit integers, so far positions lose nothing.
- * n below 2^31 (else ISPA_ERR_UNSUPPORTED). */
+ * n below 2^30 (else ISPA_ERR_UNSUPPORTED). */
 ISPA_API ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows,
                                      const int32_t* pos, int64_t pos0, int64_t n, ispa_stream stream);
 

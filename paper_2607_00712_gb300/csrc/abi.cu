@@ -957,12 +957,13 @@ ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, i
     if (width > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
   }
   if (rope->head_dim % 8 != 0 || rope->head_dim > 256 || 2 * pairs > rope->head_dim ||
-      (rope->layout == ISPA_ROPE_HALF && pairs % 8 != 0) || n > INT32_MAX)
+      (rope->layout == ISPA_ROPE_HALF && pairs % 4 != 0) || n > INT32_MAX / 2)
     return ISPA_ERR_UNSUPPORTED;
   RopeParams p = {};
   for (int i = 0; i < n_rows; ++i)
     p.rows[i] = {rows[i].x, rows[i].out, rows[i].x_stride, rows[i].out_stride, rows[i].norm_weight, rows[i].eps,
                  rows[i].heads, rows[i].norm};
+  p.n_rows = n_rows;
   p.n = n;
   p.pos0 = pos0;
   p.pos = pos;
@@ -974,7 +975,7 @@ ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, i
   p.axis_end[0] = rope->axis_pairs[0];
   p.axis_end[1] = p.axis_end[0] + (rope->n_axes > 1 ? rope->axis_pairs[1] : 0);
   p.factor = rope->factor;
-  return launch_rope(p, n_rows, rope->layout == ISPA_ROPE_HALF, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+  return launch_rope(p, rope->layout == ISPA_ROPE_HALF, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
 }
 
 ispa_status ispa_rope_steps(const ispa_rope_frequencies* f, int32_t n_pairs, uint64_t* steps, float* factor) {

@@ -156,6 +156,7 @@ struct RopeRowsParams {
 };
 struct RopeParams {
   RopeRowsParams rows[2];
+  int32_t n_rows;           // 1 or 2: queries, keys
   int64_t n, pos0;
   const int32_t* pos;       // [axes][n]
   const uint64_t* steps;    // [pairs]
@@ -164,7 +165,7 @@ struct RopeParams {
   int32_t axis_end[2];      // pairs before axis 1 and before axis 2
   float factor;
 };
-cudaError_t launch_rope(const RopeParams& p, int n_ops, bool half, cudaStream_t s);
+cudaError_t launch_rope(const RopeParams& p, bool half, cudaStream_t s);
 // Turns per position of n_pairs pairs (64-bit fractions) and the factor on the rotated features; false: bad arguments.
 bool rope_steps(const ispa_rope_frequencies& f, int32_t n_pairs, uint64_t* steps, float* factor);
 

@@ -125,7 +125,7 @@ def test_shapes(n, heads, d, layout, norm):
 
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_part_of_the_head_passes(layout):
-    for d, pairs in [(128, 32), (64, 8), (96, 24), (256, 8)]:
+    for d, pairs in [(128, 32), (64, 8), (96, 24), (256, 8), (128, 20), (40, 4)]:
         _case(9, (4, 4), d, [pairs], layout, abi.ISPA_QK_NORM_HEAD)
         _case(9, (4, 4), d, [pairs], layout, abi.ISPA_QK_NORM_NONE)
 
