@@ -888,7 +888,7 @@ ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, 
 
 ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
                            const float* bias, int64_t T, int32_t D, int32_t D_out, void* out, ispa_stream stream) {
-  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || T <= 0 || T > INT32_MAX || D <= 0 || D_out <= 0 ||
+  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || T <= 0 || T > INT32_MAX - 1024 || D <= 0 || D_out <= 0 ||
       !aligned16(out))
     return ISPA_ERR_INVALID_ARG;
   if (D % 16 != 0 || D > ISPA_LINEAR_I8_MAX_D || D_out % 8 != 0) return ISPA_ERR_UNSUPPORTED;
@@ -975,6 +975,9 @@ ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, i
   p.axis_end[0] = rope->axis_pairs[0];
   p.axis_end[1] = p.axis_end[0] + (rope->n_axes > 1 ? rope->axis_pairs[1] : 0);
   p.factor = rope->factor;
+  p.status = device_status_ptr();
+  p.wait_limit_ns = g_wait_limit.load();
+  if (!p.status) return ISPA_ERR_CUDA;
   return launch_rope(p, rope->layout == ISPA_ROPE_HALF, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
 }
 

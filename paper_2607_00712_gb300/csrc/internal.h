@@ -164,6 +164,8 @@ struct RopeParams {
   int32_t lanes_per_head;   // the power of two of 16-byte words that a head's lanes are dealt in
   int32_t axis_end[2];      // pairs before axis 1 and before axis 2
   float factor;
+  int* status;
+  uint64_t wait_limit_ns;
 };
 cudaError_t launch_rope(const RopeParams& p, bool half, cudaStream_t s);
 // Turns per position of n_pairs pairs (64-bit fractions) and the factor on the rotated features; false: bad arguments.

@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "internal.h"
 #include "pdl.cuh"
@@ -536,12 +537,16 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   }
 }
 
-// The register split of gemm_i8_kernel fits into what its blocks are launched with.
-cudaError_t check_registers(const void* func, int sum) {
+// The register split of gemm_i8_kernel fits into what its blocks are launched with; asked once per kernel (the code is
+// the same on every device).
+cudaError_t check_registers(const void* func, int sum, std::atomic<bool>& checked) {
+  if (checked.load(std::memory_order_relaxed)) return cudaSuccess;
   cudaFuncAttributes attr;
   const cudaError_t e = cudaFuncGetAttributes(&attr, func);
   if (e != cudaSuccess) return e;
-  return attr.numRegs * (I_THREADS / 128) >= sum ? cudaSuccess : cudaErrorInvalidConfiguration;
+  if (attr.numRegs * (I_THREADS / 128) < sum) return cudaErrorInvalidConfiguration;
+  checked.store(true, std::memory_order_relaxed);
+  return cudaSuccess;
 }
 
 template <int BN, bool PAIR, bool SPLIT = false>
@@ -550,9 +555,9 @@ cudaError_t launch_gemm(int split, const int8_t* a_q, const float* a_scale, cons
                         uint64_t wait_limit_ns, int sms, cudaStream_t s) {
   using C = ICfg<BN, PAIR>;
   const void* func = reinterpret_cast<const void*>(gemm_i8_kernel<BN, PAIR, SPLIT>);
-  static const cudaError_t registers = check_registers(func, C::REGS_SUM);   // of the code, the same on every device
-  if (registers != cudaSuccess) return registers;
-  const cudaError_t e = set_smem_limit_once(func, C::SMEM);
+  static std::atomic<bool> checked{false};
+  cudaError_t e = check_registers(func, C::REGS_SUM, checked);
+  if (e == cudaSuccess) e = set_smem_limit_once(func, C::SMEM);
   if (e != cudaSuccess) return e;
   CUtensorMap ta, tw, to;
   if (!encode_tmap_2d_u8_rows(&ta, a_q, D, T, D, IK, IM, true) ||

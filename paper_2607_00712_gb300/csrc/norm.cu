@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormP
 
 // ------------------------------------------------------------ many rows
 constexpr int S_DIM = 8192;             // four factors a column of such rows: 128 KB
-constexpr int S_WARPS = S_DIM / 1024;   // warps of a team, four vectors of eight values a thread
+static_assert(S_DIM <= 1024 * TEAM_WARPS, "four vectors of eight values a thread");
 constexpr int S_SMEM = 224 * 1024;
 // Threads a block: what the registers a thread needs leave room for (64, 80 or 96).
 __host__ __device__ constexpr int s_threads(int v, bool res) { return !res ? 1024 : v == 4 ? 640 : 768; }
@@ -253,29 +253,10 @@ struct Cols {
   }
 };
 
-// A team of `warps` warps with its own named barrier and its own part of shared memory.
-struct Team {
-  float2* red;   // [2][S_WARPS]
-  int warps, barrier, slot;
-  __device__ __forceinline__ void sync() const {
-    if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-    else __syncwarp();
-  }
-  // Every warp's `v` to the lanes i with i % S_WARPS = its number, zeros where there is no such warp.
-  __device__ __forceinline__ float2 gather(float2 v) {
-    float2* r = red + slot * S_WARPS;
-    slot ^= 1;   // written again after the barrier of the call in between
-    const int i = threadIdx.x & (S_WARPS - 1);
-    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
-    sync();
-    return i < warps ? r[i] : make_float2(0.f, 0.f);
-  }
-};
-
 // -mean / root and 1 / root of the team's row, whose values past the row are zeros.  A warp takes its own values' mean and squares
 // about that mean; the warps' are joined by n_w (m_w - m)^2 (Chan, Golub, LeVeque 1983), which needs one barrier where
 // the plain two passes need two, and loses as little.  vectors: this thread's of the row; inv_own, other: 1 / values of this warp, and
-// values of warp lane % S_WARPS.
+// values of warp lane % TEAM_WARPS.
 template <int V>
 __device__ __forceinline__ float2 team_norm(const float (&v)[V][8], const ispa_norm& n, float inv_dim, int vectors,
                                             float inv_own, float other, Team& tm) {
@@ -287,7 +268,7 @@ __device__ __forceinline__ float2 team_norm(const float (&v)[V][8], const ispa_n
 #pragma unroll
       for (int e = 0; e < 8; ++e) q = fmaf(v[i][e], v[i][e], q);
     q = warp_reduce<SumOp>(q);
-    if (tm.warps > 1) q = group_reduce<SumOp>(tm.gather(make_float2(0.f, q)).y, S_WARPS);
+    if (tm.warps > 1) q = group_reduce<SumOp>(tm.gather(make_float2(0.f, q)).y, TEAM_WARPS);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -302,8 +283,8 @@ __device__ __forceinline__ float2 team_norm(const float (&v)[V][8], const ispa_n
     q = warp_reduce<SumOp>(q);
     if (tm.warps > 1) {
       const float2 a = tm.gather(make_float2(m, q));
-      m = group_reduce<SumOp>(a.x * other, S_WARPS) * inv_dim;
-      q = group_reduce<SumOp>(fmaf((a.x - m) * other, a.x - m, a.y), S_WARPS);
+      m = group_reduce<SumOp>(a.x * other, TEAM_WARPS) * inv_dim;
+      q = group_reduce<SumOp>(fmaf((a.x - m) * other, a.x - m, a.y), TEAM_WARPS);
     }
   }
   const float rstd = rsqrtf(fmaf(q, inv_dim, n.eps));   // off by 2^-22.9 at most, a tenth of what the sums may be
@@ -327,14 +308,14 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1) stream_kernel(const __gr
   uint8_t* const rows = smem + 32 * arrays * nv + 2 * row_bytes * threadIdx.y;
   uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + 32 * arrays * nv + 2 * row_bytes * teams);
   const uint32_t full = smem_u32(bars + 2 * threadIdx.y);
-  Team tm{reinterpret_cast<float2*>(bars + 2 * teams) + threadIdx.y * 2 * S_WARPS, step >> 5,
+  Team tm{reinterpret_cast<float2*>(bars + 2 * teams) + threadIdx.y * 2 * TEAM_WARPS, step >> 5,
           1 + static_cast<int>(threadIdx.y), 0};
   const int vectors = t < nv ? (nv - t + step - 1) / step : 0;   // of this thread
   const float inv_dim = 1.f / static_cast<float>(dim);
   float own = 0.f, other = 0.f;   // values of this warp, and of the warp that this lane joins
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int left = nv - i * step, w = lane & (S_WARPS - 1);
+    const int left = nv - i * step, w = lane & (TEAM_WARPS - 1);
     own += 8.f * static_cast<float>(max(0, min(32, left - (t & ~31))));
     if (w < tm.warps) other += 8.f * static_cast<float>(max(0, min(32, left - 32 * w)));
   }
@@ -486,7 +467,7 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1) stream_kernel(const __gr
           }
         if (p.format != ISPA_ROWS_BF16) {
           amax = warp_reduce<MaxOp>(amax);
-          if (tm.warps > 1) amax = group_reduce<MaxOp>(tm.gather(make_float2(amax, 0.f)).x, S_WARPS);
+          if (tm.warps > 1) amax = group_reduce<MaxOp>(tm.gather(make_float2(amax, 0.f)).x, TEAM_WARPS);
           const bool e4m3 = p.format == ISPA_ROWS_E4M3;
           const float top = e4m3 ? 448.f : 127.f, inv = amax == 0.f ? 1.f : __fdiv_rn(top, amax);
 #pragma unroll
@@ -521,7 +502,7 @@ cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
     const int warps = (nv + 127) / 128, v = (nv + 32 * warps - 1) / (32 * warps);
     const int arrays = !RES ? 2 : p.post.bias ? 4 : 3;
     const int fixed = 32 * arrays * nv;
-    const int row = p.dim * ((XF32 ? 4 : 2) + (RES ? 2 : 0)), rest = 2 * 8 + 2 * S_WARPS * 8;
+    const int row = p.dim * ((XF32 ? 4 : 2) + (RES ? 2 : 0)), rest = 2 * 8 + 2 * TEAM_WARPS * 8;
     // registers, 15 named barriers, and what shared memory has room for
     int teams = std::max(1, std::min({s_threads(v, RES) / 32 / warps, warps > 1 ? 15 : 32,
                                       (S_SMEM - fixed) / (2 * row + rest)}));

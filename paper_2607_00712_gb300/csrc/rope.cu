@@ -10,12 +10,15 @@
 // 1.5e-9 rad) go to fp32.  The reduced angle lies in [-pi, pi), where __sinf and __cosf are off by at most 2^-21.19:
 // 2^-12 of a bf16 rounding step of the largest value, against a dozen more instructions a pair for sincosf.
 //
-// Memory bounds it: each value crosses HBM once in and once out.  A block first makes the sines and cosines of its tokens
-// (a warp that made them for itself spent more on them than on its heads: 3117 tokens of 24 and 8 heads of 128, half
-// layout, 58 us), then a warp takes a row, the queries or keys of one token, held in registers between the norm's sum
-// and the rotation; with few rows a block takes one.  A thread takes eight features of one head per step: eight
-// neighbours, or four and the four that they turn with, so that no pair is spread over two lanes.  A warp's lanes are
-// dealt to heads in groups of a power of two, so a lane meets the same features, angles and weights in every head.
+// Memory bounds it: each value crosses HBM once in and once out.
+//
+//   rope_stream_kernel   many tokens: a team of warps a token, queries and keys, with its angles made once
+//   rope_kernel          few tokens, or rows too long for shared memory: a block for a token's queries or keys
+//
+// A thread takes eight features of one head per step: eight neighbours, or four and the four that they turn with, so
+// that no pair is spread over two lanes.  A warp's lanes are dealt to heads in groups of a power of two, so a lane meets
+// the same features, angles and weights in every head.  (Angles made by every warp for itself cost more than its heads:
+// 3117 tokens of 24 and 8 heads of 128, half layout, took 58 us.)
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -35,97 +38,41 @@ __device__ __forceinline__ uint32_t turn_fraction(int64_t pos, uint64_t step) {
   return static_cast<uint32_t>((static_cast<uint64_t>(pos) * step) >> 32);
 }
 
-// V: vectors a thread holds at once.  Block: 8 warps of a row each, or (MULTI) the warps of one row; row r is token
-// r / n_rows, tensor r % n_rows.
-template <int V, bool HALF, bool MULTI>
-__global__ void __launch_bounds__(MULTI ? 512 : 256) rope_kernel(const __grid_constant__ RopeParams p) {
-  __shared__ float2 table[MULTI ? 1 : 8][128];   // cosine and sine of the block's tokens' pairs
-  __shared__ float red[2][32];
-  const int tensors = p.n_rows, lane = threadIdx.x & 31;
-  const int64_t n_rows = p.n * tensors, row0 = static_cast<int64_t>(blockIdx.x) * (MULTI ? 1 : 8);
-  const int64_t tok0 = row0 / tensors;
-  const int64_t row = row0 + (MULTI ? 0 : threadIdx.x >> 5), tok = row / tensors;
-  const RopeRowsParams& o = p.rows[row - tok * tensors];
-  const int lph = p.lanes_per_head, d = p.head_dim, pairs = p.pairs;
-  const int c = lane & (lph - 1);                                     // this lane's vector of every head it meets
-  const bool live = 8 * c < d && row < n_rows;
-  const int heads_step = (MULTI ? blockDim.x : 32) / lph;             // heads a row's warps take per step
-  const int head0 = (MULTI ? threadIdx.x : lane) / lph;
-  // features at[0] .. + 3 and at[1] .. + 3 of a head, pairs 4 c .. 4 c + 3
-  const int at0 = !HALF ? 8 * c : 4 * c < pairs ? 4 * c : 8 * c;
-  const int at1 = HALF && 4 * c < pairs ? pairs + 4 * c : at0 + 4;
-  const int turned = min(4, max(0, pairs - 4 * c));                   // of the lane's pairs; what follows them passes
-  pdl_wait();
-  pdl_trigger();
-
-  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(o.x) + tok * o.x_stride;
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride;
-  uint4 raw[V];
-  auto load = [&](int h) {
-    if (!live || h >= o.heads) return make_uint4(0, 0, 0, 0);
-    const __nv_bfloat16* s = x + static_cast<int64_t>(h) * d;
-    if constexpr (!HALF) return *reinterpret_cast<const uint4*>(s + at0);
-    const uint2 a = *reinterpret_cast<const uint2*>(s + at0), b = *reinterpret_cast<const uint2*>(s + at1);
-    return make_uint4(a.x, a.y, b.x, b.y);
-  };
-#pragma unroll
-  for (int i = 0; i < V; ++i) raw[i] = load(head0 + i * heads_step);
-
-  // the block's tokens: all its rows' (of the last block, those that there are)
-  const int toks = MULTI ? 1 : static_cast<int>(min(p.n, (row0 + 7) / tensors + 1) - tok0);
-  for (int i = threadIdx.x; i < toks * pairs; i += blockDim.x) {
-    const int k = i / pairs, j = i - k * pairs;
-    const int axis = j < p.axis_end[0] ? 0 : j < p.axis_end[1] ? 1 : 2;
-    const int64_t pos = static_cast<int64_t>(p.pos[axis * p.n + tok0 + k]) + (axis == 0 ? p.pos0 : 0);
-    const float a = static_cast<float>(static_cast<int32_t>(turn_fraction(pos, p.steps[j]))) *
-                    1.46291807926715968105e-9f;   // 2 pi / 2^32
-    table[k][j] = make_float2(p.factor * __cosf(a), p.factor * __sinf(a));
+// What a lane does in every head it meets: features at0 .. + 3 and at1 .. + 3, pairs 4 c .. 4 c + 3, of which the first
+// `turned` turn.
+template <bool HALF>
+struct Lane {
+  int c, at0, at1, turned;
+  bool live;
+  __device__ __forceinline__ Lane(int lane, const RopeParams& p) {
+    c = lane & (p.lanes_per_head - 1);
+    live = 8 * c < p.head_dim;
+    at0 = !HALF ? 8 * c : 4 * c < p.pairs ? 4 * c : 8 * c;
+    at1 = HALF && 4 * c < p.pairs ? p.pairs + 4 * c : at0 + 4;
+    turned = min(4, max(0, p.pairs - 4 * c));
   }
-  __syncthreads();
-  if (row >= n_rows) return;   // whole warps, and no barrier follows where a block has several rows
-  float2 cs[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) cs[j] = j < turned ? table[MULTI ? 0 : tok - tok0][4 * c + j] : make_float2(1.f, 0.f);
-
-  float rstd = 1.f;
-  if (o.norm == ISPA_QK_NORM_TOKEN) {
-    float s = 0.f, f[8];
-    auto add = [&](const uint4& w) {
-      unpack8(w, f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(f[e], f[e], s);
-    };
-#pragma unroll
-    for (int i = 0; i < V; ++i) add(raw[i]);
-    for (int h = head0 + V * heads_step; h < o.heads; h += heads_step) add(load(h));
-    s = MULTI ? block_reduce<SumOp>(s, blockDim.x >> 5, red, 0) : warp_reduce<SumOp>(s);
-    rstd = rsqrtf(s / static_cast<float>(o.heads * d) + o.eps);   // off by 2^-22.9 at most
-  }
-  float w[8];
-  auto weight = [&](const float* from) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(from + at0)), b = __ldg(reinterpret_cast<const float4*>(from + at1));
-    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-  };
-#pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = 1.f;
-  if (o.norm == ISPA_QK_NORM_HEAD && o.weight && live) weight(o.weight);
-  const float inv_d = 1.f / static_cast<float>(d);
-
-  auto finish = [&](const uint4& v, int h) {
-    float f[8];
-    unpack8(v, f);
-    if (o.norm == ISPA_QK_NORM_HEAD) {
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(f[e], f[e], s);
-      const float r = rsqrtf(fmaf(group_reduce<SumOp>(s, lph), inv_d, o.eps));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= r * w[e];
-    } else if (o.norm == ISPA_QK_NORM_TOKEN) {
-      if (o.weight && live && h < o.heads) weight(o.weight + static_cast<int64_t>(h) * d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= rstd * w[e];
+  __device__ __forceinline__ uint4 load(const __nv_bfloat16* head) const {
+    if constexpr (!HALF) {
+      return *reinterpret_cast<const uint4*>(head + at0);
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(head + at0), b = *reinterpret_cast<const uint2*>(head + at1);
+      return make_uint4(a.x, a.y, b.x, b.y);
     }
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* head, const float* f) const {
+    const uint4 g = pack8(f);
+    if constexpr (!HALF) {
+      *reinterpret_cast<uint4*>(head + at0) = g;
+    } else {
+      *reinterpret_cast<uint2*>(head + at0) = make_uint2(g.x, g.y);
+      *reinterpret_cast<uint2*>(head + at1) = make_uint2(g.z, g.w);
+    }
+  }
+  __device__ __forceinline__ void weight(const float* from, float* w) const {
+    const float4 a = *reinterpret_cast<const float4*>(from + at0), b = *reinterpret_cast<const float4*>(from + at1);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+  }
+  __device__ __forceinline__ void turn(float* f, const float2* cs) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int a = HALF ? j : 2 * j, b = HALF ? 4 + j : 2 * j + 1;
@@ -135,16 +82,80 @@ __global__ void __launch_bounds__(MULTI ? 512 : 256) rope_kernel(const __grid_co
         f[b] = fmaf(cs[j].y, u, cs[j].x * q);
       }
     }
-    if (live && h < o.heads) {
-      __nv_bfloat16* to = out + static_cast<int64_t>(h) * d;
-      const uint4 g = pack8(f);
-      if constexpr (!HALF) {
-        *reinterpret_cast<uint4*>(to + at0) = g;
-      } else {
-        *reinterpret_cast<uint2*>(to + at0) = make_uint2(g.x, g.y);
-        *reinterpret_cast<uint2*>(to + at1) = make_uint2(g.z, g.w);
-      }
+  }
+};
+
+__device__ __forceinline__ float sum_squares(const uint4& w, float s) {
+  float f[8];
+  unpack8(w, f);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(f[e], f[e], s);
+  return s;
+}
+
+// Cosine and sine (times the factor) of pair j at a position of its axis.
+__device__ __forceinline__ float2 cos_sin(int64_t pos, uint64_t step, float factor) {
+  const float a = static_cast<float>(static_cast<int32_t>(turn_fraction(pos, step))) *
+                  1.46291807926715968105e-9f;   // 2 pi / 2^32
+  return make_float2(factor * __cosf(a), factor * __sinf(a));
+}
+__device__ __forceinline__ int axis_of(int pair, const RopeParams& p) {
+  return pair < p.axis_end[0] ? 0 : pair < p.axis_end[1] ? 1 : 2;
+}
+
+// ------------------------------------------------------------ few rows
+// A block a row (a token's queries or keys); V: vectors a thread holds at once.  blockIdx.y: which of the two.
+template <int V, bool HALF>
+__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeParams p) {
+  __shared__ float2 table[128];
+  __shared__ float red[2][32];
+  const int64_t tok = blockIdx.x;
+  const RopeRowsParams& o = p.rows[blockIdx.y];
+  const int lph = p.lanes_per_head, d = p.head_dim;
+  const Lane<HALF> ln(threadIdx.x, p);
+  const int heads_step = blockDim.x / lph, head0 = threadIdx.x / lph;
+  pdl_wait();
+  pdl_trigger();
+
+  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(o.x) + tok * o.x_stride;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride;
+  uint4 raw[V];
+  auto load = [&](int h) {
+    return ln.live && h < o.heads ? ln.load(x + static_cast<int64_t>(h) * d) : make_uint4(0, 0, 0, 0);
+  };
+#pragma unroll
+  for (int i = 0; i < V; ++i) raw[i] = load(head0 + i * heads_step);
+  for (int j = threadIdx.x; j < p.pairs; j += blockDim.x) {
+    const int axis = axis_of(j, p);
+    table[j] = cos_sin(static_cast<int64_t>(p.pos[axis * p.n + tok]) + (axis == 0 ? p.pos0 : 0), p.steps[j], p.factor);
+  }
+  float s = 0.f;
+  if (o.norm == ISPA_QK_NORM_TOKEN) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) s = sum_squares(raw[i], s);
+    for (int h = head0 + V * heads_step; h < o.heads; h += heads_step) s = sum_squares(load(h), s);
+  }
+  s = block_reduce<SumOp>(s, blockDim.x >> 5, red, 0);   // the table is there too
+  const float rstd = rsqrtf(s / static_cast<float>(o.heads * d) + o.eps);   // off by 2^-22.9 at most
+  float2 cs[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) cs[j] = j < ln.turned ? table[4 * ln.c + j] : make_float2(1.f, 0.f);
+  float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+  if (o.norm == ISPA_QK_NORM_HEAD && o.weight && ln.live) ln.weight(o.weight, w);
+
+  auto finish = [&](const uint4& v, int h) {
+    float f[8], r = rstd;
+    unpack8(v, f);
+    if (o.norm == ISPA_QK_NORM_HEAD)
+      r = rsqrtf(group_reduce<SumOp>(sum_squares(v, 0.f), lph) / static_cast<float>(d) + o.eps);
+    else if (o.norm == ISPA_QK_NORM_TOKEN && o.weight && ln.live && h < o.heads)
+      ln.weight(o.weight + static_cast<int64_t>(h) * d, w);
+    if (o.norm != ISPA_QK_NORM_NONE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= r * w[e];
     }
+    ln.turn(f, cs);
+    if (ln.live && h < o.heads) ln.store(out + static_cast<int64_t>(h) * d, f);
   };
   // Every lane of a warp goes round alike (the head's sum needs all of them): the step counts from the first head.
 #pragma unroll
@@ -159,25 +170,238 @@ __global__ void __launch_bounds__(MULTI ? 512 : 256) rope_kernel(const __grid_co
   }
 }
 
+// ------------------------------------------------------------ many tokens
+constexpr int R_SMEM = 224 * 1024;
+constexpr int R_TABLE = 128 * 8;   // bytes of a team's cosines and sines
+constexpr uint64_t R_DRAIN_NS = 200ull * 1000 * 1000;
+
+// Block (32 * warps of a team, teams), one an SM; block b takes tokens [b, b + 1) * per_block, its teams in turn.  A token's
+// queries and keys come through shared memory by bulk copies, a team's next token while it works on one; weights of
+// a norm over the token's heads stand there too, the eight of a lane in two planes, so that a warp reads whole lines.
+// NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
+template <bool HALF, int NORM, bool FULL>
+__global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_constant__ RopeParams p, int per_block) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int abort_word;
+  const int t = threadIdx.x, threads = blockDim.x, teams = blockDim.y, d = p.head_dim, lph = p.lanes_per_head;
+  const Lane<HALF> ln(t, p);
+  const bool live = FULL || ln.live;
+  const int heads_step = threads / lph, head0 = t / lph, vecs = d / 8;
+  // weights [queries, keys][plane][vectors of a row], the teams' tokens [2][queries, keys], tables, barriers, reductions
+  constexpr bool kWeights = NORM == ISPA_QK_NORM_TOKEN;
+  const int n0 = p.rows[0].heads * d, n1 = p.n_rows > 1 ? p.rows[1].heads * d : 0, r_bytes = 2 * (n0 + n1);
+  const int w_bytes = kWeights ? 4 * (n0 + n1) : 0;
+  uint8_t* const rows = smem + w_bytes + 2 * r_bytes * threadIdx.y;
+  uint8_t* at = smem + w_bytes + 2 * r_bytes * teams;
+  float2* const table = reinterpret_cast<float2*>(at + R_TABLE * threadIdx.y);
+  at += R_TABLE * teams;
+  const uint32_t full = smem_u32(at + 16 * threadIdx.y);
+  at += 16 * teams;
+  Team tm{reinterpret_cast<float2*>(at) + threadIdx.y * 2 * TEAM_WARPS, threads >> 5, 1 + static_cast<int>(threadIdx.y), 0};
+  if (t == 0) {
+    mbar_init(full, 1);
+    mbar_init(full + 8, 1);
+    abort_word = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const WaitCtx wc{&abort_word, p.status, p.wait_limit_ns};
+  const int first = blockIdx.x * per_block;   // tokens are fewer than 2^30
+  const int last = static_cast<int>(min(static_cast<int64_t>(first) + per_block, p.n));
+  auto fetch = [&](int tok, int stage) {
+    mbar_arrive_expect_tx(full + 8 * stage, r_bytes);
+    const uint32_t dst = smem_u32(rows) + stage * r_bytes;
+    bulk_load(dst, static_cast<const __nv_bfloat16*>(p.rows[0].x) + tok * p.rows[0].x_stride, 2 * n0, full + 8 * stage);
+    if (n1)
+      bulk_load(dst + 2 * n0, static_cast<const __nv_bfloat16*>(p.rows[1].x) + tok * p.rows[1].x_stride, 2 * n1,
+                full + 8 * stage);
+  };
+  int tok = first + threadIdx.y;
+  if (t == 0 && tok < last) fetch(tok, 0);
+  // This thread's pairs t, t + threads, ...: their steps, and their position at the team's next token.
+  uint64_t step[4];
+  int pos[4];
+  auto positions = [&](int k) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (t + j * threads < p.pairs && k < last) pos[j] = __ldg(p.pos + axis_of(t + j * threads, p) * p.n + k);
+  };
+#pragma unroll
+  for (int j = 0; j < 4; ++j) step[j] = t + j * threads < p.pairs ? p.steps[t + j * threads] : 0;
+  positions(tok);
+  auto copy_weights = [&](const float* from, float4* to, int n) {
+    for (int k = threadIdx.y * threads + t; k < n / 8; k += threads * teams) {   // vector k of a row
+      const int c = k % vecs;
+      const Lane<HALF> of(c, p);
+      const float* w = from + (k - c) * 8;
+      to[k] = from ? __ldg(reinterpret_cast<const float4*>(w + of.at0)) : make_float4(1.f, 1.f, 1.f, 1.f);
+      to[n / 8 + k] = from ? __ldg(reinterpret_cast<const float4*>(w + of.at1)) : make_float4(1.f, 1.f, 1.f, 1.f);
+    }
+  };
+  if constexpr (kWeights) {
+    copy_weights(p.rows[0].weight, reinterpret_cast<float4*>(smem), n0);
+    if (n1) copy_weights(p.rows[1].weight, reinterpret_cast<float4*>(smem + 4 * n0), n1);
+  }
+  __syncthreads();
+  const float inv_n0 = 1.f / static_cast<float>(n0), inv_n1 = n1 ? 1.f / static_cast<float>(n1) : 0.f;
+  const float inv_d = 1.f / static_cast<float>(d);
+
+  // the sum of a tensor's squares
+  auto squares = [&](const uint8_t* src, int heads) {
+    float q = 0.f;
+    if (live) {
+      const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
+#pragma unroll 2
+      for (int h = head0; h < heads; h += heads_step, x += heads_step * d) q = sum_squares(ln.load(x), q);
+    }
+    return warp_reduce<SumOp>(q);
+  };
+  // norm, rotation and way out of a tensor; cs: the pairs' cosines and sines, with 1 / root of a norm over the token in
+  // them, r that factor for what passes
+  auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs, float r) {
+    const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride + head0 * d;
+    const float4* wp = planes + head0 * vecs + ln.c;
+    float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    if (NORM == ISPA_QK_NORM_HEAD && o.weight && live) ln.weight(o.weight, w);
+    // every lane goes round alike: a head's sum needs all of them
+    int h = head0;
+#pragma unroll 2
+    for (int left = o.heads; left > 0; left -= heads_step) {
+      const bool here = live && h < o.heads;
+      float f[8];
+      const uint4 raw = here ? ln.load(x) : make_uint4(0, 0, 0, 0);
+      unpack8(raw, f);
+      if constexpr (NORM == ISPA_QK_NORM_HEAD) {
+        const float q = rsqrtf(fmaf(group_reduce<SumOp>(sum_squares(raw, 0.f), lph), inv_d, o.eps));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= q * w[e];
+      }
+      if constexpr (NORM == ISPA_QK_NORM_TOKEN) {
+        if (here) {
+          const float4 a = wp[0], b = wp[n / 8];
+          f[0] *= a.x, f[1] *= a.y, f[2] *= a.z, f[3] *= a.w, f[4] *= b.x, f[5] *= b.y, f[6] *= b.z, f[7] *= b.w;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int a = HALF ? j : 2 * j, b = HALF ? 4 + j : 2 * j + 1;
+        const float u = f[a], v = f[b];
+        if (FULL || j < ln.turned) {
+          f[a] = fmaf(cs[j].x, u, -cs[j].y * v);
+          f[b] = fmaf(cs[j].y, u, cs[j].x * v);
+        } else if (NORM == ISPA_QK_NORM_TOKEN) {   // the others pass as they are, infinities too
+          f[a] *= r;
+          f[b] *= r;
+        }
+      }
+      if (here) ln.store(out, f);
+      h += heads_step;
+      x += heads_step * d;
+      out += heads_step * d;
+      wp += heads_step * vecs;
+    }
+  };
+
+  uint32_t turn = 0;   // tokens that this team has begun
+  for (; tok < last; tok += teams, ++turn) {
+    const int stage = turn & 1;
+    if (t == 0 && last - tok > teams) fetch(tok + teams, stage ^ 1);   // all have read the team's last token there
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int pair = t + j * threads;
+      if (pair < p.pairs) table[pair] = cos_sin(pos[j] + (axis_of(pair, p) == 0 ? p.pos0 : 0), step[j], p.factor);
+    }
+    positions(tok + teams);
+    mbar_wait(full + 8 * stage, (turn >> 1) & 1, wc, 52, tok);   // a token that never comes: recorded
+    const uint8_t* src = rows + stage * r_bytes;
+    float2 s = make_float2(0.f, 0.f);
+    if constexpr (NORM == ISPA_QK_NORM_TOKEN) {
+      s.x = squares(src, p.rows[0].heads);
+      if (n1) s.y = squares(src + 2 * n0, p.rows[1].heads);
+    }
+    if (NORM == ISPA_QK_NORM_TOKEN && tm.warps > 1) {   // also: the table is there
+      const float2 all = tm.gather(s);
+      s = make_float2(group_reduce<SumOp>(all.x, TEAM_WARPS), group_reduce<SumOp>(all.y, TEAM_WARPS));
+    } else {
+      tm.sync();
+    }
+    float2 cs[4], c1[4];
+    float r0 = 1.f, r1 = 1.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) cs[j] = FULL || j < ln.turned ? table[4 * ln.c + j] : make_float2(1.f, 0.f);
+    if constexpr (NORM == ISPA_QK_NORM_TOKEN) {
+      r0 = rsqrtf(fmaf(s.x, inv_n0, p.rows[0].eps));   // off by 2^-22.9 at most
+      r1 = rsqrtf(fmaf(s.y, inv_n1, p.rows[1].eps));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        c1[j] = make_float2(cs[j].x * r0, cs[j].y * r0);
+        cs[j] = make_float2(cs[j].x * r1, cs[j].y * r1);
+      }
+      finish(src, p.rows[0], reinterpret_cast<const float4*>(smem), n0, c1, r0);
+      if (n1) finish(src + 2 * n0, p.rows[1], reinterpret_cast<const float4*>(smem + 4 * n0), n1, cs, r1);
+    } else {
+      finish(src, p.rows[0], nullptr, n0, cs, 1.f);
+      if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f);
+    }
+    tm.sync();   // the token's stage and the table are free
+  }
+  // After a timeout: nothing in flight when the block leaves.  The team's last two tokens.
+  if (t == 0 && abort_word)
+    for (uint32_t i = turn < 2 ? 0 : turn - 2; i < turn; ++i)
+      mbar_wait_drain(full + 8 * (i & 1), (i >> 1) & 1, R_DRAIN_NS);
+}
+
 template <bool HALF>
 cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
-  int heads = p.rows[0].heads;
-  if (p.n_rows > 1 && p.rows[1].heads > heads) heads = p.rows[1].heads;
-  const int steps = (heads * p.lanes_per_head + 31) / 32;   // vectors a lane of one warp takes
-  const int64_t rows = p.n * p.n_rows;
-  const auto go = [&](auto kernel, int threads, int rows_per_block) {
-    const int64_t blocks = (rows + rows_per_block - 1) / rows_per_block;
-    return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, s, p);
-  };
-  if (rows > 8 * sms) {
-    if (steps <= 2) return go(rope_kernel<2, HALF, false>, 256, 8);
-    if (steps <= 6) return go(rope_kernel<6, HALF, false>, 256, 8);
-    if (steps <= 12) return go(rope_kernel<12, HALF, false>, 256, 8);
-    return go(rope_kernel<20, HALF, false>, 256, 8);
+  int heads = 0;
+  int64_t values = 0;   // of a token's queries and keys
+  for (int i = 0; i < p.n_rows; ++i) {
+    heads = std::max(heads, p.rows[i].heads);
+    values += static_cast<int64_t>(p.rows[i].heads) * p.head_dim;
   }
-  if (steps <= 16) return go(rope_kernel<1, HALF, true>, 32 * steps, 1);
-  if (steps <= 32) return go(rope_kernel<2, HALF, true>, 32 * ((steps + 1) / 2), 1);
-  return go(rope_kernel<4, HALF, true>, 32 * (steps <= 64 ? (steps + 3) / 4 : 16), 1);
+  // warps that take all heads of a token in one step
+  const int64_t steps = (static_cast<int64_t>(heads) * p.lanes_per_head + 31) / 32;
+  const int norm = p.rows[0].norm;
+  // Estimates in ns, from measured runs: a block a row starts at once but takes blocks and values slowly (900 tokens of
+  // 2 x 1536 5.0 us against 6.9, of 2 x 5120 14.7 against 12.2; 9400 of 640 19.4 against 5.7).
+  const int64_t block_ns = 2000 + std::max(p.n * p.n_rows * 9 / 10, p.n * values * 12 / 10000);
+  const int64_t stream_ns =
+      (norm == ISPA_QK_NORM_TOKEN ? 4000 + std::min<int64_t>(3000, values) : 4500) + p.n * values * 56 / 100000;
+  if (stream_ns < block_ns && values <= R_SMEM / 4 && (p.n_rows == 1 || p.rows[1].norm == norm)) {
+    // Few warps a team where that makes more teams (4680 x 2 x 1536: one warp 15.0 us, two 17.1), more where shared
+    // memory holds few tokens anyway (4680 x 2 x 5120: five warps 38.2 us, four 39.8, two 51.0).
+    const int warps = static_cast<int>(steps <= 6 ? 1 : std::min<int64_t>(TEAM_WARPS, (steps + 3) / 4));
+    const int fixed = norm == ISPA_QK_NORM_TOKEN ? 4 * static_cast<int>(values) : 0;
+    const int token = 4 * static_cast<int>(values) + R_TABLE + 16 + 2 * TEAM_WARPS * 8;
+    const int teams = std::min({32 / warps, warps > 1 ? 15 : 32, (R_SMEM - fixed) / token});
+    const auto go = [&](auto kernel) {
+      const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
+      if (e != cudaSuccess) return e;
+      const int64_t per = std::max<int64_t>((p.n + sms - 1) / sms, teams);
+      return launch_pdl(kernel, dim3(static_cast<unsigned>((p.n + per - 1) / per)), dim3(32 * warps, teams),
+                        fixed + teams * token, s, p, static_cast<int>(per));
+    };
+    if (teams >= 1) {
+      const bool full = 2 * p.pairs == p.head_dim && 8 * p.lanes_per_head == p.head_dim;
+      if (norm == ISPA_QK_NORM_TOKEN)
+        return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true>)
+                    : go(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false>);
+      if (norm == ISPA_QK_NORM_HEAD)
+        return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true>)
+                    : go(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false>);
+      return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true>)
+                  : go(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false>);
+    }
+  }
+  const auto go = [&](auto kernel, int warps) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), p.n_rows), dim3(32 * warps), 0, s, p);
+  };
+  if (steps <= 16) return go(rope_kernel<1, HALF>, static_cast<int>(steps));
+  if (steps <= 32) return go(rope_kernel<2, HALF>, static_cast<int>((steps + 1) / 2));
+  return go(rope_kernel<4, HALF>, steps <= 64 ? static_cast<int>((steps + 3) / 4) : 16);
 }
 
 }  // namespace

@@ -67,4 +67,25 @@ __device__ __forceinline__ float block_reduce(float v, int warps, float (*red)[3
   return v;
 }
 
+constexpr int TEAM_WARPS = 8;   // at most
+
+// A team of `warps` warps with its own named barrier and its own part of shared memory.
+struct Team {
+  float2* red;   // [2][TEAM_WARPS]
+  int warps, barrier, slot;
+  __device__ __forceinline__ void sync() const {
+    if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+    else __syncwarp();
+  }
+  // Every warp's `v` to the lanes i with i % TEAM_WARPS = its number, zeros where there is no such warp.
+  __device__ __forceinline__ float2 gather(float2 v) {
+    float2* r = red + slot * TEAM_WARPS;
+    slot ^= 1;   // written again after the barrier of the call in between
+    const int i = threadIdx.x & (TEAM_WARPS - 1);
+    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
+    sync();
+    return i < warps ? r[i] : make_float2(0.f, 0.f);
+  }
+};
+
 }  // namespace ispa
