@@ -537,57 +537,61 @@ def ispa_linear_i8(a_q, a_scale, w_q, w_scale, bias, T: int, D: int, D_out: int,
 
 
 # ---------------------------------------------------------------- norms, gate and residual
-def _holding(s, *tensors):
-    """A struct of pointers that keeps the tensors it points into alive."""
-    s.tensors = tensors
+# The structs below are pointers and numbers; each keeps the tensors that it points into alive (attribute `tensors`).
+# A struct is passed as it is: its parameter's type takes its address.
+def norm(kind: int, eps: float = 1e-6, weight=None, bias=None) -> Norm:
+    s = Norm(kind, eps, _ptr(weight), _ptr(bias))
+    if weight is not None or bias is not None:
+        s.tensors = weight, bias
     return s
 
 
-def norm(kind: int, eps: float = 1e-6, weight=None, bias=None) -> Norm:
-    return _holding(Norm(kind, eps, _ptr(weight), _ptr(bias)), weight, bias)
-
-
 def modulation(scale=None, shift=None, gate=None, stride: int = 0, rows_per_group: int = 1) -> Modulation:
-    return _holding(Modulation(_ptr(scale), _ptr(shift), _ptr(gate), stride, rows_per_group), scale, shift, gate)
+    s = Modulation(_ptr(scale), _ptr(shift), _ptr(gate), stride, rows_per_group)
+    s.tensors = scale, shift, gate
+    return s
 
 
 def rows_out(data, format: int = ISPA_ROWS_BF16, scale=None) -> RowsOut:
-    return _holding(RowsOut(_ptr(data), _ptr(scale), format, 0), data, scale)
-
-
-def _ref(s):
-    return None if s is None else ctypes.byref(s)
+    s = RowsOut(_ptr(data), _ptr(scale), format)
+    s.tensors = data, scale
+    return s
 
 
 def ispa_norm_modulate(x, x_type: int, rows: int, dim: int, norm: Norm, mod: Modulation | None, out: RowsOut,
                        stream=None) -> None:
-    _check(lib().ispa_norm_modulate(_ptr(x), x_type, rows, dim, _ref(norm), _ref(mod), _ref(out), _stream(stream)),
-           "ispa_norm_modulate")
+    _check(lib().ispa_norm_modulate(_ptr(x), x_type, rows, dim, norm, mod, out, _stream(stream)), "ispa_norm_modulate")
 
 
 def ispa_gate_residual(x, x_type: int, y, rows: int, dim: int, post: Norm | None, x_scale: float, y_scale: float,
                        mod: Modulation | None, x_out, pre: Norm | None = None, out: RowsOut | None = None,
                        stream=None) -> None:
-    _check(lib().ispa_gate_residual(_ptr(x), x_type, _ptr(y), rows, dim, _ref(post), x_scale, y_scale, _ref(mod),
-                                    _ptr(x_out), _ref(pre), _ref(out), _stream(stream)), "ispa_gate_residual")
+    _check(lib().ispa_gate_residual(_ptr(x), x_type, _ptr(y), rows, dim, post, x_scale, y_scale, mod, _ptr(x_out), pre,
+                                    out, _stream(stream)), "ispa_gate_residual")
 
 
 # ---------------------------------------------------------------- rotary positions
 def rope(layout: int, head_dim: int, axis_pairs, steps, factor: float = 1.0) -> Rope:
     """axis_pairs: pairs of each axis; steps: device int64 / uint64 tensor of all pairs (ispa_rope_steps)."""
-    return _holding(Rope(layout, head_dim, len(axis_pairs), tuple(axis_pairs[:3]), factor, 0, _ptr(steps)), steps)
+    s = Rope(layout, head_dim, len(axis_pairs), tuple(axis_pairs[:3]), factor, 0, _ptr(steps))
+    s.tensors = steps
+    return s
 
 
 def rope_rows(x, out, heads: int, x_stride: int, out_stride: int, norm: int = ISPA_QK_NORM_NONE, norm_weight=None,
               eps: float = 1e-6) -> RopeRows:
-    return _holding(RopeRows(_ptr(x), _ptr(out), x_stride, out_stride, _ptr(norm_weight), eps, norm, heads, 0),
-                    x, out, norm_weight)
+    s = RopeRows(_ptr(x), _ptr(out), x_stride, out_stride, _ptr(norm_weight), eps, norm, heads)
+    s.tensors = x, out, norm_weight
+    return s
+
+
+_ROPE_ROWS = [RopeRows * i for i in range(4)]
 
 
 def ispa_rope_apply(rope: Rope, rows: list, pos, pos0: int, n: int, stream=None) -> None:
-    arr = (RopeRows * len(rows))(*rows)
-    _check(lib().ispa_rope_apply(ctypes.byref(rope), arr, len(rows), _ptr(pos), pos0, n, _stream(stream)),
-           "ispa_rope_apply")
+    k = len(rows)
+    arr = (_ROPE_ROWS[k] if k < 4 else RopeRows * k)(*rows)
+    _check(lib().ispa_rope_apply(rope, arr, k, _ptr(pos), pos0, n, _stream(stream)), "ispa_rope_apply")
 
 
 def ispa_rope_steps(n_pairs: int, base: float = 10000.0, scaling: int = ISPA_ROPE_SCALE_NONE, scale: float = 1.0,
