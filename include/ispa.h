@@ -34,11 +34,11 @@
  *     1: an empty call is an argument error (ISPA_ERR_INVALID_ARG) and
  *     enqueues nothing, so callers skip empty work themselves.
  *   - CUDA graphs: after one eager call on a device, the attention, append, LS
- *     accumulate / reset, quantisation, norm, rotary and W8A8 entry points enqueue only
+ *     accumulate / reset, quantisation, norm, rotary and projection entry points enqueue only
  *     kernel launches and memsets on `stream` and can be captured.  A replay reuses what the call
  *     saw at capture time: pointers, and the ring's frames_written and hence its
  *     key sets (an append advances frames_written on the host when it is
- *     captured, not when it is replayed).  ispa_ls_solve and the functions that
+ *     captured, not when it is replayed), and ispa_rope_apply's pos0.  ispa_ls_solve and the functions that
  *     read the device error record synchronise and cannot be captured.
  *   - Threads: entry points may be called from several host threads for
  *     different rings, states and streams.  ispa_set_wait_limit_ns and the
@@ -702,7 +702,7 @@ ISPA_API ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, in
  * integer whatever T, for any codes in [-128, 127]; then, in fp32, each step rounded to nearest: the integer, times
  * a_scale, times w_scale, plus bias (fp32 [D_out], NULL: none), and last to bf16.
  * a_q [T][D], w_q [D_out][D].  D % 16 == 0, D <= ISPA_LINEAR_I8_MAX_D and D_out % 8 == 0 (else
- * ISPA_ERR_UNSUPPORTED); a_q, w_q and out 16-byte aligned. */
+ * ISPA_ERR_UNSUPPORTED); T and D_out at most 2^31 - 1025; a_q, w_q and out 16-byte aligned. */
 ISPA_API ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
                                     const float* bias, int64_t T, int32_t D, int32_t D_out, void* out,
                                     ispa_stream stream);

@@ -888,8 +888,8 @@ ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, 
 
 ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
                            const float* bias, int64_t T, int32_t D, int32_t D_out, void* out, ispa_stream stream) {
-  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || T <= 0 || T > INT32_MAX - 1024 || D <= 0 || D_out <= 0 ||
-      !aligned16(out))
+  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || !aligned16(out) || T <= 0 || D <= 0 || D_out <= 0 ||
+      T > INT32_MAX - 1024 || D_out > INT32_MAX - 1024)
     return ISPA_ERR_INVALID_ARG;
   if (D % 16 != 0 || D > ISPA_LINEAR_I8_MAX_D || D_out % 8 != 0) return ISPA_ERR_UNSUPPORTED;
   int* status = device_status_ptr();

@@ -8,16 +8,25 @@
 // rate is a fraction of theirs.  But codes are exact in fp16, their products are integers up to 2^14, and the sum of
 // 1024 of them stays within 2^24, where every integer is exact in the fp32 accumulator.  So codes go through
 // kind::f16, and every 1024 of the contraction the accumulator is read back and added up in int32: the result is the
-// integer sum, bit for bit, whatever the tile shape.  Against fp8 digits (two e4m3 digits a code, three or four products
-// at twice the rate) this is the cheapest exact form: one product at the fp16 rate.
+// integer sum, bit for bit, whatever the tile shape.  Against fp8 digits (two e4m3 digits a code, three or four
+// products at twice the rate) this is the cheapest exact form: one product at the fp16 rate.
 //
-// GEMM: persistent CTAs over 128 x BN tiles, or pairs over 256 x BN tiles (cta_group::2).  Per 64 codes of the
-// contraction: TMA brings the bytes as they are (warp 0); eight warps turn them into fp16 in the 128-byte swizzle
-// that the tensor cores read (byte u = code + 128 beside 0x64 is the fp16 number 1024 + u, less 1152 the code: a
-// permute and a subtraction for two codes); warp 1 issues the UMMAs; eight warps read the accumulators back, two
-// sets in TMEM in turn.  These hold up to 128 int32 sums each thread, so the warpgroups share the registers out anew
-// (setmaxnreg).  Shared memory bounds it: a block's bytes are written by TMA, read and written as fp16 by the
-// converters and read by the UMMAs; in a pair each CTA does that for half of B.  Every wait is bounded.
+// GEMM: persistent CTAs over 128 x 128 tiles, pairs over 256 x 192 or 256 x 128 tiles (cta_group::2), or clusters that
+// share a tile's contraction, whichever gives the shortest estimated run.  Per block of 64 codes: warp 0 has TMA bring
+// the bytes as they are; four of twelve converter warps turn them into fp16 (byte u = code + 128 beside 0x64 is the
+// fp16 number 1024 + u, less 1152 the code: a permute and a subtraction for two codes), activations into TMEM, weights
+// into shared memory in the 128-byte swizzle that the UMMAs read; warp 1 issues the UMMAs; eight warps read the
+// accumulators back, two sets in TMEM in turn.  Their int32 sums take up to 96 registers a thread, so the warpgroups
+// share the registers out anew (setmaxnreg).  Every wait is bounded.
+//
+// 4680 x 5120 -> 5120 149.8 us, 1638 TFLOP/s; 4680 x 1536 -> 4608 46.4 us; 61 x 5120 -> 640 9.0 us; one token of
+// 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit: a block of 192 columns takes 0.25 us where its
+// UMMAs take 0.19, a team 0.47 us for a block (there are three), and the ring of four stages, from one block's
+// conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave 134 us, three quarters of the UMMAs
+// 143.  On the way: one team of eight converter warps 405 us, four teams of two 218; a release at cluster scope a
+// block, a memory barrier, taken back 168; A in TMEM, so that shared memory moves a third less, 225 in pairs of 192,
+// because one lane issued TMA and UMMAs with each operand moved to a uniform register one by one; whole warps in these
+// roles 159; twelve converter warps 157; sums of two runs in fp32 155; running stage counters 150.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -66,7 +75,8 @@ __global__ void __launch_bounds__(256)
                                  : make_int4(0, 0, 0, 0);
 #pragma unroll
       for (int c = 0; c < NC; ++c)
-        acc[t][c] = __dp4a(av.x, wv[c].x, __dp4a(av.y, wv[c].y, __dp4a(av.z, wv[c].z, __dp4a(av.w, wv[c].w, acc[t][c]))));
+        acc[t][c] = __dp4a(av.x, wv[c].x, __dp4a(av.y, wv[c].y, __dp4a(av.z, wv[c].z,
+                                                                       __dp4a(av.w, wv[c].w, acc[t][c]))));
     }
   }
 #pragma unroll
@@ -81,11 +91,11 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------ many tokens
-constexpr int IM = 128;          // rows (tokens) of a CTA's part of a tile
-constexpr int IK = 64;           // contraction codes per block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
-constexpr int I_EXACT = 1024 / IK;   // blocks whose sums the fp32 accumulator holds exactly
+constexpr int IM = 128;                 // rows (tokens) of a CTA's part of a tile
+constexpr int IK = 64;                  // codes of a block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
+constexpr int I_EXACT = 1024 / IK;      // blocks whose sums the fp32 accumulator holds exactly
 constexpr int I_CONV = 12, I_EPI = 8;   // converter and read-back warps
-constexpr int I_TEAMS = I_CONV / 4;    // four converter warps, one per TMEM lane quarter, share a block
+constexpr int I_TEAMS = I_CONV / 4;     // four converter warps, one per TMEM lane quarter, share a block
 constexpr int I_THREADS = 32 * (4 + I_CONV + I_EPI);
 constexpr int I_OUT_BLOCK = 32 * 64;
 constexpr uint64_t I_DRAIN_NS = 200ull * 1000 * 1000;
@@ -96,13 +106,15 @@ struct ICfg {
   static constexpr int BR = BN / CTAS;              // this CTA's rows of B
   static constexpr int RAW = (IM + BR) * IK;        // bytes of a block as codes
   static constexpr int B16 = BR * 2 * IK;           // of its part of B as fp16
-  static constexpr int FST = 4, RST = BR == 128 ? 6 : 9;   // stages of fp16 (A in TMEM, B in shared memory) and of codes
-  // A team waits for a stage of codes knowing that its own last block has landed, and for an fp16 stage knowing that the
-  // UMMAs have read all blocks up to its own last one less FST.  Parities tell two uses of a stage apart, not three: the
-  // stage's use before must be one that the team knows of.
+  // stages of fp16 (A in TMEM, B in shared memory) and of codes
+  static constexpr int FST = 4, RST = BR == 128 ? 6 : 9;
+  // A team waits for a stage of codes knowing that its own last block has landed, and for an fp16 stage knowing that
+  // the UMMAs have read all blocks up to its own last one less FST.  Parities tell two uses of a stage apart, not
+  // three: the stage's use before must be one that the team knows of.
   static_assert(RST % I_TEAMS == 0 && FST >= I_TEAMS, "parities stay unambiguous");
   static constexpr int A_COL = 512 - FST * IK / 2;  // TMEM columns of A's stages: two fp16 a column
   static_assert(2 * BN <= A_COL, "two accumulator sets and A fit in TMEM");
+  static_assert(BN != 128 || PAIR || FST * B16 >= IM * BN * 4, "a split tile's sums fit into the fp16 stages");
   static constexpr int OFF_RAW = FST * B16;
   static constexpr int OFF_OUT = OFF_RAW + RST * RAW;
   static constexpr int OFF_SCALE = OFF_OUT + I_EPI * 2 * I_OUT_BLOCK;   // two blocks of 32 x 32 bf16 a read-back warp
@@ -132,13 +144,9 @@ struct LinearParams {
   uint64_t wait_limit_ns;
 };
 
-// A converged warp's test of a barrier (CLUSTER: that the pair's other CTA arrives at too), the same answer in every
-// lane, and its bounded wait (as mbar_wait, with the polling loop in line: a kernel that shares its registers out anew
-// cannot call functions).  The test never suspends the warp; the wait's polls do, for up to microseconds.
-template <bool CLUSTER = false>
-__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, CLUSTER ? mbar_test_wait_cluster(bar, parity) : mbar_test_wait(bar, parity));
-}
+// A converged warp's bounded wait (CLUSTER: for a barrier that the pair's other CTA arrives at too), the same answer in
+// every lane; mbar_wait with the polling loop in line, because a kernel that shares its registers out anew cannot call
+// functions.
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx& w, int site, int detail) {
   uint64_t t0 = 0;
@@ -160,7 +168,8 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const W
 
 // mbar_wait_drain by a converged warp; the timer, hundreds of cycles a reading, only for what has not landed yet.
 __device__ __forceinline__ void warp_drain(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
-  if (!warp_test(bar, parity) && (threadIdx.x & 31) == 0) mbar_wait_drain(bar, parity, limit_ns);
+  const bool done = __all_sync(0xffffffffu, mbar_test_wait(bar, parity));
+  if (!done && (threadIdx.x & 31) == 0) mbar_wait_drain(bar, parity, limit_ns);
   __syncwarp();
 }
 
@@ -320,15 +329,15 @@ __global__ void __launch_bounds__(I_THREADS, 1)
   } else if (warp < 4 + I_CONV) {
     // ------------------------------------------------------------ converters
     regs_dec<C::REGS_CONV>();
-    // Each team its own blocks: the waits, the fence and the arrivals of one block hide behind the other team's work.
+    // Each team its own blocks: the waits, the fence and the arrivals of one block hide behind the other teams' work.
     const int quarter = warp & 3;
     const int n = (unit < p.n_tiles ? (p.n_tiles - 1 - unit) / units + 1 : 0) * (kb1 - kb0);   // this CTA's blocks
-    // A: a lane a row, 64 codes; the 64-byte swizzle puts 16-byte word c of row r at word c ^ (r / 2 mod 4), so that eight
-    // rows' words lie in eight different bank groups.
+    // A: a lane a row, 64 codes; the 64-byte swizzle puts 16-byte word c of row r at word c ^ (r / 2 mod 4), so that
+    // eight rows' words lie in eight different bank groups.
     const int ra = quarter * 32 + lane, xa = (ra >> 1) & 3;
-    // B: eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and write, of two
-    // neighbouring rows, the even (then the odd) 16-byte words, which the 128-byte swizzle puts into eight different
-    // bank groups.
+    // B: eight rows at a time, four lanes a row with 16 codes each: eight lanes read 128 bytes in a row and write, of
+    // two neighbouring rows, the even (then the odd) 16-byte words, which the 128-byte swizzle puts into eight
+    // different bank groups.
     const int rb = 8 * quarter + (lane >> 2), q = lane & 3;
     const uint32_t even = ((2 * q) ^ (rb & 7)) * 16, odd = ((2 * q + 1) ^ (rb & 7)) * 16;
     for (int g = (warp - 4) / 4; g < n; g += I_TEAMS) {
@@ -442,7 +451,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       }
       if (!ok) break;
       if constexpr (SPLIT) {
-        // The partial sums, as integers, into the fp16 stages, which have been read: 16-byte word q of row r at q ^ (r & 7).
+        // The partial sums, as integers, into the fp16 stages, which have been read: 16-byte word q of row r at
+        // q ^ (r & 7).
         if (in_fp32) {
 #pragma unroll
           for (int e = 0; e < HC * 32; ++e) sum[e] = __float2int_rn(__int_as_float(sum[e]));
@@ -508,7 +518,8 @@ __global__ void __launch_bounds__(I_THREADS, 1)
         bi[e] = p.bias && n0 + e < p.Dout ? p.bias[n0 + e] : 0.f;
       }
       // one warp per row of this CTA's share; Dout is a multiple of 8, so a lane's four columns are all in or all out
-      for (int r = IM * part / p.split + warp - 4; r < IM * (part + 1) / p.split && m0 + r < p.T; r += I_CONV + I_EPI) {
+      const int end = min(IM * (part + 1) / p.split, p.T - m0);
+      for (int r = IM * part / p.split + warp - 4; r < end; r += I_CONV + I_EPI) {
         const uint32_t x = sbase + (r * (BN / 4) + (lane ^ (r & 7))) * 16;
         int4 o = make_int4(0, 0, 0, 0);
         for (int i = 0; i < p.split; ++i) {
@@ -588,9 +599,9 @@ struct GemmChoice {
   int split;
 };
 
-// The form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in L2) of 9 to 9400
-// tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's fixed part) +
-// launch, fill and the last tile's way out.  A block of a pair of 192 columns costs little more than one of 128, so
+// The form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in L2) of 9 to
+// 9400 tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's fixed part)
+// + launch, fill and the last tile's way out.  A block of a pair of 192 columns costs little more than one of 128, so
 // those win where tiles fill whole waves (4680 x 1536 -> 1536: 19.7 against 22.4 us with pairs of 128 and 23.6 with
 // single CTAs); single CTAs win where there are few tiles (1000 x 1536 -> 1536: 10.0 against 10.9 and 10.3).
 GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms, int64_t* ns) {
@@ -641,11 +652,11 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
   // 16 x 5120 -> 5120: 20.8 against 16.4.
   if (T <= 32 && 2000 + 55 * (static_cast<int64_t>(T) * D * Dout / 1000000) + D / 2 < gemm_ns) {
     const auto go = [&](auto kernel, int tt, int nc) {
-      return launch_pdl(kernel, dim3((Dout + 8 * nc - 1) / (8 * nc), (T + tt - 1) / tt), dim3(256), 0, s, a_q, a_scale, w_q,
-                        w_scale, bias, static_cast<int>(T), static_cast<int>(D), static_cast<int>(Dout), o);
+      return launch_pdl(kernel, dim3((Dout + 8 * nc - 1) / (8 * nc), (T + tt - 1) / tt), dim3(256), 0, s, a_q, a_scale,
+                        w_q, w_scale, bias, static_cast<int>(T), static_cast<int>(D), static_cast<int>(Dout), o);
     };
-    // Two channels a warp share the tokens' loads, one makes twice the warps: 2 x 1536 -> 1536 2.1 us with one, 2.6 with
-    // two; 2 x 5120 -> 5120 7.7 with one, 5.4 with two; 16 x 1536 -> 1536, two groups of tokens, 5.5 and 4.5.
+    // Two channels a warp share the tokens' loads, one makes twice the warps: 2 x 1536 -> 1536 2.1 us with one, 2.6
+    // with two; 2 x 5120 -> 5120 7.7 with one, 5.4 with two; 16 x 1536 -> 1536, two groups of tokens, 5.5 and 4.5.
     if (Dout <= 16 * sms && T <= 8)
       return T == 1   ? go(gemv_i8_kernel<1, 1>, 1, 1)
              : T == 2 ? go(gemv_i8_kernel<2, 1>, 2, 1)
@@ -657,8 +668,8 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
                     : go(gemv_i8_kernel<8, 2>, 8, 2);
   }
   if (g.split > 1)
-    return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns,
-                                         sms, s);
+    return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status,
+                                         wait_limit_ns, sms, s);
   const auto run = !g.pair ? launch_gemm<128, false>
                    : g.bn == 192 ? launch_gemm<192, true> : launch_gemm<128, true>;
   return run(1, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status, wait_limit_ns, sms, s);

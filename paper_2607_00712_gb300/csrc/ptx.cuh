@@ -127,24 +127,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   return mbar_wait_slow(bar, parity, w, site, detail);
 }
 
-// The same two tests of a barrier that the other CTA of a pair arrives at too: what its threads wrote to their own shared
-// memory before they arrived is ordered before what follows.
+// mbar_try_wait for a barrier that the other CTA of a pair arrives at too: what its threads wrote to their own
+// shared memory before they arrived is ordered before what follows.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_test_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
       : "r"(bar), "r"(parity)
@@ -322,8 +311,8 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 // ---------------------------------------------------------------- register shares
-// All four warps of a warpgroup give registers back (down to N a thread) or take free ones (up to N).  Takers wait until
-// there are enough: the shares of a block must not exceed what it was launched with.
+// All four warps of a warpgroup give registers back (down to N a thread) or take free ones (up to N).  Takers wait
+// until there are enough: the shares of a block must not exceed what it was launched with.
 template <int N>
 __device__ __forceinline__ void regs_dec() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
@@ -507,7 +496,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
 
 // The same where what it releases is the arriving CTA's own shared memory, written through the generic proxy, fenced
 // (fence_proxy_async_smem) and read by that same SM's tensor core when the pair's UMMA runs: ordering within the
-// arriving CTA is enough, and the wider release is a memory barrier that waits about a microsecond.
+// arriving CTA is enough, and the wider release is a memory barrier (a quarter of an int8 GEMM's time at one a block).
 __device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }

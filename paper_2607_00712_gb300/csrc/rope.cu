@@ -16,9 +16,13 @@
 //   rope_kernel          few tokens, or rows too long for shared memory: a block for a token's queries or keys
 //
 // A thread takes eight features of one head per step: eight neighbours, or four and the four that they turn with, so
-// that no pair is spread over two lanes.  A warp's lanes are dealt to heads in groups of a power of two, so a lane meets
-// the same features, angles and weights in every head.  (Angles made by every warp for itself cost more than its heads:
-// 3117 tokens of 24 and 8 heads of 128, half layout, took 58 us.)
+// that no pair is spread over two lanes.  A warp's lanes are dealt to heads in groups of a power of two, so a lane
+// meets the same features, angles and weights in every head.
+//
+// Queries and keys of 4680 x 40 heads of 128, norm over the token: 38.1 us, 74 % of the measured copy rate (32.9
+// without the norm); 12 heads 14.9 us, of which 7 are the start (angles, weights); one token 2.0 us.  Angles made by
+// every warp for itself cost more than its heads: 69 us, and 58 for 3117 tokens of 24 and 8 heads in the half layout
+// (17.5 now); a warp a token with its row in registers 77 (164 registers, too few warps).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -34,8 +38,8 @@ namespace ispa {
 namespace {
 
 // The upper 32 bits of the 64-bit product's lower half: the position's fraction of a turn in units of 2^-32.
-__device__ __forceinline__ uint32_t turn_fraction(int64_t pos, uint64_t step) {
-  return static_cast<uint32_t>((static_cast<uint64_t>(pos) * step) >> 32);
+__device__ __forceinline__ uint32_t turn_fraction(uint64_t pos, uint64_t step) {
+  return static_cast<uint32_t>((pos * step) >> 32);
 }
 
 // What a lane does in every head it meets: features at0 .. + 3 and at1 .. + 3, pairs 4 c .. 4 c + 3, of which the first
@@ -93,9 +97,10 @@ __device__ __forceinline__ float sum_squares(const uint4& w, float s) {
   return s;
 }
 
-// Cosine and sine (times the factor) of pair j at a position of its axis.
-__device__ __forceinline__ float2 cos_sin(int64_t pos, uint64_t step, float factor) {
-  const float a = static_cast<float>(static_cast<int32_t>(turn_fraction(pos, step))) *
+// Cosine and sine (times the factor) of a pair at position pos + pos0 of its axis; all of it modulo 2^64.
+__device__ __forceinline__ float2 cos_sin(int32_t pos, int64_t pos0, uint64_t step, float factor) {
+  const uint64_t at = static_cast<uint64_t>(static_cast<int64_t>(pos)) + static_cast<uint64_t>(pos0);
+  const float a = static_cast<float>(static_cast<int32_t>(turn_fraction(at, step))) *
                   1.46291807926715968105e-9f;   // 2 pi / 2^32
   return make_float2(factor * __cosf(a), factor * __sinf(a));
 }
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeP
   for (int i = 0; i < V; ++i) raw[i] = load(head0 + i * heads_step);
   for (int j = threadIdx.x; j < p.pairs; j += blockDim.x) {
     const int axis = axis_of(j, p);
-    table[j] = cos_sin(static_cast<int64_t>(p.pos[axis * p.n + tok]) + (axis == 0 ? p.pos0 : 0), p.steps[j], p.factor);
+    table[j] = cos_sin(p.pos[axis * p.n + tok], axis == 0 ? p.pos0 : 0, p.steps[j], p.factor);
   }
   float s = 0.f;
   if (o.norm == ISPA_QK_NORM_TOKEN) {
@@ -175,10 +180,10 @@ constexpr int R_SMEM = 224 * 1024;
 constexpr int R_TABLE = 128 * 8;   // bytes of a team's cosines and sines
 constexpr uint64_t R_DRAIN_NS = 200ull * 1000 * 1000;
 
-// Block (32 * warps of a team, teams), one an SM; block b takes tokens [b, b + 1) * per_block, its teams in turn.  A token's
-// queries and keys come through shared memory by bulk copies, a team's next token while it works on one; weights of
-// a norm over the token's heads stand there too, the eight of a lane in two planes, so that a warp reads whole lines.
-// NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
+// Block (32 * warps of a team, teams), one an SM; block b takes tokens [b, b + 1) * per_block, its teams in turn.  A
+// token's queries and keys come through shared memory by bulk copies, a team's next token while it works on one;
+// weights of a norm over the token's heads stand there too, the eight of a lane in two planes, so that a warp reads
+// whole lines. NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
 template <bool HALF, int NORM, bool FULL>
 __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_constant__ RopeParams p, int per_block) {
   extern __shared__ __align__(128) uint8_t smem[];
@@ -187,7 +192,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   const Lane<HALF> ln(t, p);
   const bool live = FULL || ln.live;
   const int heads_step = threads / lph, head0 = t / lph, vecs = d / 8;
-  // weights [queries, keys][plane][vectors of a row], the teams' tokens [2][queries, keys], tables, barriers, reductions
+  // weights [queries, keys][plane][vectors of a row], the teams' tokens [2][queries, keys], tables, barriers,
+  // reductions
   constexpr bool kWeights = NORM == ISPA_QK_NORM_TOKEN;
   const int n0 = p.rows[0].heads * d, n1 = p.n_rows > 1 ? p.rows[1].heads * d : 0, r_bytes = 2 * (n0 + n1);
   const int w_bytes = kWeights ? 4 * (n0 + n1) : 0;
@@ -197,7 +203,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   at += R_TABLE * teams;
   const uint32_t full = smem_u32(at + 16 * threadIdx.y);
   at += 16 * teams;
-  Team tm{reinterpret_cast<float2*>(at) + threadIdx.y * 2 * TEAM_WARPS, threads >> 5, 1 + static_cast<int>(threadIdx.y), 0};
+  Team tm{reinterpret_cast<float2*>(at) + threadIdx.y * 2 * TEAM_WARPS, threads >> 5,
+          1 + static_cast<int>(threadIdx.y), 0};
   if (t == 0) {
     mbar_init(full, 1);
     mbar_init(full + 8, 1);
@@ -219,7 +226,9 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
                 full + 8 * stage);
   };
   int tok = first + threadIdx.y;
-  if (t == 0 && tok < last) fetch(tok, 0);
+  uint32_t issued = 0;   // (thread 0) tokens that it has sent for
+  bool ok = true;
+  if (t == 0 && tok < last) fetch(tok, issued++ & 1);
   // This thread's pairs t, t + threads, ...: their steps, and their position at the team's next token.
   uint64_t step[4];
   int pos[4];
@@ -260,7 +269,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   };
   // norm, rotation and way out of a tensor; cs: the pairs' cosines and sines, with 1 / root of a norm over the token in
   // them, r that factor for what passes
-  auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs, float r) {
+  auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs,
+                    float r) {
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride + head0 * d;
     const float4* wp = planes + head0 * vecs + ln.c;
@@ -308,14 +318,14 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   uint32_t turn = 0;   // tokens that this team has begun
   for (; tok < last; tok += teams, ++turn) {
     const int stage = turn & 1;
-    if (t == 0 && last - tok > teams) fetch(tok + teams, stage ^ 1);   // all have read the team's last token there
+    if (t == 0 && ok && last - tok > teams) fetch(tok + teams, issued++ & 1);   // all have read the last token there
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int pair = t + j * threads;
-      if (pair < p.pairs) table[pair] = cos_sin(pos[j] + (axis_of(pair, p) == 0 ? p.pos0 : 0), step[j], p.factor);
+      if (pair < p.pairs) table[pair] = cos_sin(pos[j], axis_of(pair, p) == 0 ? p.pos0 : 0, step[j], p.factor);
     }
     positions(tok + teams);
-    mbar_wait(full + 8 * stage, (turn >> 1) & 1, wc, 52, tok);   // a token that never comes: recorded
+    ok &= mbar_wait(full + 8 * stage, (turn >> 1) & 1, wc, 52, tok);   // a token that never comes: recorded
     const uint8_t* src = rows + stage * r_bytes;
     float2 s = make_float2(0.f, 0.f);
     if constexpr (NORM == ISPA_QK_NORM_TOKEN) {
@@ -348,9 +358,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
     }
     tm.sync();   // the token's stage and the table are free
   }
-  // After a timeout: nothing in flight when the block leaves.  The team's last two tokens.
-  if (t == 0 && abort_word)
-    for (uint32_t i = turn < 2 ? 0 : turn - 2; i < turn; ++i)
+  if (t == 0 && !ok)   // after a timeout: nothing in flight when the block leaves
+    for (uint32_t i = issued < 2 ? 0 : issued - 2; i < issued; ++i)
       mbar_wait_drain(full + 8 * (i & 1), (i >> 1) & 1, R_DRAIN_NS);
 }
 

@@ -140,7 +140,8 @@ __global__ void col_amax_kernel(const float* __restrict__ W, const float* __rest
   const int n = blockIdx.x * 32 + threadIdx.x;
   float m = 0.f;
   if (n < Dout)
-    for (int k = threadIdx.y; k < D; k += 8) m = amax_of<I8>(m, fabsf(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n)));
+    for (int k = threadIdx.y; k < D; k += 8)
+      m = amax_of<I8>(m, fabsf(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n)));
   red[threadIdx.y][threadIdx.x] = m;
   __syncthreads();
   if (threadIdx.y == 0 && n < Dout) {

@@ -112,7 +112,7 @@ def _norm_case(rows, dim, fp32, kind, fmt, affine, per, vectors="both"):
 
 @pytest.mark.parametrize("fp32", [False, True])
 @pytest.mark.parametrize("rows,dim", [(1, 8), (7, 264), (3, 1536), (1203, 1536), (640, 2048), (5, 5120), (2, 32768),
-                                      (700, 2056)])
+                                      (700, 2056), (613, 8192), (640, 4104)])
 def test_gate_residual(rows, dim, fp32):
     for post, pre, fmt in [(ol.NONE, ol.LAYER, "bf16"), (ol.RMS, ol.RMS, "i8"), (ol.LAYER, ol.NONE, "bf16"),
                            (ol.RMS, None, None)]:

@@ -146,7 +146,7 @@ def test_three_axes(layout):
 
 def test_far_and_negative_positions():
     far = [[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 1_000_003, 65_537]]
-    for pos0 in (0, 2 ** 40 + 17, -(2 ** 45)):
+    for pos0 in (0, 2 ** 40 + 17, -(2 ** 45), 2 ** 63 - 1):
         _case(7, (2, 2), 128, [64], abi.ISPA_ROPE_INTERLEAVED, abi.ISPA_QK_NORM_NONE, pos0=pos0, pos=far)
 
 

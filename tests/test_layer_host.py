@@ -95,6 +95,7 @@ def test_linear_i8_refusals():
 
     assert call(a=None) == BAD and call(a=24) == BAD and call(w=None) == BAD and call(w=8) == BAD
     assert call(sa=None) == BAD and call(sw=None) == BAD and call(out=None) == BAD and call(out=24) == BAD
+    assert call(T=2 ** 31 - 1024) == BAD and call(N=2 ** 31 - 1024) == BAD
     assert call(T=0) == BAD and call(T=2 ** 31) == BAD and call(D=0) == BAD and call(N=0) == BAD
     assert call(D=72) == UNSUP and call(N=36) == UNSUP and call(D=131072) == UNSUP
     assert _status(lambda: abi.ispa_quantize_rows_i8(16, 10, 24, 16, 16)) == UNSUP
