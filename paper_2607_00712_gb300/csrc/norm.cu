@@ -419,30 +419,25 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1)
       }
       if constexpr (RES) {
         const __nv_bfloat16* ys = reinterpret_cast<const __nv_bfloat16*>(src + x_bytes);
-        float2 n = make_float2(0.f, 1.f);
-        if (p.post.kind != ISPA_NORM_NONE) {
-          float y[V][8];
+        float y[V][8];
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            if (i < vectors) {
-              Cols<XF32>(t + i * step, dim).bf16(ys, y[i]);
-            } else {
+        for (int i = 0; i < V; ++i) {
+          if (i < vectors) {
+            Cols<XF32>(t + i * step, dim).bf16(ys, y[i]);
+          } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[i][e] = 0.f;
-            }
+            for (int e = 0; e < 8; ++e) y[i][e] = 0.f;
           }
-          n = team_norm<V>(y, p.post, inv_dim, vectors, inv_own, other, tm);
         }
+        const float2 n = team_norm<V>(y, p.post, inv_dim, vectors, inv_own, other, tm);
 #pragma unroll
         for (int i = 0; i < V; ++i)
           if (i < vectors) {
             const Cols<XF32> cols(t + i * step, dim);
-            float y[8];
             load_x(i);
-            cols.bf16(ys, y);
             get(2, t + i * step, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = fmaf(fmaf(y[e], n.y, n.x), f[e], p.x_scale * x[i][e]);
+            for (int e = 0; e < 8; ++e) x[i][e] = fmaf(fmaf(y[i][e], n.y, n.x), f[e], p.x_scale * x[i][e]);
             if (p.post.bias) {
               get(3, t + i * step, f);
 #pragma unroll
