@@ -150,8 +150,9 @@ def _residual_case(rows, dim, fp32, post, pre, fmt, in_place, gate=True):
     lh.assert_within(got, want, (1 + half) * err + half * np.abs(want) + 1e-45)
     if pre is not None:   # of x as it was stored
         n2 = ol.norm(got, pre, EPS, w2, b2)
-        h = ol.modulate(n2, e[:, 4], e[:, 3], per)
-        _check(t, s, rows, h, lh.modulate_error(lh.norm_error(got, pre, EPS, w2, b2), n2, e[:, 4], e[:, 3], per), fmt)
+        sc, sh = (e[:, 4], e[:, 3]) if gate else (None, None)      # without vectors there is no modulation either
+        h = ol.modulate(n2, sc, sh, per)
+        _check(t, s, rows, h, lh.modulate_error(lh.norm_error(got, pre, EPS, w2, b2), n2, sc, sh, per), fmt)
 
 
 def test_one_pass_equals_the_two_calls():
