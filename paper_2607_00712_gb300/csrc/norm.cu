@@ -505,7 +505,10 @@ cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
   // Many rows, by what a team keeps in shared memory.  4680 x 1536 bf16: 9.5 us against 12.7 with a block a row, 620 x
   // 5120 (both norms) 8.4 against 12.0, 450 rows 6.1 against 6.5; below that, and with vectors of a few rows each (2:
   // 14.5 us a block a row), there is nothing for a team to keep.
-  const int team_warps = (nv + 127) / 128, v = (nv + 32 * team_warps - 1) / (32 * team_warps);
+  // Three vectors a thread in more warps where shared memory has room for their teams (5120 bf16, both norms 39.7 -> 37.2
+  // us, layer norms 48.9 -> 44.7; 5120 fp32, where it has not, 51.5 -> 55.7), else four.
+  const int few = (nv + 127) / 128, team_warps = XF32 ? few : std::max(few, std::min(TEAM_WARPS, (nv + 95) / 96));
+  const int v = (nv + 32 * team_warps - 1) / (32 * team_warps);
   const int fixed = 32 * (!RES ? 2 : p.post.bias ? 4 : 3) * nv;
   const int row_bytes = p.dim * ((XF32 ? 4 : 2) + (RES ? 2 : 0)), rest = 2 * 8 + 2 * TEAM_WARPS * 8;
   // registers, 15 named barriers, and what shared memory has room for
