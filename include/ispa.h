@@ -678,8 +678,9 @@ ISPA_API ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, 
 /*
  * W8A8 with int8 codes (Sec. 4 names no 8-bit format; checkpoints quantised after training mostly hold
  * integers), one fp32 scale per token for activations and one per output channel for weights:
- *   amax = max |x| over the group; inv = 127 / amax and scale = amax / 127 in fp32 (both 1 for an all-zero
- *   group); code = x * inv rounded to nearest even, in [-127, 127].
+ *   amax = max |x| over the group; inv = 127 / amax and scale = amax / 127 in fp32 (both 1, the codes 0, for
+ *   a group with amax < 2^-117, whose quotients fp32 does not hold); code = x * inv rounded to nearest
+ *   even, in [-127, 127].
  * A group with an infinity or a NaN has an infinite or NaN scale (its codes say nothing), so that what is
  * computed from it is no finite number.
  */
@@ -690,8 +691,8 @@ ISPA_API ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t 
                                            ispa_stream stream);
 
 /* Weight W (+ dW, nullable): fp32 [D][D_out] (row-vector convention y = a W) -> codes q_t [D_out][D] (K-major)
- * and scale fp32 [D_out], one per output channel of W + dW (summed in fp32).  D % 16 == 0.  Three launches;
- * once per weight update, not per step. */
+ * and scale fp32 [D_out], one per output channel of W + dW (summed in fp32).  D % 16 == 0 and D_out <= 2097120
+ * (else ISPA_ERR_UNSUPPORTED).  Three launches; once per weight update, not per step. */
 ISPA_API ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
                                              float* scale, ispa_stream stream);
 
@@ -752,7 +753,7 @@ typedef struct {
  *   amax = max |h| of the row (fp32, before any rounding to bf16);
  *   E4M3: scale = amax / 448, code = e4m3(h * (448 / amax)), as ispa_quantize_rows_e4m3 does;
  *   I8:   scale = amax / 127, code = round(h * (127 / amax)) to nearest even, in [-127, 127];
- *   an all-zero row has scale 1.  A row with an infinity or a NaN has an infinite or NaN scale (its
+ *   a row with amax < 2^-117 has scale 1 and zero codes.  A row with an infinity or a NaN has an infinite or NaN scale (its
  *   codes say nothing), so that what is computed from it is no finite number. */
 #define ISPA_ROWS_BF16 0
 #define ISPA_ROWS_E4M3 1

@@ -84,10 +84,10 @@ def frequencies(n, base, scaling="none", scale=1.0, trained=1.0, low=1.0, high=3
 
 
 def quantize_i8(x):
-    """fp32 rows -> (int8 codes, fp32 scales), each step in fp32."""
+    """fp32 rows -> (int8 codes, fp32 scales), each step in fp32; a row below 2^-117 counts as zeros."""
     x = np.asarray(x, np.float32)
     amax = np.abs(x).max(-1)
-    zero = amax == 0
+    zero = amax < 2.0 ** -117
     safe = np.where(zero, np.float32(1), amax).astype(np.float32)
     inv = np.where(zero, np.float32(1), np.float32(127) / safe).astype(np.float32)
     scale = np.where(zero, np.float32(1), safe / np.float32(127)).astype(np.float32)

@@ -881,7 +881,7 @@ ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int
 ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
                                     float* scale, ispa_stream stream) {
   if (!W || !q_t || !scale || D <= 0 || D_out <= 0 || !aligned16(q_t)) return ISPA_ERR_INVALID_ARG;
-  if (D % 16 != 0) return ISPA_ERR_UNSUPPORTED;
+  if (D % 16 != 0 || D_out > 32 * 65535) return ISPA_ERR_UNSUPPORTED;   // 32 channels a block, along the grid's y
   if (launch_quant_weight_i8(W, dW, D, D_out, q_t, scale, stream) != cudaSuccess) return ISPA_ERR_CUDA;
   return ISPA_OK;
 }

@@ -95,13 +95,6 @@ __device__ __forceinline__ void norm_row(float (&v)[V][8], const ispa_norm& n, i
   }
 }
 
-__device__ __forceinline__ uint32_t pack_i8x4(const float* f) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) r |= (static_cast<uint32_t>(__float2int_rn(f[e])) & 0xFFu) << (8 * e);
-  return r;
-}
-
 // One row a block, V vectors of eight values a thread.
 template <int V, bool XF32, bool RES>
 __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormParams p) {
@@ -195,21 +188,17 @@ __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormP
   if (p.format == ISPA_ROWS_BF16) return;
   amax = r.template all<MaxOp>(amax);
   const float top = p.format == ISPA_ROWS_E4M3 ? 448.f : 127.f;
-  const float inv = amax == 0.f ? 1.f : __fdiv_rn(top, amax);
+  const float inv = code_factor(amax, top);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int c = t + i * step;
     if (c < nv) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = __fmul_rn(x[i][e], inv);
       *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.out) + base + 8 * c) =
-          p.format == ISPA_ROWS_E4M3
-              ? make_uint2(pack_e4m3x4(x[i][0], x[i][1], x[i][2], x[i][3]),
-                           pack_e4m3x4(x[i][4], x[i][5], x[i][6], x[i][7]))
-              : make_uint2(pack_i8x4(x[i]), pack_i8x4(x[i] + 4));
+          p.format == ISPA_ROWS_E4M3 ? make_uint2(pack_e4m3x4(x[i], inv), pack_e4m3x4(x[i] + 4, inv))
+                                     : make_uint2(pack_i8x4(x[i], inv), pack_i8x4(x[i] + 4, inv));
     }
   }
-  if (t == 0) p.out_scale[row] = amax == 0.f ? 1.f : __fdiv_rn(amax, top);
+  if (t == 0) p.out_scale[row] = code_scale(amax, top);
 }
 
 // ------------------------------------------------------------ many rows
@@ -474,19 +463,16 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1)
           amax = warp_reduce<MaxOp>(amax);
           if (tm.warps > 1) amax = group_reduce<MaxOp>(tm.gather(make_float2(amax, 0.f)).x, TEAM_WARPS);
           const bool e4m3 = p.format == ISPA_ROWS_E4M3;
-          const float top = e4m3 ? 448.f : 127.f, inv = amax == 0.f ? 1.f : __fdiv_rn(top, amax);
+          const float top = e4m3 ? 448.f : 127.f, inv = code_factor(amax, top);
 #pragma unroll
           for (int i = 0; i < V; ++i)
             if (i < vectors) {
-              float* h = x[i];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) h[e] = __fmul_rn(h[e], inv);
+              const float* h = x[i];
               Cols<XF32>(t + i * step, dim)
-                  .put_codes(static_cast<uint8_t*>(p.out) + base,
-                             e4m3 ? pack_e4m3x4(h[0], h[1], h[2], h[3]) : pack_i8x4(h),
-                             e4m3 ? pack_e4m3x4(h[4], h[5], h[6], h[7]) : pack_i8x4(h + 4));
+                  .put_codes(static_cast<uint8_t*>(p.out) + base, e4m3 ? pack_e4m3x4(h, inv) : pack_i8x4(h, inv),
+                             e4m3 ? pack_e4m3x4(h + 4, inv) : pack_i8x4(h + 4, inv));
             }
-          if (t == 0) p.out_scale[row] = amax == 0.f ? 1.f : __fdiv_rn(amax, top);
+          if (t == 0) p.out_scale[row] = code_scale(amax, top);
         }
       }
       tm.sync();   // the row's stage is free

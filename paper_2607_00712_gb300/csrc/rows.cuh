@@ -35,6 +35,37 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// Below this largest magnitude a group counts as all zeros: the quotient 448 / amax (127 / amax) would be infinite and
+// amax / 448 lose bits of its mantissa.  Not for NaN.
+constexpr float kTinyGroup = 6.0185310762101e-36f;   // 2^-117
+__device__ __forceinline__ float code_factor(float amax, float top) {
+  return amax < kTinyGroup ? 1.f : __fdiv_rn(top, amax);
+}
+__device__ __forceinline__ float code_scale(float amax, float top) {
+  return amax < kTinyGroup ? 1.f : __fdiv_rn(amax, top);
+}
+
+// Four values of magnitude 127 at most, each rounded to the nearest even integer, as bytes.  Added to 1.5 * 2^23, whose
+// unit is one, a value leaves its integer in the low bits: an addition each and three byte permutes, where conversions
+// run at an eighth of that rate (int8 codes of 4680 x 5120 bf16 values 17.7 -> 14.7 us).
+constexpr float kToInteger = 12582912.f;
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                     __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t pack_i8x4(const float* f) {
+  return low_bytes(__fadd_rn(f[0], kToInteger), __fadd_rn(f[1], kToInteger), __fadd_rn(f[2], kToInteger),
+                   __fadd_rn(f[3], kToInteger));
+}
+// Of h * inv, rounded once.
+__device__ __forceinline__ uint32_t pack_i8x4(const float* h, float inv) {
+  return low_bytes(fmaf(h[0], inv, kToInteger), fmaf(h[1], inv, kToInteger), fmaf(h[2], inv, kToInteger),
+                   fmaf(h[3], inv, kToInteger));
+}
+__device__ __forceinline__ uint32_t pack_e4m3x4(const float* h, float inv) {
+  return pack_e4m3x4(__fmul_rn(h[0], inv), __fmul_rn(h[1], inv), __fmul_rn(h[2], inv), __fmul_rn(h[3], inv));
+}
+
 struct SumOp {
   static __device__ __forceinline__ float of(float a, float b) { return a + b; }
 };

@@ -57,11 +57,22 @@ __device__ __forceinline__ float amax_of(float a, float b) {
   return I8 ? max_nan(a, b) : fmaxf(a, b);
 }
 
-// Two fp32 values -> two codes, x0 in the low byte.
+// Four scaled fp32 values -> four codes, f[0] in the low byte.
 template <bool I8>
-__device__ __forceinline__ uint16_t code2(float x0, float x1) {
-  if constexpr (I8) return static_cast<uint16_t>((__float2int_rn(x0) & 0xFF) | (__float2int_rn(x1) & 0xFF) << 8);
-  else return e4m3x2(x0, x1);
+__device__ __forceinline__ uint32_t code4(const float* f) {
+  if constexpr (I8) return pack_i8x4(f);
+  else return static_cast<uint32_t>(e4m3x2(f[0], f[1])) | static_cast<uint32_t>(e4m3x2(f[2], f[3])) << 16;
+}
+
+template <bool I8>
+__device__ __forceinline__ float factor_of(float amax) {
+  if constexpr (I8) return code_factor(amax, kCodeMax<I8>);
+  else return amax == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, amax);
+}
+template <bool I8>
+__device__ __forceinline__ float scale_of(float amax) {
+  if constexpr (I8) return code_scale(amax, kCodeMax<I8>);
+  else return amax == 0.f ? 1.f : __fdiv_rn(amax, kCodeMax<I8>);
 }
 
 // One warp per row (grid-stride over rows); cols % 8 == 0.  Rows of up to 32 * CACHE
@@ -103,20 +114,14 @@ __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = amax_of<I8>(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const float inv = amax == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, amax);
+    const float inv = factor_of<I8>(amax);
     uint2* qr = reinterpret_cast<uint2*>(q + r * cols);
     auto quant8 = [&](const uint4& v) {
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t out[2];
+      float f[8];
+      unpack8(v, f);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint16_t lo = code2<I8>(__fmul_rn(__uint_as_float(w[2 * h] << 16), inv),
-                                      __fmul_rn(__uint_as_float(w[2 * h] & 0xFFFF0000u), inv));
-        const uint16_t hi = code2<I8>(__fmul_rn(__uint_as_float(w[2 * h + 1] << 16), inv),
-                                      __fmul_rn(__uint_as_float(w[2 * h + 1] & 0xFFFF0000u), inv));
-        out[h] = static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
-      }
-      return make_uint2(out[0], out[1]);
+      for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], inv);
+      return make_uint2(code4<I8>(f), code4<I8>(f + 4));
     };
 #pragma unroll
     for (int c = 0; c < CACHE; ++c) {
@@ -124,8 +129,59 @@ __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <
       if (i < nw) qr[i] = quant8(cache[c]);
     }
     for (int i = lane + 32 * CACHE; i < nw; i += 32) qr[i] = quant8(xr[i]);
-    if (lane == 0) scale[r] = amax == 0.f ? 1.f : __fdiv_rn(amax, kCodeMax<I8>);
+    if (lane == 0) scale[r] = scale_of<I8>(amax);
   }
+}
+
+// The same for rows that are too long for a warp's registers, int8 codes: WARPS warps a row, 8 / WARPS rows a block.
+// Rows of up to 32 * WARPS * CACHE words are read once.
+template <int CACHE, int WARPS>
+__global__ void __launch_bounds__(256) quant_long_rows_kernel(const __nv_bfloat16* __restrict__ x, int64_t rows,
+                                                              int cols, uint8_t* __restrict__ q,
+                                                              float* __restrict__ scale) {
+  __shared__ float part[8];
+  pdl_wait();
+  pdl_trigger();
+  constexpr int STEP = 32 * WARPS;
+  const int t = threadIdx.x % STEP, team = threadIdx.x / STEP, nw = cols / 8;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (256 / STEP) + team;
+  const bool live = r < rows;   // a whole team
+  const uint4* xr = reinterpret_cast<const uint4*>(x + (live ? r : 0) * cols);
+  float amax = 0.f;
+  auto look = [&](const uint4& v) {
+    float f[8];
+    unpack8(v, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = amax_of<true>(amax, fabsf(f[e]));
+  };
+  uint4 cache[CACHE];
+#pragma unroll
+  for (int c = 0; c < CACHE; ++c) cache[c] = live && t + STEP * c < nw ? xr[t + STEP * c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int c = 0; c < CACHE; ++c) look(cache[c]);
+  if (live)
+    for (int i = t + STEP * CACHE; i < nw; i += STEP) look(xr[i]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) amax = amax_of<true>(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) amax = amax_of<true>(amax, part[team * WARPS + i]);
+  if (!live) return;
+  const float inv = factor_of<true>(amax);
+  uint2* qr = reinterpret_cast<uint2*>(q + r * cols);
+  auto put = [&](int i, const uint4& v) {
+    float f[8];
+    unpack8(v, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], inv);
+    qr[i] = make_uint2(code4<true>(f), code4<true>(f + 4));
+  };
+#pragma unroll
+  for (int c = 0; c < CACHE; ++c)
+    if (t + STEP * c < nw) put(t + STEP * c, cache[c]);
+  for (int i = t + STEP * CACHE; i < nw; i += STEP) put(i, xr[i]);
+  if (t == 0) scale[r] = scale_of<true>(amax);
 }
 
 __device__ __forceinline__ float w_plus_dw(const float* W, const float* dW, int64_t i) {
@@ -160,13 +216,13 @@ __global__ void quant_wt_kernel(const float* __restrict__ W, const float* __rest
   const int k0 = blockIdx.x * 32, n0 = blockIdx.y * 32;
   const int n = n0 + threadIdx.x;
   const float am = n < Dout ? amax[n] : 0.f;
-  const float inv = am == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, am);
+  const float inv = factor_of<I8>(am);
   for (int j = threadIdx.y; j < 32; j += 8) {
     const int k = k0 + j;
     uint8_t c = 0;
     if (k < D && n < Dout) {
-      const float v = __fmul_rn(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n), inv);
-      c = static_cast<uint8_t>(code2<I8>(v, 0.f) & 0xFF);
+      const float v[4] = {__fmul_rn(w_plus_dw(W, dW, static_cast<int64_t>(k) * Dout + n), inv)};
+      c = static_cast<uint8_t>(code4<I8>(v) & 0xFF);
     }
     tile[j][threadIdx.x] = c;   // [k][n]
   }
@@ -180,7 +236,7 @@ __global__ void quant_wt_kernel(const float* __restrict__ W, const float* __rest
 template <bool I8>
 __global__ void col_scale_kernel(float* __restrict__ s, int Dout) {
   const int n = blockIdx.x * blockDim.x + threadIdx.x;
-  if (n < Dout) s[n] = s[n] == 0.f ? 1.f : __fdiv_rn(s[n], kCodeMax<I8>);
+  if (n < Dout) s[n] = scale_of<I8>(s[n]);
 }
 
 // ------------------------------------------------------------ GEMM
@@ -555,6 +611,18 @@ cudaError_t launch_rows(const void* x, int64_t rows, int32_t cols, uint8_t* q, f
   // at once.  4680 x 1536: 4.4 -> 3.2 us, 9400 x 1024: 7.0 -> 4.0 (against 12 words a lane for every row).  Rows of
   // more than 3072 values keep 12 and read the rest twice: with 20 only 8 warps a SM fit, 8.1 -> 10.2 us at 5120.
   const int words = (cols / 8 + 31) / 32;
+  if constexpr (I8) {
+    // Int8 codes: rows of more than 12 words a lane by several warps.  4680 x 5120 14.7 us a warp a row, 15.9 two, 12.5
+    // four; 4680 x 8960 26 four, 20.8 eight; 9400 x 13824 73.9 five words a thread, 57.9 seven; of 2560 values 8.2 a
+    // warp a row, 8.3 two, 9.3 four.  64 x 5120 3.0 -> 1.6.
+    const auto go = [&](auto long_rows, int per_block) {
+      return launch_pdl(long_rows, dim3(static_cast<unsigned>((rows + per_block - 1) / per_block)), dim3(256), 0, s,
+                        static_cast<const __nv_bfloat16*>(x), rows, static_cast<int>(cols), q, scale);
+    };
+    if (words > 40) return go(quant_long_rows_kernel<7, 8>, 1);
+    if (words > 20) return go(quant_long_rows_kernel<5, 8>, 1);
+    if (words > 12) return go(quant_long_rows_kernel<5, 4>, 2);
+  }
   const auto kernel = words <= 4   ? quant_rows_kernel<4, I8>
                       : words <= 6 ? quant_rows_kernel<6, I8>
                       : words <= 8 ? quant_rows_kernel<8, I8>

@@ -53,7 +53,7 @@ def check_codes(codes, scale, h, err, fmt):
     """Codes of the rows h (fp32 error err) in a format: the scale, then every value the codes stand for."""
     top = 448.0 if fmt == "e4m3" else 127.0
     amax = np.abs(h).max(-1)
-    want = np.where(amax == 0, 1.0, amax / top)
+    want = np.where(amax < 2.0 ** -117, 1.0, amax / top)
     # amax is off by at most the row's largest err; one division
     assert_within(scale, want, 2 * U * want + err.max(-1) / top + 1e-45, "scale")
     s = np.asarray(scale, np.float64)[:, None]

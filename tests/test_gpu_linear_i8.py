@@ -146,6 +146,32 @@ def test_quantized_rows(T, D):
     assert (q[T] == 77).all() and s[T] == 7.0
 
 
+# a row shared by two or eight warps of a block, a block's last row missing, rows that run past what the block holds
+@pytest.mark.parametrize("T,D", [(1, 3216), (2, 4096), (3, 5120), (5, 5136), (1, 10240), (3, 10256), (2, 16400), (301, 8960)])
+def test_quantized_long_rows(T, D):
+    test_quantized_rows(T, D)
+
+
+# 2^-117 and what is below it (subnormal values too), on both sides of the quotients that fp32 holds
+@pytest.mark.parametrize("D", [64, 1536, 5120])
+def test_groups_of_tiny_values(D):
+    g = np.random.default_rng(D)
+    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -8), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126, 2.0 ** -133,
+                    0.0], np.float32)
+    x = synth.bf16_round(((2 * g.random((len(top), D)) - 1) * 0.99 * top[:, None]).astype(np.float32))
+    x[:, 5], x[:, 7], x[:, 9] = top, -top, 0
+    codes, scale = ol.quantize_i8(x)
+    assert (scale[:2] != 1).all() and (scale[2:] == 1).all() and not codes[2:].any() and codes[1, 5] == 127
+    T = len(top)
+    q, s = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    abi.ispa_quantize_rows_i8(torch.from_numpy(x).cuda().to(torch.bfloat16), T, D, q, s)
+    qw, sw = torch.empty(T, D, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    abi.ispa_quantize_weight_i8(torch.from_numpy(np.ascontiguousarray(x.T)).cuda(), None, D, T, qw, sw)
+    torch.cuda.synchronize()
+    for codes_of, scale_of in ((q, s), (qw, sw)):
+        assert np.array_equal(codes_of.cpu().numpy(), codes) and np.array_equal(scale_of.cpu().numpy(), scale)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_a_non_finite_row_is_no_finite_result(bad):
     T, D, N = 20, 2064, 64

@@ -10,6 +10,7 @@ torch = pytest.importorskip("torch")
 
 import layer_helpers as lh  # noqa: E402
 from oracle import layer as ol  # noqa: E402
+from oracle.quant import decode as ol_decode  # noqa: E402
 from paper_2607_00712_gb300 import abi, synth  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -179,6 +180,29 @@ def test_rows_of_zeros(fmt):
         abi.ispa_norm_modulate(xt, abi.ISPA_BF16, 4, 64, abi.norm(kind), None, out)
         torch.cuda.synchronize()
         assert (t[:4] == 0).all() and (s is None or (s[:4] == 1).all())
+
+
+# Codes of rows about 2^-117, below which a row counts as zeros; no norm, whose output is the row itself in fp32.
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("rows,dim", [(8, 64), (8, 5120), (1304, 1536)])   # a block a row, and many rows
+def test_rows_of_tiny_values(rows, dim, fmt):
+    g = np.random.default_rng(dim)
+    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -20), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126, 2.0 ** -140,
+                    0.0], np.float32)
+    top = np.resize(top, rows)
+    x = ((2 * g.random((rows, dim)) - 1) * 0.99 * top[:, None]).astype(np.float32)
+    x[:, 5], x[:, 7], x[:, 9] = top, -top, 0
+    t, s, out = _out(rows, dim, fmt)
+    abi.ispa_norm_modulate(_cuda(x), abi.ISPA_FP32, rows, dim, abi.norm(ol.NONE), None, out)
+    torch.cuda.synchronize()
+    tiny = top < 2.0 ** -117
+    largest = 448.0 if fmt == "e4m3" else 127.0
+    want = np.where(tiny, np.float32(1), top / np.float32(largest)).astype(np.float32)
+    assert np.array_equal(s[:rows].cpu().numpy(), want)
+    codes = t[:rows].cpu().numpy()
+    value = ol_decode(codes) if fmt == "e4m3" else codes.astype(np.float64)   # e4m3 has a negative zero
+    assert not value[tiny].any()
+    assert (value[~tiny, 5] == largest).all() and (value[~tiny, 7] == -largest).all() and not value[:, 9].any()
 
 
 def test_constant_rows_and_a_large_offset():

@@ -103,6 +103,7 @@ def test_linear_i8_refusals():
     assert _status(lambda: abi.ispa_quantize_rows_i8(16, 0, 32, 16, 16)) == BAD
     assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 24, 32, 16, 16)) == UNSUP
     assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 32, 0, 16, 16)) == BAD
+    assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 16, 2097121, 16, 16)) == UNSUP
 
 
 def test_rope_refusals():
