@@ -460,18 +460,19 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1)
             }
           }
         if (p.format != ISPA_ROWS_BF16) {
-          amax = warp_reduce<MaxOp>(amax);
-          if (tm.warps > 1) amax = group_reduce<MaxOp>(tm.gather(make_float2(amax, 0.f)).x, TEAM_WARPS);
+          amax = warp_max(amax);
+          if (tm.warps > 1) amax = warp_max(tm.gather(make_float2(amax, 0.f)).x);
           const bool e4m3 = p.format == ISPA_ROWS_E4M3;
           const float top = e4m3 ? 448.f : 127.f, inv = code_factor(amax, top);
+          const auto put = [&](auto&& pack) {
 #pragma unroll
-          for (int i = 0; i < V; ++i)
-            if (i < vectors) {
-              const float* h = x[i];
-              Cols<XF32>(t + i * step, dim)
-                  .put_codes(static_cast<uint8_t*>(p.out) + base, e4m3 ? pack_e4m3x4(h, inv) : pack_i8x4(h, inv),
-                             e4m3 ? pack_e4m3x4(h + 4, inv) : pack_i8x4(h + 4, inv));
-            }
+            for (int i = 0; i < V; ++i)
+              if (i < vectors)
+                Cols<XF32>(t + i * step, dim)
+                    .put_codes(static_cast<uint8_t*>(p.out) + base, pack(x[i]), pack(x[i] + 4));
+          };
+          if (e4m3) put([&](const float* h) { return pack_e4m3x4(h, inv); });
+          else put([&](const float* h) { return pack_i8x4(h, inv); });
           if (t == 0) p.out_scale[row] = code_scale(amax, top);
         }
       }

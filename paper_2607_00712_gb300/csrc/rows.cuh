@@ -85,6 +85,11 @@ __device__ __forceinline__ float warp_reduce(float v) {
   for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
+// The largest of a warp's values, none of them negative: their order is their bits', NaN above all (one instruction, where
+// the shuffles of the sums take ten).
+__device__ __forceinline__ float warp_max(float v) {
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
+}
 // Op over the block's `warps` warps (at most 32); every thread gets it.  `slot` (0 or 1) alternates from one call of
 // a kernel to the next, so that one barrier a call is enough: a slot is written again only after the barrier of the
 // call in between, which every thread reaches after its reads.

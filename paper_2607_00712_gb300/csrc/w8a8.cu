@@ -112,8 +112,7 @@ __global__ void __launch_bounds__(256, CACHE <= 4 ? 5 : CACHE <= 6 ? 4 : CACHE <
         amax = amax_of<I8>(amax, amax_of<I8>(fabsf(__uint_as_float(w[e] << 16)),
                                              fabsf(__uint_as_float(w[e] & 0xFFFF0000u))));
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = amax_of<I8>(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    amax = warp_max(amax);
     const float inv = factor_of<I8>(amax);
     uint2* qr = reinterpret_cast<uint2*>(q + r * cols);
     auto quant8 = [&](const uint4& v) {
@@ -161,8 +160,7 @@ __global__ void __launch_bounds__(256) quant_long_rows_kernel(const __nv_bfloat1
   for (int c = 0; c < CACHE; ++c) look(cache[c]);
   if (live)
     for (int i = t + STEP * CACHE; i < nw; i += STEP) look(xr[i]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) amax = amax_of<true>(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  amax = warp_max(amax);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
   __syncthreads();
 #pragma unroll
