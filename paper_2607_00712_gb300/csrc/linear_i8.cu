@@ -19,8 +19,8 @@
 // accumulators back, two sets in TMEM in turn.  Their int32 sums take up to 96 registers a thread, so the warpgroups
 // share the registers out anew (setmaxnreg).  Every wait is bounded.
 //
-// 4680 x 5120 -> 5120 149.8 us, 1638 TFLOP/s; 4680 x 1536 -> 4608 46.4 us; 61 x 5120 -> 640 9.0 us; one token of
-// 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit: a block of 192 columns takes 0.25 us where its
+// 4680 x 5120 -> 5120 149.8 us, 1638 TFLOP/s, with operands and result in L2, 160 from and to HBM; 4680 x 1536 -> 4608
+// 46.4 us; 61 x 5120 -> 640 9.0 us; one token of 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit: a block of 192 columns takes 0.25 us where its
 // UMMAs take 0.19, a team 0.47 us for a block (there are three), and the ring of four stages, from one block's
 // conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave 134 us, three quarters of the UMMAs
 // 143.  On the way: one team of eight converter warps 405 us, four teams of two 218; a release at cluster scope a

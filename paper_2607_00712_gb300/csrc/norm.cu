@@ -18,12 +18,13 @@
 //                   factors of the columns (weights, gate, modulation) kept there per group of rows
 //   norm_kernel     few rows, very long ones, or vectors that change every few rows: a block a row
 //
-// Gate, residual and two RMS norms of 4680 x 5120 bf16: 38.6 us, 73 % of the measured copy rate.  With a block a row 59
+// Gate, residual and two RMS norms of 4680 x 5120 bf16: 37.1 us, 76 % of the measured copy rate.  With a block a row 59
 // us (the vectors, fp32, were 2.5 times the rows' own bytes through L1); with the factors in registers and the next
 // row's loads too, 48 (one team of 640 threads an SM: nothing to do while it reduces); with one vector of eight a
 // thread and everything in shared memory, 59 (the reductions' instructions); loads into registers instead of bulk
-// copies, 53.  A layer norm takes 47: its mean, then its squares, are two reductions in a row.  Norm of 4680 x 1536
-// bf16: 9.5 us, of which 3.3 are launch, factors and the last rows' way out; one row of 1536 2.4 us.
+// copies, 53.  Layer norms take 44.6: the mean, then the squares, are two reductions in a row.  Norm of 4680 x 1536
+// bf16: 9.4 us, of which 4 are launch, factors and the last rows' way out (each further row at 84 % of the copy rate);
+// with a warp a row, the vectors from L1, 10.7.  One row of 1536 2.4 us.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -492,8 +493,8 @@ cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
   // Many rows, by what a team keeps in shared memory.  4680 x 1536 bf16: 9.5 us against 12.7 with a block a row, 620 x
   // 5120 (both norms) 8.4 against 12.0, 450 rows 6.1 against 6.5; below that, and with vectors of a few rows each (2:
   // 14.5 us a block a row), there is nothing for a team to keep.
-  // Three vectors a thread in more warps where shared memory has room for their teams (5120 bf16, both norms 39.7 -> 37.2
-  // us, layer norms 48.9 -> 44.7; 5120 fp32, where it has not, 51.5 -> 55.7), else four.
+  // Three vectors a thread in more warps where shared memory has room for their teams (5120 bf16, both norms 39.7 ->
+  // 37.2 us, layer norms 48.9 -> 44.7; 5120 fp32, where it has not, 51.5 -> 55.7), else four.
   const int few = (nv + 127) / 128, team_warps = XF32 ? few : std::max(few, std::min(TEAM_WARPS, (nv + 95) / 96));
   const int v = (nv + 32 * team_warps - 1) / (32 * team_warps);
   const int fixed = 32 * (!RES ? 2 : p.post.bias ? 4 : 3) * nv;

@@ -19,10 +19,10 @@
 // that no pair is spread over two lanes.  A warp's lanes are dealt to heads in groups of a power of two, so a lane
 // meets the same features, angles and weights in every head.
 //
-// Queries and keys of 4680 x 40 heads of 128, norm over the token: 38.1 us, 74 % of the measured copy rate (32.9
-// without the norm); 12 heads 14.9 us, of which 7 are the start (angles, weights); one token 2.0 us.  Angles made by
+// Queries and keys of 4680 x 40 heads of 128, norm over the token: 39.6 us, 71 % of the measured copy rate (32.9
+// without the norm); 12 heads 15.8 us, of which 7 are the start (angles, weights); one token 2.0 us.  Angles made by
 // every warp for itself cost more than its heads: 69 us, and 58 for 3117 tokens of 24 and 8 heads in the half layout
-// (17.5 now); a warp a token with its row in registers 77 (164 registers, too few warps).
+// (16.9 now); a warp a token with its row in registers 77 (164 registers, too few warps).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     if (NORM == ISPA_QK_NORM_HEAD && o.weight && live) ln.weight(o.weight, w);
     // every lane goes round alike: a head's sum needs all of them
-    // Four heads of a lane side by side where each has a sum to wait for (3117 tokens of 24 and 8 heads 18.0 -> 16.8 us,
-    // 1560 of 160 and 40 44 -> 38); the others are slower so (4680 x 2 x 5120 39.7 -> 43).
+    // Four heads of a lane side by side where each has a sum to wait for (3117 tokens of 24 and 8 heads 18.0 -> 16.9
+    // us, 1560 of 160 and 40 44 -> 38); the others are slower so (4680 x 2 x 5120 39.7 -> 43).
     constexpr int kAhead = NORM == ISPA_QK_NORM_HEAD ? 4 : 2;
     int h = head0;
 #pragma unroll kAhead

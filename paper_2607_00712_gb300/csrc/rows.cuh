@@ -85,8 +85,8 @@ __device__ __forceinline__ float warp_reduce(float v) {
   for (int o = 16; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-// The largest of a warp's values, none of them negative: their order is their bits', NaN above all (one instruction, where
-// the shuffles of the sums take ten).
+// The largest of a warp's values, none of them negative: their order is their bits', NaN above all (one instruction,
+// where the shuffles of the sums take ten).
 __device__ __forceinline__ float warp_max(float v) {
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }

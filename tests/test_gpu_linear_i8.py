@@ -147,7 +147,8 @@ def test_quantized_rows(T, D):
 
 
 # a row shared by two or eight warps of a block, a block's last row missing, rows that run past what the block holds
-@pytest.mark.parametrize("T,D", [(1, 3216), (2, 4096), (3, 5120), (5, 5136), (1, 10240), (3, 10256), (2, 16400), (301, 8960)])
+@pytest.mark.parametrize("T,D", [(1, 3216), (2, 4096), (3, 5120), (5, 5136), (1, 10240), (3, 10256), (2, 16400),
+                                 (301, 8960)])
 def test_quantized_long_rows(T, D):
     test_quantized_rows(T, D)
 
@@ -156,8 +157,8 @@ def test_quantized_long_rows(T, D):
 @pytest.mark.parametrize("D", [64, 1536, 5120])
 def test_groups_of_tiny_values(D):
     g = np.random.default_rng(D)
-    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -8), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126, 2.0 ** -133,
-                    0.0], np.float32)
+    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -8), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126,
+                    2.0 ** -133, 0.0], np.float32)
     x = synth.bf16_round(((2 * g.random((len(top), D)) - 1) * 0.99 * top[:, None]).astype(np.float32))
     x[:, 5], x[:, 7], x[:, 9] = top, -top, 0
     codes, scale = ol.quantize_i8(x)

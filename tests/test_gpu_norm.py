@@ -187,8 +187,8 @@ def test_rows_of_zeros(fmt):
 @pytest.mark.parametrize("rows,dim", [(8, 64), (8, 5120), (1304, 1536)])   # a block a row, and many rows
 def test_rows_of_tiny_values(rows, dim, fmt):
     g = np.random.default_rng(dim)
-    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -20), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126, 2.0 ** -140,
-                    0.0], np.float32)
+    top = np.array([2.0 ** -116, 2.0 ** -117, 2.0 ** -117 * (1 - 2.0 ** -20), 2.0 ** -119, 2.0 ** -121, 2.0 ** -126,
+                    2.0 ** -140, 0.0], np.float32)
     top = np.resize(top, rows)
     x = ((2 * g.random((rows, dim)) - 1) * 0.99 * top[:, None]).astype(np.float32)
     x[:, 5], x[:, 7], x[:, 9] = top, -top, 0
