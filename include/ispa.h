@@ -685,19 +685,20 @@ ISPA_API ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, 
  * computed from it is no finite number.
  */
 
+/* Largest D of ispa_linear_i8: D * 128 * 128 stays below 2^31. */
+#define ISPA_LINEAR_I8_MAX_D 131056
+
 /* Activations x: bf16 [rows][cols] -> codes q [rows][cols], scale fp32 [rows].  cols % 16 == 0 (else
  * ISPA_ERR_UNSUPPORTED); x and q 16-byte aligned. */
 ISPA_API ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale,
                                            ispa_stream stream);
 
 /* Weight W (+ dW, nullable): fp32 [D][D_out] (row-vector convention y = a W) -> codes q_t [D_out][D] (K-major)
- * and scale fp32 [D_out], one per output channel of W + dW (summed in fp32).  D % 16 == 0 and D_out <= 2097120
- * (else ISPA_ERR_UNSUPPORTED).  Three launches; once per weight update, not per step. */
+ * and scale fp32 [D_out], one per output channel of W + dW (summed in fp32).  D % 16 == 0,
+ * D <= ISPA_LINEAR_I8_MAX_D and D_out <= 2097120 (else ISPA_ERR_UNSUPPORTED); q_t 16-byte aligned.  Three
+ * launches; once per weight update, not per step. */
 ISPA_API ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
                                              float* scale, ispa_stream stream);
-
-/* Largest D of ispa_linear_i8: D * 128 * 128 stays below 2^31. */
-#define ISPA_LINEAR_I8_MAX_D 131056
 
 /* out: bf16 [T][D_out] = sum_k a_q[t][k] * w_q[n][k] * a_scale[t] * w_scale[n] + bias[n].  The sum is the exact
  * integer whatever T, for any codes in [-128, 127]; then, in fp32, each step rounded to nearest: the integer, times
@@ -815,7 +816,8 @@ typedef struct {
 
 /* One of the tensors to turn: bf16, token t's heads at x + t * x_stride, [heads][head_dim] dense.
  * Strides in values, at least heads * head_dim and multiples of 8 (16 bytes): q and k may be columns of
- * a fused projection.  out may be x with the same stride; else they must not overlap. */
+ * a fused projection.  out may be x with the same stride; else they must not overlap, nor may one tensor's out
+ * and the other's x or out. */
 typedef struct {
   const void* x;
   void* out;

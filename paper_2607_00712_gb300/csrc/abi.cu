@@ -525,6 +525,7 @@ __global__ void wait_probe_kernel(uint64_t limit_ns, int* status) {
 }
 
 bool aligned16_or_null(const void* p) { return !p || aligned16(p); }
+bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 bool good_norm(const ispa_norm* n) {
   return n->kind >= ISPA_NORM_NONE && n->kind <= ISPA_NORM_LAYER && n->eps >= 0.f && isfinite(n->eps) &&
@@ -542,7 +543,7 @@ ispa_status norm_params(NormParams& p, const void* x, int32_t x_type, int64_t ro
               !aligned16_or_null(mod->shift) || !aligned16_or_null(mod->gate)))
     return ISPA_ERR_INVALID_ARG;
   if (out && (!aligned16(out->data) || out->format < ISPA_ROWS_BF16 || out->format > ISPA_ROWS_I8 ||
-              (out->format != ISPA_ROWS_BF16 && !out->scale)))
+              (out->format != ISPA_ROWS_BF16 && !aligned4(out->scale))))
     return ISPA_ERR_INVALID_ARG;
   if (dim % 8 != 0 || dim > kMaxNormDim || rows > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
   const ispa_norm none{ISPA_NORM_NONE, 0.f, nullptr, nullptr};
@@ -872,7 +873,7 @@ ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, const uin
 
 ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int8_t* q, float* scale,
                                   ispa_stream stream) {
-  if (!x || !q || !scale || rows <= 0 || cols <= 0 || !aligned16(x) || !aligned16(q)) return ISPA_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(q) || !aligned4(scale) || rows <= 0 || cols <= 0) return ISPA_ERR_INVALID_ARG;
   if (cols % 16 != 0) return ISPA_ERR_UNSUPPORTED;
   if (launch_quant_rows_i8(x, rows, cols, q, scale, stream) != cudaSuccess) return ISPA_ERR_CUDA;
   return ISPA_OK;
@@ -880,16 +881,18 @@ ispa_status ispa_quantize_rows_i8(const void* x, int64_t rows, int32_t cols, int
 
 ispa_status ispa_quantize_weight_i8(const float* W, const float* dW, int32_t D, int32_t D_out, int8_t* q_t,
                                     float* scale, ispa_stream stream) {
-  if (!W || !q_t || !scale || D <= 0 || D_out <= 0 || !aligned16(q_t)) return ISPA_ERR_INVALID_ARG;
-  if (D % 16 != 0 || D_out > 32 * 65535) return ISPA_ERR_UNSUPPORTED;   // 32 channels a block, along the grid's y
+  if (!aligned4(W) || (dW && !aligned4(dW)) || !aligned16(q_t) || !aligned4(scale) || D <= 0 || D_out <= 0)
+    return ISPA_ERR_INVALID_ARG;
+  if (D % 16 != 0 || D > ISPA_LINEAR_I8_MAX_D || D_out > 32 * 65535)   // 32 channels a block, along the grid's y
+    return ISPA_ERR_UNSUPPORTED;
   if (launch_quant_weight_i8(W, dW, D, D_out, q_t, scale, stream) != cudaSuccess) return ISPA_ERR_CUDA;
   return ISPA_OK;
 }
 
 ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
                            const float* bias, int64_t T, int32_t D, int32_t D_out, void* out, ispa_stream stream) {
-  if (!aligned16(a_q) || !a_scale || !aligned16(w_q) || !w_scale || !aligned16(out) || T <= 0 || D <= 0 || D_out <= 0 ||
-      T > INT32_MAX - 1024 || D_out > INT32_MAX - 1024)
+  if (!aligned16(a_q) || !aligned4(a_scale) || !aligned16(w_q) || !aligned4(w_scale) || (bias && !aligned4(bias)) ||
+      !aligned16(out) || T <= 0 || D <= 0 || D_out <= 0 || T > INT32_MAX - 1024 || D_out > INT32_MAX - 1024)
     return ISPA_ERR_INVALID_ARG;
   if (D % 16 != 0 || D > ISPA_LINEAR_I8_MAX_D || D_out % 8 != 0) return ISPA_ERR_UNSUPPORTED;
   int* status = device_status_ptr();

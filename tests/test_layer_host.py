@@ -67,7 +67,7 @@ def test_norm_refusals():
         assert call(norm=abi.norm(1, eps)) == BAD
     assert call(norm=abi.norm(1, 1e-6, 24)) == BAD and call(norm=abi.norm(1, 1e-6, None, 20)) == BAD
     assert call(out=abi.rows_out(None)) == BAD and call(out=abi.rows_out(24)) == BAD
-    assert call(out=abi.rows_out(16, 3, 16)) == BAD
+    assert call(out=abi.rows_out(16, 3, 16)) == BAD and call(out=abi.rows_out(16, abi.ISPA_ROWS_I8, 18)) == BAD
     assert call(out=abi.rows_out(16, abi.ISPA_ROWS_E4M3)) == BAD and call(out=abi.rows_out(16, abi.ISPA_ROWS_I8)) == BAD
     for mod in (abi.modulation(16, 16, None, 64, 0), abi.modulation(16, 16, None, -64, 1),
                 abi.modulation(16, 16, None, 66, 1), abi.modulation(20, 16, None, 64, 1),
@@ -104,6 +104,12 @@ def test_linear_i8_refusals():
     assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 24, 32, 16, 16)) == UNSUP
     assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 32, 0, 16, 16)) == BAD
     assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 16, 2097121, 16, 16)) == UNSUP
+    assert _status(lambda: abi.ispa_quantize_weight_i8(16, None, 131072, 16, 16, 16)) == UNSUP
+    # fp32 arrays off their four bytes
+    assert call(sa=18) == BAD and call(sw=17) == BAD and call(bias=22) == BAD
+    assert _status(lambda: abi.ispa_quantize_rows_i8(16, 10, 32, 16, 18)) == BAD
+    for W, dW, s in ((18, None, 16), (16, 18, 16), (16, None, 18)):
+        assert _status(lambda: abi.ispa_quantize_weight_i8(W, dW, 32, 32, 16, s)) == BAD
 
 
 def test_rope_refusals():
