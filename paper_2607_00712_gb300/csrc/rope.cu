@@ -19,10 +19,10 @@
 // that no pair is spread over two lanes.  A warp's lanes are dealt to heads in groups of a power of two, so a lane
 // meets the same features, angles and weights in every head.
 //
-// Queries and keys of 4680 x 40 heads of 128, norm over the token: 39.6 us, 71 % of the measured copy rate (32.9
-// without the norm); 12 heads 15.8 us, of which 7 are the start (angles, weights); one token 2.0 us.  Angles made by
-// every warp for itself cost more than its heads: 69 us, and 58 for 3117 tokens of 24 and 8 heads in the half layout
-// (16.9 now); a warp a token with its row in registers 77 (164 registers, too few warps).
+// Queries and keys of 4680 x 40 heads of 128, norm over the token: 39.0 us, 72 % of the measured copy rate (33.5
+// without the norm); 12 heads 15.2 us, 13.4 with a norm per head, of which 6 are the start (angles, weights); one token
+// 2.0 us.  Angles made by every warp for itself cost more than its heads: 69 us, and 58 for 3117 tokens of 24 and 8
+// heads in the half layout (15.4 now); a warp a token with its row in registers 77 (164 registers, too few warps).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -177,14 +177,14 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeP
 
 // ------------------------------------------------------------ many tokens
 constexpr int R_SMEM = 224 * 1024;
-constexpr int R_TABLE = 128 * 8;   // bytes of a team's cosines and sines
 constexpr uint64_t R_DRAIN_NS = 200ull * 1000 * 1000;
 
 // Block (32 * warps of a team, teams), one an SM; block b takes tokens [b, b + 1) * per_block, its teams in turn.  A
 // token's queries and keys come through shared memory by bulk copies, a team's next token while it works on one;
 // weights of a norm over the token's heads stand there too, the eight of a lane in two planes, so that a warp reads
-// whole lines. NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
-template <bool HALF, int NORM, bool FULL>
+// whole lines.  NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
+// STAGES: tokens of a team in shared memory, one where all of the block's tokens fit at once.
+template <bool HALF, int NORM, bool FULL, int STAGES>
 __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_constant__ RopeParams p, int per_block) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int abort_word;
@@ -197,10 +197,11 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   constexpr bool kWeights = NORM == ISPA_QK_NORM_TOKEN;
   const int n0 = p.rows[0].heads * d, n1 = p.n_rows > 1 ? p.rows[1].heads * d : 0, r_bytes = 2 * (n0 + n1);
   const int w_bytes = kWeights ? 4 * (n0 + n1) : 0;
-  uint8_t* const rows = smem + w_bytes + 2 * r_bytes * threadIdx.y;
-  uint8_t* at = smem + w_bytes + 2 * r_bytes * teams;
-  float2* const table = reinterpret_cast<float2*>(at + R_TABLE * threadIdx.y);
-  at += R_TABLE * teams;
+  uint8_t* const rows = smem + w_bytes + STAGES * r_bytes * threadIdx.y;
+  uint8_t* at = smem + w_bytes + STAGES * r_bytes * teams;
+  const int table_bytes = (8 * p.pairs + 15) & ~15;   // a team's cosines and sines
+  float2* const table = reinterpret_cast<float2*>(at + table_bytes * threadIdx.y);
+  at += table_bytes * teams;
   const uint32_t full = smem_u32(at + 16 * threadIdx.y);
   at += 16 * teams;
   Team tm{reinterpret_cast<float2*>(at) + threadIdx.y * 2 * TEAM_WARPS, threads >> 5,
@@ -217,6 +218,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   const WaitCtx wc{&abort_word, p.status, p.wait_limit_ns};
   const int first = blockIdx.x * per_block;   // tokens are fewer than 2^30
   const int last = static_cast<int>(min(static_cast<int64_t>(first) + per_block, p.n));
+  const auto stage_of = [&](uint32_t i) { return i & (STAGES - 1); };
+  const auto parity_of = [&](uint32_t i) { return (i >> (STAGES - 1)) & 1; };
   auto fetch = [&](int tok, int stage) {
     mbar_arrive_expect_tx(full + 8 * stage, r_bytes);
     const uint32_t dst = smem_u32(rows) + stage * r_bytes;
@@ -228,7 +231,7 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   int tok = first + threadIdx.y;
   uint32_t issued = 0;   // (thread 0) tokens that it has sent for
   bool ok = true;
-  if (t == 0 && tok < last) fetch(tok, issued++ & 1);
+  if (t == 0 && tok < last) fetch(tok, stage_of(issued++));
   // This thread's pairs t, t + threads, ...: their steps, and their position at the team's next token.
   uint64_t step[4];
   int pos[4];
@@ -326,15 +329,16 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 
   uint32_t turn = 0;   // tokens that this team has begun
   for (; tok < last; tok += teams, ++turn) {
-    const int stage = turn & 1;
-    if (t == 0 && ok && last - tok > teams) fetch(tok + teams, issued++ & 1);   // all have read the last token there
+    const int stage = stage_of(turn);
+    if (STAGES == 2 && t == 0 && ok && last - tok > teams)
+      fetch(tok + teams, stage_of(issued++));   // all have read the last token there
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int pair = t + j * threads;
       if (pair < p.pairs) table[pair] = cos_sin(pos[j], axis_of(pair, p) == 0 ? p.pos0 : 0, step[j], p.factor);
     }
     positions(tok + teams);
-    ok &= mbar_wait(full + 8 * stage, (turn >> 1) & 1, wc, 52, tok);   // a token that never comes: recorded
+    ok &= mbar_wait(full + 8 * stage, parity_of(turn), wc, 52, tok);   // a token that never comes: recorded
     const uint8_t* src = rows + stage * r_bytes;
     float2 s = make_float2(0.f, 0.f);
     if constexpr (NORM == ISPA_QK_NORM_TOKEN) {
@@ -366,10 +370,11 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
       if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f);
     }
     tm.sync();   // the token's stage and the table are free
+    if (STAGES == 1 && t == 0 && ok && last - tok > teams) fetch(tok + teams, stage_of(issued++));
   }
   if (t == 0 && !ok)   // after a timeout: nothing in flight when the block leaves
-    for (uint32_t i = issued < 2 ? 0 : issued - 2; i < issued; ++i)
-      mbar_wait_drain(full + 8 * (i & 1), (i >> 1) & 1, R_DRAIN_NS);
+    for (uint32_t i = issued < STAGES ? 0 : issued - STAGES; i < issued; ++i)
+      mbar_wait_drain(full + 8 * stage_of(i), parity_of(i), R_DRAIN_NS);
 }
 
 template <bool HALF>
@@ -383,18 +388,39 @@ cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
   // warps that take all heads of a token in one step
   const int64_t steps = (static_cast<int64_t>(heads) * p.lanes_per_head + 31) / 32;
   const int norm = p.rows[0].norm;
-  // Estimates in ns, from measured runs: a block a row starts at once but takes blocks and values slowly (900 tokens of
-  // 2 x 1536 5.0 us against 6.9, of 2 x 5120 14.7 against 12.2; 9400 of 640 19.4 against 5.7).
-  const int64_t block_ns = 2000 + std::max(p.n * p.n_rows * 9 / 10, p.n * values * 12 / 10000);
+  // Estimates in ns, from measured runs of 150 to 4680 tokens: a block a row starts at once but takes blocks and values
+  // slowly (norm over the token, 900 tokens of 2 x 1536 5.0 us against 6.9, of 2 x 5120 14.7 against 12.3; per head,
+  // 450 of 24 and 8 heads 5.8 against 5.7, 1560 18.6 against 8.6; none, 310 of 2 x 5120 4.9 against 3.8).
+  const int64_t lanes = 8 * values / p.head_dim * p.lanes_per_head, work = p.n * lanes / 1000;   // idle ones too
+  const bool token_norm = norm == ISPA_QK_NORM_TOKEN, head_norm = norm == ISPA_QK_NORM_HEAD;
+  const int64_t block_ns =
+      2000 + std::max(p.n * p.n_rows * 9 / 10, work * (token_norm ? 130 : !head_norm ? 114 : HALF ? 200 : 140) / 100);
   const int64_t stream_ns =
-      (norm == ISPA_QK_NORM_TOKEN ? 4000 + std::min<int64_t>(3000, values) : 4500) + p.n * values * 56 / 100000;
+      token_norm ? std::max(5500 + std::min<int64_t>(1400, values * 45 / 100) + values * 9 / 100,
+                            4500 + work * 80 / 100)
+      : head_norm ? std::max(4800 + lanes / 4, 2000 + work * 85 / 100)
+                  : std::max(3500 + values * 9 / 100, 2600 + work * 60 / 100);
   if (stream_ns < block_ns && values <= R_SMEM / 4 && (p.n_rows == 1 || p.rows[1].norm == norm)) {
+    const int fixed = norm == ISPA_QK_NORM_TOKEN ? 4 * static_cast<int>(values) : 0;
+    const auto token_bytes = [&](int stages) {
+      return 2 * stages * static_cast<int>(values) + ((8 * p.pairs + 15) & ~15) + 16 + 2 * TEAM_WARPS * 8;
+    };
+    const auto teams_of = [&](int warps, int stages) {
+      return std::min({32 / warps, warps > 1 ? 15 : 32, (R_SMEM - fixed) / token_bytes(stages)});
+    };
     // Few warps a team where that makes more teams (4680 x 2 x 1536: one warp 15.0 us, two 17.1), more where shared
     // memory holds few tokens anyway (4680 x 2 x 5120: five warps 38.2 us, four 39.8, two 51.0).
-    const int warps = static_cast<int>(steps <= 6 ? 1 : std::min<int64_t>(TEAM_WARPS, (steps + 3) / 4));
-    const int fixed = norm == ISPA_QK_NORM_TOKEN ? 4 * static_cast<int>(values) : 0;
-    const int token = 4 * static_cast<int>(values) + R_TABLE + 16 + 2 * TEAM_WARPS * 8;
-    const int teams = std::min({32 / warps, warps > 1 ? 15 : 32, (R_SMEM - fixed) / token});
+    int warps = static_cast<int>(steps <= 6 ? 1 : std::min<int64_t>(TEAM_WARPS, (steps + 3) / 4));
+    // A team's next token on its way while it works on one, unless that leaves half of the teams (1560 tokens of 160
+    // and 40 heads of 96, per head: 36.9 us with one token each, 42.5 with two).
+    int stages = teams_of(warps, 1) >= 2 * teams_of(warps, 2) ? 1 : 2;
+    // A team for each of the SM's tokens where they all fit: none waits for another (per head, 1560 tokens of 24 and 8
+    // heads 11.3 -> 8.6 us, 4680 of 2 x 1536 15.7 -> 13.5; over the token, 2600 of 2 x 1536 13.0 -> 10.6).
+    const int64_t each = (p.n + sms - 1) / sms;
+    const int all = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({TEAM_WARPS, 32 / each, (steps + 1) / 2})));
+    const bool at_once = teams_of(all, 1) >= each;
+    if (at_once) warps = all, stages = 1;
+    const int teams = at_once ? static_cast<int>(each) : teams_of(warps, stages), token = token_bytes(stages);
     const auto go = [&](auto kernel) {
       const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
       if (e != cudaSuccess) return e;
@@ -404,14 +430,21 @@ cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
     };
     if (teams >= 1) {
       const bool full = 2 * p.pairs == p.head_dim && 8 * p.lanes_per_head == p.head_dim;
-      if (norm == ISPA_QK_NORM_TOKEN)
-        return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true>)
-                    : go(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false>);
-      if (norm == ISPA_QK_NORM_HEAD)
-        return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true>)
-                    : go(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false>);
-      return full ? go(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true>)
-                  : go(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false>);
+      const auto pick = [&](auto one, auto two) { return stages == 1 ? go(one) : go(two); };
+      if (token_norm)
+        return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 1>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 2>)
+                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 1>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 2>);
+      if (head_norm)
+        return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 1>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 2>)
+                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 1>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 2>);
+      return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 1>,
+                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 2>)
+                  : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 1>,
+                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 2>);
     }
   }
   const auto go = [&](auto kernel, int warps) {

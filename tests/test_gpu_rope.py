@@ -123,6 +123,16 @@ def test_shapes(n, heads, d, layout, norm):
     _case(n, heads, d, [d // 2], layout, norm)
 
 
+# Many tokens: a team for each of an SM's tokens (one warp, several), rounds with one token a team in shared memory and with
+# two, a last round that not all teams have, full heads and not; out of place and in place.
+@pytest.mark.parametrize("norm", NORMS)
+@pytest.mark.parametrize("n,heads,d,in_place", [(1820, (8, 8), 128, False), (1217, (24, 8), 128, True),
+                                                (1001, (96, 24), 96, True), (460, (160, 40), 96, False),
+                                                (6151, (6, 2), 64, True), (2129, (24, 24), 128, False)])
+def test_many_tokens(n, heads, d, in_place, norm):
+    _case(n, heads, d, [d // 2], LAYOUTS[n % 2], norm, in_place=in_place)
+
+
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_part_of_the_head_passes(layout):
     for d, pairs in [(128, 32), (64, 8), (96, 24), (256, 8), (128, 20), (40, 4)]:
