@@ -490,9 +490,10 @@ template <bool XF32, bool RES>
 cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
   const int nv = p.dim / 8;
   const bool modulated = p.gate || p.scale || p.shift;
-  // Many rows, by what a team keeps in shared memory.  4680 x 1536 bf16: 9.5 us against 12.7 with a block a row, 620 x
-  // 5120 (both norms) 8.4 against 12.0, 450 rows 6.1 against 6.5; below that, and with vectors of a few rows each (2:
-  // 14.5 us a block a row), there is nothing for a team to keep.
+  // Many rows, by what a team keeps in shared memory: more than two an SM, of short rows one.  4680 x 1536 bf16 9.4 us
+  // against 12.6 with a block a row, 620 x 5120 (both norms) 8.4 against 13.1, 310 x 4096 3.7 against 5.4, 310 x 1536
+  // 2.9 each, 230 x 2560 3.3 against 3.0; 160 x 512 2.2 against 2.5.  With vectors of a few rows each (2: 14.5 us a
+  // block a row) there is nothing for a team to keep.
   // Three vectors a thread in more warps where shared memory has room for their teams (5120 bf16, both norms 39.7 ->
   // 37.2 us, layer norms 48.9 -> 44.7; 5120 fp32, where it has not, 51.5 -> 55.7), else four.
   const int few = (nv + 127) / 128, team_warps = XF32 ? few : std::max(few, std::min(TEAM_WARPS, (nv + 95) / 96));
@@ -502,15 +503,17 @@ cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
   // registers, 15 named barriers, and what shared memory has room for
   int teams = std::min({s_threads(v, RES) / 32 / team_warps, team_warps > 1 ? 15 : 32,
                         (S_SMEM - fixed) / (2 * row_bytes + rest)});
-  if (p.rows > 4 * sms && p.rows < INT32_MAX - 64 && p.dim <= S_DIM && teams >= 1 &&
+  if (p.rows > (p.dim <= 512 ? 1 : 2) * sms && p.rows < INT32_MAX - 64 && p.dim <= S_DIM && teams >= 1 &&
       !(modulated && p.rows_per_group < 8)) {
-    // Two blocks an SM where both fit: one starts, or waits for its factors, while the other works.
-    const int blocks = teams >= 8 && 2 * (fixed + teams / 2 * (2 * row_bytes + rest) + 1024) <= S_SMEM ? 2 : 1;
-    teams /= blocks;
+    // Two blocks an SM where both fit and have rows enough: one starts, or waits for its factors, while the other works
+    // (gate and norm of 1536 fp32: 4680 rows 17.4 us against 17.9 with one, 1560 8.5 against 7.7).
+    const bool two = teams >= 8 && p.rows > 16 * sms &&
+                     2 * (fixed + teams / 2 * (2 * row_bytes + rest) + 1024) <= S_SMEM;
+    const int64_t rows = two ? (p.rows + 2 * sms - 1) / (2 * sms) : (p.rows + sms - 1) / sms;   // of a block
+    teams = static_cast<int>(std::min<int64_t>(two ? teams / 2 : teams, rows));
     const auto go = [&](auto kernel) {
       const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), S_SMEM);
       if (e != cudaSuccess) return e;
-      const int64_t rows = std::max<int64_t>((p.rows + blocks * sms - 1) / (blocks * sms), teams);
       return launch_pdl(kernel, dim3(static_cast<unsigned>((p.rows + rows - 1) / rows)), dim3(32 * team_warps, teams),
                         fixed + teams * (2 * row_bytes + rest), s, p, static_cast<int>(rows));
     };

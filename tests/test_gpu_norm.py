@@ -120,6 +120,14 @@ def test_gate_residual(rows, dim, fp32):
         _residual_case(rows, dim, fp32, post, pre, fmt, in_place=pre == ol.RMS)
 
 
+# One to three rows of an SM and a team, a block's last row missing; few rows and one block an SM or two (2433 and more)
+@pytest.mark.parametrize("rows,dim,fp32", [(153, 264, True), (305, 8192, True), (306, 5120, False), (457, 1536, False),
+                                           (911, 1536, True), (2431, 512, False), (2443, 1024, True)])
+def test_a_few_rows_an_sm(rows, dim, fp32):
+    _norm_case(rows, dim, fp32, ol.LAYER, "i8", affine=True, per=59)
+    _residual_case(rows, dim, fp32, ol.RMS, ol.LAYER, "bf16", in_place=True)
+
+
 def test_gate_residual_without_norms_or_vectors():
     _residual_case(20, 128, True, None, None, None, in_place=True, gate=False)
 
