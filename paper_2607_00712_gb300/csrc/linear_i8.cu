@@ -24,9 +24,8 @@
 // UMMAs take 0.19, a team 0.47 us for a block (there are three), and the ring of four stages, from one block's
 // conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave 134 us, three quarters of the UMMAs
 // 143.  On the way: one team of eight converter warps 405 us, four teams of two 218; a release at cluster scope a
-// block, a memory barrier, taken back 168; A in TMEM, so that shared memory moves a third less, 225 in pairs of 192,
-// because one lane issued TMA and UMMAs with each operand moved to a uniform register one by one; whole warps in these
-// roles 159; twelve converter warps 157; sums of two runs in fp32 155; running stage counters 150.
+// block, a memory barrier, taken back 168; A in TMEM, so that shared memory moves a third less, 225 in pairs of 192
+// with one lane in the TMA and UMMA roles; whole warps in these roles 159; twelve converter warps 157; sums of two runs in fp32 155; running stage counters 150.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -8,7 +8,7 @@
 // Angles: steps_i is the pair's turns per position as a 64-bit fraction of a turn, so pos * steps_i modulo 2^64 is the
 // position's fraction of a turn with no rounding however far the position is; its upper 32 bits (2^-32 of a turn,
 // 1.5e-9 rad) go to fp32.  The reduced angle lies in [-pi, pi), where __sinf and __cosf are off by at most 2^-21.19:
-// 2^-12 of a bf16 rounding step of the largest value, against a dozen more instructions a pair for sincosf.
+// 2^-12 of a bf16 rounding step of the largest value.
 //
 // Memory bounds it: each value crosses HBM once in and once out.
 //
