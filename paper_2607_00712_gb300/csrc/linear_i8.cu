@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(rawe0 + 8 * rs);
-        if constexpr (PAIR) mbar_arrive_cluster_own(cluster_map(f16f0 + 8 * fs, 0));
+        if (PAIR && rank == 1) mbar_arrive_cluster_smem(cluster_map(f16f0 + 8 * fs, 0));
         else mbar_arrive(f16f0 + 8 * fs);
       }
     }

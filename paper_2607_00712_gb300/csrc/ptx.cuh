@@ -127,8 +127,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   return mbar_wait_slow(bar, parity, w, site, detail);
 }
 
-// mbar_try_wait for a barrier that the other CTA of a pair arrives at too: what its threads wrote to their own
-// shared memory before they arrived is ordered before what follows.
+// mbar_try_wait for a barrier that the other CTA of a pair arrives at too (mbar_arrive_cluster: both sides at cluster
+// scope): what is ordered before that arrival is ordered before what follows.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -493,12 +493,14 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-
-// The same where what it releases is the arriving CTA's own shared memory, written through the generic proxy, fenced
-// (fence_proxy_async_smem) and read by that same SM's tensor core when the pair's UMMA runs: ordering within the
-// arriving CTA is enough, and the wider release is a memory barrier (a quarter of an int8 GEMM's time at one a block).
-__device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// The same for accesses to this CTA's shared memory alone: a fence of cluster scope that orders nothing else, and the
+// arrival behind it.  (Of TMEM, tcgen05.wait::st and tcgen05.fence::before_thread_sync in front of it and
+// tcgen05.fence::after_thread_sync behind the wait make the order; the arrival need not release anything for that.)
+__device__ __forceinline__ void mbar_arrive_cluster_smem(uint32_t bar) {
+  asm volatile(
+      "fence.release.sync_restrict::shared::cta.cluster;\n\t"
+      "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+      : "memory");
 }
 
 // ---------------------------------------------------------------- descriptors
