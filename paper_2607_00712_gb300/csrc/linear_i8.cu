@@ -19,13 +19,14 @@
 // accumulators back, two sets in TMEM in turn.  Their int32 sums take up to 96 registers a thread, so the warpgroups
 // share the registers out anew (setmaxnreg).  Every wait is bounded.
 //
-// 4680 x 5120 -> 5120 149.8 us, 1638 TFLOP/s, with operands and result in L2, 160 from and to HBM; 4680 x 1536 -> 4608
-// 46.4 us; 61 x 5120 -> 640 9.0 us; one token of 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit: a block of 192 columns takes 0.25 us where its
-// UMMAs take 0.19, a team 0.47 us for a block (there are three), and the ring of four stages, from one block's
-// conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave 134 us, three quarters of the UMMAs
-// 143.  On the way: one team of eight converter warps 405 us, four teams of two 218; a release at cluster scope a
-// block, a memory barrier, taken back 168; A in TMEM, so that shared memory moves a third less, 225 in pairs of 192
-// with one lane in the TMA and UMMA roles; whole warps in these roles 159; twelve converter warps 157; sums of two runs in fp32 155; running stage counters 150.
+// 4680 x 5120 -> 5120 150.8 us, 1627 TFLOP/s, with operands and result in L2, 162 from and to HBM; 4680 x 1536 -> 4608
+// 47.0 us; 61 x 5120 -> 640 9.1 us; one token of 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit:
+// a block of 192 columns takes 0.25 us where its UMMAs take 0.19, a team 0.47 us for a block (there are three), and the
+// ring of four stages, from one block's conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave
+// 134 us, three quarters of the UMMAs 143.  On the way: one team of eight converter warps 405 us, four teams of two 218;
+// the hand-over without an unrestricted release of cluster scope a block 168; A in TMEM, so that shared memory moves a
+// third less, 225 in pairs of 192 with one lane in the TMA and UMMA roles; whole warps in these roles 159; twelve
+// converter warps 157; sums of two runs in fp32 155; running stage counters 150.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -381,6 +382,9 @@ __global__ void __launch_bounds__(I_THREADS, 1)
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(rawe0 + 8 * rs);
+        // The issuer stands in the other CTA: B's half needs a release of cluster scope, A's in TMEM the fence above.
+        // Restricted to shared memory it costs 1 % (149.8 -> 150.8 us at 4680 x 5120 -> 5120), an unrestricted one a
+        // quarter, and one warp that sends them all on waits 0.5 us for each (360 us).
         if (PAIR && rank == 1) mbar_arrive_cluster_smem(cluster_map(f16f0 + 8 * fs, 0));
         else mbar_arrive(f16f0 + 8 * fs);
       }

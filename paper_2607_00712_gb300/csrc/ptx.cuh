@@ -127,8 +127,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   return mbar_wait_slow(bar, parity, w, site, detail);
 }
 
-// mbar_try_wait for a barrier that the other CTA of a pair arrives at too (mbar_arrive_cluster: both sides at cluster
-// scope): what is ordered before that arrival is ordered before what follows.
+// mbar_try_wait for a barrier that the other CTA of a pair arrives at too: what is ordered before an arrival that
+// releases at cluster scope (mbar_arrive_cluster, mbar_arrive_cluster_smem) is ordered before what follows.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
