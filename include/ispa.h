@@ -649,8 +649,9 @@ ISPA_API ispa_status ispa_attn_dual_kv8(const ispa_kv_ring* ring, const float* k
  * ("fn": largest magnitude 448, no infinities) with one fp32 scale per token
  * for activations and one per output channel for weights:
  *   amax = max |x| over the group; inv = 448 / amax and scale = amax / 448 in
- *   fp32 (both 1 for an all-zero group); code = e4m3(x * inv), rounded to
- *   nearest even and saturated at +-448.
+ *   fp32 (both 1, and the codes zeros, for a group with amax <= 7 * 2^-122, whose
+ *   quotient fp32 does not hold); code = e4m3(x * inv), rounded to nearest even and
+ *   saturated at +-448.
  */
 
 /* Activations x: bf16 [rows][cols] -> codes q: uint8 [rows][cols], scale: fp32
@@ -752,10 +753,11 @@ typedef struct {
 
 /* Where normed rows go: bf16, or 8-bit codes with one fp32 scale per row (value ~ code * scale):
  *   amax = max |h| of the row (fp32, before any rounding to bf16);
- *   E4M3: scale = amax / 448, code = e4m3(h * (448 / amax)), as ispa_quantize_rows_e4m3 does;
+ *   E4M3: scale = amax / 448, code = e4m3(h * (448 / amax));
  *   I8:   scale = amax / 127, code = round(h * (127 / amax)) to nearest even, in [-127, 127];
- *   a row with amax < 2^-117 has scale 1 and zero codes.  A row with an infinity or a NaN has an infinite or NaN scale (its
- *   codes say nothing), so that what is computed from it is no finite number. */
+ *   a row with amax < 2^-117 has scale 1 and zero codes (ispa_quantize_rows_e4m3 still codes such rows, down to
+ *   7 * 2^-122).  A row with an infinity or a NaN has an infinite or NaN scale (its codes say nothing), so that what
+ *   is computed from it is no finite number. */
 #define ISPA_ROWS_BF16 0
 #define ISPA_ROWS_E4M3 1
 #define ISPA_ROWS_I8 2

@@ -16,7 +16,7 @@ Encoding rounds to nearest, ties to the even code, keeps the sign of zero, and s
 magnitudes above 448 to 448 (NaN stays NaN).
 
 Quantisation, in fp32 as both sides compute it:
-  amax = max |x| over the group; if amax == 0: inv = 1, scale = 1;
+  amax = max |x| over the group; if amax <= 7 * 2^-122 (0 too; 448 / amax >= 2^128): inv = 1, scale = 1;
   else inv = fl32(448 / amax), scale = fl32(amax / 448); code = e4m3(fl32(x * inv)).
 Linear: y[t, n] = a_scale[t] * w_scale[n] * sum_k dec(a_q[t, k]) * dec(w_q[n, k]), in float64
 (the weight codes are stored K-major, [D_out][D]).
@@ -32,6 +32,7 @@ from __future__ import annotations
 import numpy as np
 
 E4M3_MAX = 448.0
+SMALL_GROUP = np.float32(7 * 2.0 ** -122)     # largest amax whose fl32(448 / amax) is infinite
 
 
 def _value_of_code(c: int) -> float:
@@ -80,7 +81,7 @@ def quantize_groups(x: np.ndarray, axis: int):
     """Per-group e4m3 quantisation along `axis` (the reduced axis): returns (codes, scale fp32)."""
     x = np.asarray(x, dtype=np.float32)
     amax = np.max(np.abs(x), axis=axis, keepdims=True).astype(np.float32)
-    zero = amax == 0
+    zero = amax <= SMALL_GROUP
     safe = np.where(zero, np.float32(1), amax)
     inv = np.where(zero, np.float32(1), np.float32(E4M3_MAX) / safe).astype(np.float32)
     scale = np.where(zero, np.float32(1), safe / np.float32(E4M3_MAX)).astype(np.float32)

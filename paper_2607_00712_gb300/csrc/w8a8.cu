@@ -9,8 +9,8 @@
 //   w8a8_gemm_kernel     out[t][n] = bf16(a_scale[t] * w_scale[n] * sum_k a[t][k] w[n][k])
 //
 // Quantisation arithmetic (fp32, rounded to nearest at every step, identical to the
-// oracle's): amax = max |x|; inv = 448 / amax, scale = amax / 448 (both 1 for an all-zero
-// group); code = e4m3(x * inv), round to nearest even with saturation at +-448.  The same kernels
+// oracle's): amax = max |x|; inv = 448 / amax, scale = amax / 448 (both 1 for a group whose
+// quotient fp32 does not hold, amax <= 7 * 2^-122, zeros among them); code = e4m3(x * inv), round to nearest even with saturation at +-448.  The same kernels
 // make the int8 codes of linear_i8.cu (127 in 448's place, rounded to the nearest even integer).
 //
 // GEMM: persistent, one CTA per SM looping over 128 x BN output tiles (BN = 256, 192 or 128), or one pair of
@@ -67,12 +67,12 @@ __device__ __forceinline__ uint32_t code4(const float* f) {
 template <bool I8>
 __device__ __forceinline__ float factor_of(float amax) {
   if constexpr (I8) return code_factor(amax, kCodeMax<I8>);
-  else return amax == 0.f ? 1.f : __fdiv_rn(kCodeMax<I8>, amax);
+  else return amax <= kTinyE4M3Group ? 1.f : __fdiv_rn(kCodeMax<I8>, amax);
 }
 template <bool I8>
 __device__ __forceinline__ float scale_of(float amax) {
   if constexpr (I8) return code_scale(amax, kCodeMax<I8>);
-  else return amax == 0.f ? 1.f : __fdiv_rn(amax, kCodeMax<I8>);
+  else return amax <= kTinyE4M3Group ? 1.f : __fdiv_rn(amax, kCodeMax<I8>);
 }
 
 // One warp per row (grid-stride over rows); cols % 8 == 0.  Rows of up to 32 * CACHE

@@ -155,3 +155,12 @@ def test_query_blocks_are_per_head_quantisation_of_each_block():
         assert np.array_equal(q[b * 128:(b + 1) * 128], qb) and np.array_equal(s[:, b], sb)
     back = qt.dequantize_query_blocks(q, s)
     assert np.all(np.abs(back - x) <= 2.0 ** -4 * np.abs(x) * (1 + 1e-6) + 2.0 ** -10 * s.max())
+
+
+def test_groups_whose_quotient_is_infinite_count_as_zeros():
+    edge = np.float32(7 * 2.0 ** -122)
+    above = np.nextafter(edge, np.float32(1))
+    x = np.array([[edge, 0, -edge / 2], [above, 0, -above], [0, 0, 0]], np.float32)
+    q, s = qt.quantize_rows(x)
+    assert s[0] == 1 and s[2] == 1 and s[1] == np.float32(above / np.float32(448))
+    assert not qt.decode(q[[0, 2]]).any() and qt.decode(q[1]).tolist() == [448, 0, -448]
