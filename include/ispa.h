@@ -532,8 +532,9 @@ ISPA_API ispa_status ispa_ls_solve(const ispa_ls_state* state, const float* W, i
  */
 
 /* x: bf16 [n][H][d] -> codes q: uint8 [n][H][d] and scale: fp32 [H] (written),
- * scale_h = max |x_h| / 448 (1 for an all-zero head), code = e4m3(x * (1 / scale_h))
- * (each step in fp32, rounded to nearest even), saturating.  d % 16 == 0, H <= 256. */
+ * scale_h = max |x_h| / 448 (1, and the codes zeros, for a head up to 7 * 2^-122, whose
+ * 1 / scale fp32 does not hold), code = e4m3(x * (1 / scale_h)) (each step in fp32, rounded
+ * to nearest even), saturating.  d % 16 == 0, H <= 256. */
 ISPA_API ispa_status ispa_quantize_heads_e4m3(const void* x, int64_t n, int32_t H, int32_t d, uint8_t* q,
                                               float* scale, ispa_stream stream);
 
@@ -545,8 +546,9 @@ ISPA_API ispa_status ispa_quantize_q_e4m3(const void* x, int64_t n, int32_t H, i
                                           float* scale, ispa_stream stream);
 
 /* Codes with given per-head scales: x bf16 [n][H][d], scale fp32 [H] (device)
- * -> q [n][H][d], code = e4m3(x * (1 / scale_h)).  For the chunk's keys, with
- * the ring's key scales.  d % 16 == 0. */
+ * -> q [n][H][d], code = e4m3(x * (1 / scale_h)); scale_h finite and above 2^-128 (here
+ * and wherever scales are given).  For the chunk's keys, with the ring's key scales.
+ * d % 16 == 0. */
 ISPA_API ispa_status ispa_quantize_k_e4m3(const void* x, int64_t n, int32_t H, int32_t d, const float* scale,
                                           uint8_t* q, ispa_stream stream);
 

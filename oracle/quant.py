@@ -120,10 +120,10 @@ def quantize_heads_with_scale(x, scale) -> np.ndarray:
 
 
 def head_scales(x) -> np.ndarray:
-    """Per-head scale fl32(amax / 448) of token-major [n][H][d] values (1 for an all-zero head)."""
+    """Per-head scale fl32(amax / 448) of token-major [n][H][d] values (1 for a head up to SMALL_GROUP)."""
     x = np.asarray(x, dtype=np.float32)
     amax = np.max(np.abs(x), axis=(0, 2)).astype(np.float32)
-    return np.where(amax == 0, np.float32(1), amax / np.float32(E4M3_MAX)).astype(np.float32)
+    return np.where(amax <= SMALL_GROUP, np.float32(1), amax / np.float32(E4M3_MAX)).astype(np.float32)
 
 
 def quantize_heads(x):
@@ -139,7 +139,7 @@ def dequantize_heads(q, scale) -> np.ndarray:
 
 def quantize_query_blocks(x, block: int = 128):
     """Queries [n][H][d] -> (codes, scales [H][ceil(n / block)]): one scale per head and block of
-    `block` consecutive tokens, scale = fl32(amax / 448) (1 for an all-zero block)."""
+    `block` consecutive tokens, scale = fl32(amax / 448) (1 for a block up to SMALL_GROUP)."""
     x = np.asarray(x, dtype=np.float32)
     n, H, _ = x.shape
     nb = (n + block - 1) // block

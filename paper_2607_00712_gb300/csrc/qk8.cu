@@ -3,11 +3,11 @@
 // scale per head.
 //
 //   head_amax_kernel + quant_heads_kernel + head_scale_kernel
-//       x bf16 [n][H][d] -> codes [n][H][d], scale[h] = amax_h / 448 (1 for an all-zero head),
-//       code = e4m3(x * (1 / scale_h)); the three launches run in stream order, the scale
-//       array holding amax (as fp32 bits, reduced with integer atomicMax: non-negative fp32
-//       values order like their bit patterns; per block in shared memory first) until the
-//       last one converts it.
+//       x bf16 [n][H][d] -> codes [n][H][d], scale[h] = amax_h / 448 (1 for a head of zeros or up
+//       to 7 * 2^-122, whose 1 / scale fp32 does not hold), code = e4m3(x * (1 / scale_h)); the
+//       three launches run in stream order, the scale array holding amax (as fp32 bits, reduced
+//       with integer atomicMax: non-negative fp32 values order like their bit patterns; per block
+//       in shared memory first) until the last one converts it.
 //   quant_q_blocks_kernel
 //       queries: one scale per head and block of 128 tokens (one attention CTA), one pass.
 //   quant_given_kernel
@@ -30,6 +30,7 @@
 #include "internal.h"
 #include "pdl.cuh"
 #include "ptx.cuh"
+#include "rows.cuh"
 
 namespace ispa {
 
@@ -58,7 +59,10 @@ __device__ __forceinline__ uint2 quant8(const uint4 v, float inv) {
   return make_uint2(out[0], out[1]);
 }
 
-__device__ __forceinline__ float scale_of_amax(float amax) { return amax == 0.f ? 1.f : __fdiv_rn(amax, kE4M3Max); }
+// 1 where 1 / scale would be infinite: the group counts as zeros.
+__device__ __forceinline__ float scale_of_amax(float amax) {
+  return amax <= kTinyE4M3Group ? 1.f : __fdiv_rn(amax, kE4M3Max);
+}
 __device__ __forceinline__ float inv_of_scale(float s) { return __fdiv_rn(1.f, s); }
 
 // One warp per (token, head) row of d bf16 (d % 8 == 0); amax_bits[h] must start at 0.

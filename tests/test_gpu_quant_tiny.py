@@ -76,3 +76,25 @@ def test_a_product_with_small_rows_and_channels_is_finite():
     torch.cuda.synchronize()
     y = y.float()
     assert torch.isfinite(y).all() and not y[3].any() and not y[:, 6].any()
+
+
+# heads of keys and blocks of queries, whose codes go by 1 / scale
+def test_heads_and_query_blocks():
+    H, d, n = len(TOP), 128, 130
+    g = np.random.default_rng(5)
+    x = synth.bf16_round(((2 * g.random((n, H, d)) - 1) * 0.99 * TOP[None, :, None]).astype(np.float32))
+    x[0, :, 5], x[1, :, 7], x[129, :, 5], x[128, :, 7] = TOP, -TOP, TOP, -TOP
+    x[:, :, 9] = 0
+    xt = torch.from_numpy(x).cuda().to(torch.bfloat16)
+    q, s = torch.empty(n, H, d, dtype=torch.uint8, device="cuda"), torch.empty(H, device="cuda")
+    abi.ispa_quantize_heads_e4m3(xt, n, H, d, q, s)
+    qb, sb = torch.empty(n, H, d, dtype=torch.uint8, device="cuda"), torch.empty(H, 2, device="cuda")
+    abi.ispa_quantize_q_e4m3(xt, n, H, d, qb, sb)
+    codes, scale = qt.quantize_heads(x)
+    assert (scale[SMALL] == 1).all() and (scale[~SMALL] < 2.0 ** -120).all()
+    assert np.array_equal(s.cpu().numpy(), scale) and np.array_equal(q.cpu().numpy(), codes)
+    codes, scale = qt.quantize_query_blocks(x)
+    assert np.array_equal(sb.cpu().numpy(), scale) and np.array_equal(qb.cpu().numpy(), codes)
+    for c in (q, qb):
+        value = qt.decode(c.cpu().numpy())
+        assert not value[:, SMALL].any() and (value[0, ~SMALL, 5] == 448).all() and (value[1, ~SMALL, 7] == -448).all()
