@@ -35,6 +35,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "forms.h"
 #include "internal.h"
 #include "pdl.cuh"
 #include "ptx.cuh"
@@ -91,8 +92,6 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------ many tokens
-constexpr int IM = 128;                 // rows (tokens) of a CTA's part of a tile
-constexpr int IK = 64;                  // codes of a block: 64 bytes raw, 128 bytes (one swizzle row) as fp16
 constexpr int I_EXACT = 1024 / IK;      // blocks whose sums the fp32 accumulator holds exactly
 constexpr int I_CONV = 12, I_EPI = 8;   // converter and read-back warps
 constexpr int I_TEAMS = I_CONV / 4;     // four converter warps, one per TMEM lane quarter, share a block
@@ -596,50 +595,6 @@ cudaError_t launch_gemm(int split, const int8_t* a_q, const float* a_scale, cons
                             tw, to, p);
 }
 
-struct GemmChoice {
-  int bn;
-  bool pair;
-  int split;
-};
-
-// The form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in L2) of 9 to
-// 9400 tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's fixed part)
-// + launch, fill and the last tile's way out.  A block of a pair of 192 columns costs little more than one of 128, so
-// those win where tiles fill whole waves (4680 x 1536 -> 1536: 19.7 against 22.4 us with pairs of 128 and 23.6 with
-// single CTAs); single CTAs win where there are few tiles (1000 x 1536 -> 1536: 10.0 against 10.9 and 10.3).
-GemmChoice choose_gemm(int64_t T, int32_t D, int32_t Dout, int sms, int64_t* ns) {
-  struct Shape {
-    int bn, ctas, block_ns, tile_ns, start_ns;
-  };
-  static constexpr Shape kShapes[3] = {{192, 2, 250, 500, 4600}, {128, 2, 230, 300, 3750}, {128, 1, 265, 300, 3100}};
-  const int64_t n_kb = (D + IK - 1) / IK;
-  GemmChoice best{128, false, 1};
-  *ns = INT64_MAX;
-  for (const Shape& f : kShapes) {
-    if (sms < f.ctas) continue;
-    const int64_t rows = IM * f.ctas, units = sms / f.ctas;
-    const int64_t tiles = (T + rows - 1) / rows * ((Dout + f.bn - 1) / f.bn);
-    const int64_t cost = (tiles + units - 1) / units * (n_kb * f.block_ns + f.tile_ns) + f.start_ns;
-    if (cost < *ns) {
-      *ns = cost;
-      best = {f.bn, f.ctas == 2, 1};
-    }
-  }
-  // Few tiles and a long contraction: clusters share a tile's blocks and add up through distributed shared memory.
-  // 61 x 5120 -> 640: 24.2 us in pairs of 192, 18.2 / 11.9 / 9.2 with 2 / 4 / 8 CTAs a tile.  As many clusters as run
-  // at once: of four or eight CTAs that is taken as four fifths of the chip.
-  for (const int c : {2, 4, 8}) {
-    const int64_t tiles = (T + IM - 1) / IM * ((Dout + 127) / 128);
-    if (n_kb < c || tiles * c * (c > 2 ? 5 : 4) > 4 * static_cast<int64_t>(sms)) break;
-    const int64_t cost = 5100 + (n_kb + c - 1) / c * 265 + 250 * c + 40 * std::min<int64_t>(T, IM) / c;
-    if (cost < *ns) {
-      *ns = cost;
-      best = {128, false, c};
-    }
-  }
-  return best;
-}
-
 }  // namespace
 
 cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8_t* w_q, const float* w_scale,
@@ -649,26 +604,22 @@ cudaError_t launch_linear_i8(const int8_t* a_q, const float* a_scale, const int8
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  int64_t gemm_ns = 0;
-  const GemmChoice g = choose_gemm(T, D, Dout, sms, &gemm_ns);
-  // Few tokens: the warps' loads and dp4a against the tensor cores' long start.  16 x 1536 -> 1536: 4.5 against 7.7 us;
-  // 16 x 5120 -> 5120: 20.8 against 16.4.
-  if (T <= 32 && 2000 + 55 * (static_cast<int64_t>(T) * D * Dout / 1000000) + D / 2 < gemm_ns) {
-    const auto go = [&](auto kernel, int tt, int nc) {
-      return launch_pdl(kernel, dim3((Dout + 8 * nc - 1) / (8 * nc), (T + tt - 1) / tt), dim3(256), 0, s, a_q, a_scale,
-                        w_q, w_scale, bias, static_cast<int>(T), static_cast<int>(D), static_cast<int>(Dout), o);
+  const LinearForm g = linear_i8_form(T, D, Dout, sms);
+  if (g.tokens) {
+    const auto go = [&](auto kernel) {
+      return launch_pdl(kernel, dim3((Dout + 8 * g.channels - 1) / (8 * g.channels), (T + g.tokens - 1) / g.tokens),
+                        dim3(256), 0, s, a_q, a_scale, w_q, w_scale, bias, static_cast<int>(T), static_cast<int>(D),
+                        static_cast<int>(Dout), o);
     };
-    // Two channels a warp share the tokens' loads, one makes twice the warps: 2 x 1536 -> 1536 2.1 us with one, 2.6
-    // with two; 2 x 5120 -> 5120 7.7 with one, 5.4 with two; 16 x 1536 -> 1536, two groups of tokens, 5.5 and 4.5.
-    if (Dout <= 16 * sms && T <= 8)
-      return T == 1   ? go(gemv_i8_kernel<1, 1>, 1, 1)
-             : T == 2 ? go(gemv_i8_kernel<2, 1>, 2, 1)
-             : T <= 4 ? go(gemv_i8_kernel<4, 1>, 4, 1)
-                      : go(gemv_i8_kernel<8, 1>, 8, 1);
-    return T == 1   ? go(gemv_i8_kernel<1, 2>, 1, 2)
-           : T == 2 ? go(gemv_i8_kernel<2, 2>, 2, 2)
-           : T <= 4 ? go(gemv_i8_kernel<4, 2>, 4, 2)
-                    : go(gemv_i8_kernel<8, 2>, 8, 2);
+    if (g.channels == 1)
+      return g.tokens == 1   ? go(gemv_i8_kernel<1, 1>)
+             : g.tokens == 2 ? go(gemv_i8_kernel<2, 1>)
+             : g.tokens == 4 ? go(gemv_i8_kernel<4, 1>)
+                             : go(gemv_i8_kernel<8, 1>);
+    return g.tokens == 1   ? go(gemv_i8_kernel<1, 2>)
+           : g.tokens == 2 ? go(gemv_i8_kernel<2, 2>)
+           : g.tokens == 4 ? go(gemv_i8_kernel<4, 2>)
+                           : go(gemv_i8_kernel<8, 2>);
   }
   if (g.split > 1)
     return launch_gemm<128, false, true>(g.split, a_q, a_scale, w_q, w_scale, bias, T, D, Dout, o, status,

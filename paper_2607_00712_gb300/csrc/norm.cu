@@ -30,6 +30,7 @@
 
 #include <algorithm>
 
+#include "forms.h"
 #include "internal.h"
 #include "pdl.cuh"
 #include "rows.cuh"
@@ -203,11 +204,6 @@ __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormP
 }
 
 // ------------------------------------------------------------ many rows
-constexpr int S_DIM = 8192;             // four factors a column of such rows: 128 KB
-static_assert(S_DIM <= 1024 * TEAM_WARPS, "four vectors of eight values a thread");
-constexpr int S_SMEM = 224 * 1024;
-// Threads a block: what the registers a thread needs leave room for (64, 80 or 96).
-__host__ __device__ constexpr int s_threads(int v, bool res) { return !res ? 1024 : v == 4 ? 640 : 768; }
 constexpr uint64_t S_DRAIN_NS = 200ull * 1000 * 1000;
 
 // Vector c of a row: two runs of four values.  With an fp32 stream they are half a row apart, so that a warp reads and
@@ -488,48 +484,27 @@ __global__ void __launch_bounds__(s_threads(V, RES), 1)
 
 template <bool XF32, bool RES>
 cudaError_t launch_typed(const NormParams& p, int sms, cudaStream_t s) {
-  const int nv = p.dim / 8;
-  const bool modulated = p.gate || p.scale || p.shift;
-  // Many rows, by what a team keeps in shared memory: more than two an SM, of short rows one.  4680 x 1536 bf16 9.4 us
-  // against 12.6 with a block a row, 620 x 5120 (both norms) 8.4 against 13.1, 310 x 4096 3.7 against 5.4, 310 x 1536
-  // 2.9 each, 230 x 2560 3.3 against 3.0; 160 x 512 2.2 against 2.5.  With vectors of a few rows each (2: 14.5 us a
-  // block a row) there is nothing for a team to keep.
-  // Three vectors a thread in more warps where shared memory has room for their teams (5120 bf16, both norms 39.7 ->
-  // 37.2 us, layer norms 48.9 -> 44.7; 5120 fp32, where it has not, 51.5 -> 55.7), else four.
-  const int few = (nv + 127) / 128, team_warps = XF32 ? few : std::max(few, std::min(TEAM_WARPS, (nv + 95) / 96));
-  const int v = (nv + 32 * team_warps - 1) / (32 * team_warps);
-  const int fixed = 32 * (!RES ? 2 : p.post.bias ? 4 : 3) * nv;
-  const int row_bytes = p.dim * ((XF32 ? 4 : 2) + (RES ? 2 : 0)), rest = 2 * 8 + 2 * TEAM_WARPS * 8;
-  // registers, 15 named barriers, and what shared memory has room for
-  int teams = std::min({s_threads(v, RES) / 32 / team_warps, team_warps > 1 ? 15 : 32,
-                        (S_SMEM - fixed) / (2 * row_bytes + rest)});
-  if (p.rows > (p.dim <= 512 ? 1 : 2) * sms && p.rows < INT32_MAX - 64 && p.dim <= S_DIM && teams >= 1 &&
-      !(modulated && p.rows_per_group < 8)) {
-    // Two blocks an SM where both fit and have rows enough: one starts, or waits for its factors, while the other works
-    // (gate and norm of 1536 fp32: 4680 rows 17.4 us against 17.9 with one, 1560 8.5 against 7.7).
-    const bool two = teams >= 8 && p.rows > 16 * sms &&
-                     2 * (fixed + teams / 2 * (2 * row_bytes + rest) + 1024) <= S_SMEM;
-    const int64_t rows = two ? (p.rows + 2 * sms - 1) / (2 * sms) : (p.rows + sms - 1) / sms;   // of a block
-    teams = static_cast<int>(std::min<int64_t>(two ? teams / 2 : teams, rows));
+  const NormForm f = norm_form(p.rows, p.dim, XF32, RES, p.post.bias != nullptr, p.gate || p.scale || p.shift,
+                               p.rows_per_group, sms);
+  if (f.stream) {
     const auto go = [&](auto kernel) {
       const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), S_SMEM);
       if (e != cudaSuccess) return e;
-      return launch_pdl(kernel, dim3(static_cast<unsigned>((p.rows + rows - 1) / rows)), dim3(32 * team_warps, teams),
-                        fixed + teams * (2 * row_bytes + rest), s, p, static_cast<int>(rows));
+      return launch_pdl(kernel, dim3(static_cast<unsigned>((p.rows + f.rows - 1) / f.rows)),
+                        dim3(32 * f.warps, f.teams), f.smem, s, p, static_cast<int>(f.rows));
     };
-    return v == 1   ? go(stream_kernel<1, XF32, RES>)
-           : v == 2 ? go(stream_kernel<2, XF32, RES>)
-           : v == 3 ? go(stream_kernel<3, XF32, RES>)
-                    : go(stream_kernel<4, XF32, RES>);
+    return f.vectors == 1   ? go(stream_kernel<1, XF32, RES>)
+           : f.vectors == 2 ? go(stream_kernel<2, XF32, RES>)
+           : f.vectors == 3 ? go(stream_kernel<3, XF32, RES>)
+                            : go(stream_kernel<4, XF32, RES>);
   }
-  const int warps = (nv + 31) / 32;
-  const auto go = [&](auto kernel, int w) {
-    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.rows)), dim3(32 * w), 0, s, p);
+  const auto go = [&](auto kernel) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.rows)), dim3(32 * f.warps), 0, s, p);
   };
-  if (warps <= 16) return go(norm_kernel<1, XF32, RES>, warps);
-  if (warps <= 32) return go(norm_kernel<2, XF32, RES>, (warps + 1) / 2);
-  if (warps <= 64) return go(norm_kernel<4, XF32, RES>, (warps + 3) / 4);
-  return go(norm_kernel<8, XF32, RES>, (warps + 7) / 8);
+  return f.vectors == 1   ? go(norm_kernel<1, XF32, RES>)
+         : f.vectors == 2 ? go(norm_kernel<2, XF32, RES>)
+         : f.vectors == 4 ? go(norm_kernel<4, XF32, RES>)
+                          : go(norm_kernel<8, XF32, RES>);
 }
 
 }  // namespace

@@ -29,6 +29,7 @@
 
 #include <algorithm>
 
+#include "forms.h"
 #include "internal.h"
 #include "pdl.cuh"
 #include "rows.cuh"
@@ -176,7 +177,6 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeP
 }
 
 // ------------------------------------------------------------ many tokens
-constexpr int R_SMEM = 224 * 1024;
 constexpr uint64_t R_DRAIN_NS = 200ull * 1000 * 1000;
 
 // Block (32 * warps of a team, teams), one an SM; block b takes tokens [b, b + 1) * per_block, its teams in turn.  A
@@ -379,80 +379,35 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 
 template <bool HALF>
 cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
-  int heads = 0;
-  int64_t values = 0;   // of a token's queries and keys
-  for (int i = 0; i < p.n_rows; ++i) {
-    heads = std::max(heads, p.rows[i].heads);
-    values += static_cast<int64_t>(p.rows[i].heads) * p.head_dim;
-  }
-  // warps that take all heads of a token in one step
-  const int64_t steps = (static_cast<int64_t>(heads) * p.lanes_per_head + 31) / 32;
-  const int norm = p.rows[0].norm;
-  // Estimates in ns, from measured runs of 150 to 4680 tokens: a block a row starts at once but takes blocks and values
-  // slowly (norm over the token, 900 tokens of 2 x 1536 5.0 us against 6.9, of 2 x 5120 14.7 against 12.3; per head,
-  // 450 of 24 and 8 heads 5.8 against 5.7, 1560 18.6 against 8.6; none, 310 of 2 x 5120 4.9 against 3.8).
-  const int64_t lanes = 8 * values / p.head_dim * p.lanes_per_head, work = p.n * lanes / 1000;   // idle ones too
-  const bool token_norm = norm == ISPA_QK_NORM_TOKEN, head_norm = norm == ISPA_QK_NORM_HEAD;
-  const int64_t block_ns =
-      2000 + std::max(p.n * p.n_rows * 9 / 10, work * (token_norm ? 130 : !head_norm ? 114 : HALF ? 200 : 140) / 100);
-  const int64_t stream_ns =
-      token_norm ? std::max(5500 + std::min<int64_t>(1400, values * 45 / 100) + values * 9 / 100,
-                            4500 + work * 80 / 100)
-      : head_norm ? std::max(4800 + lanes / 4, 2000 + work * 85 / 100)
-                  : std::max(3500 + values * 9 / 100, 2600 + work * 60 / 100);
-  if (stream_ns < block_ns && values <= R_SMEM / 4 && (p.n_rows == 1 || p.rows[1].norm == norm)) {
-    const int fixed = norm == ISPA_QK_NORM_TOKEN ? 4 * static_cast<int>(values) : 0;
-    const auto token_bytes = [&](int stages) {
-      return 2 * stages * static_cast<int>(values) + ((8 * p.pairs + 15) & ~15) + 16 + 2 * TEAM_WARPS * 8;
-    };
-    const auto teams_of = [&](int warps, int stages) {
-      return std::min({32 / warps, warps > 1 ? 15 : 32, (R_SMEM - fixed) / token_bytes(stages)});
-    };
-    // Few warps a team where that makes more teams (4680 x 2 x 1536: one warp 15.0 us, two 17.1), more where shared
-    // memory holds few tokens anyway (4680 x 2 x 5120: five warps 38.2 us, four 39.8, two 51.0).
-    int warps = static_cast<int>(steps <= 6 ? 1 : std::min<int64_t>(TEAM_WARPS, (steps + 3) / 4));
-    // A team's next token on its way while it works on one, unless that leaves half of the teams (1560 tokens of 160
-    // and 40 heads of 96, per head: 36.9 us with one token each, 42.5 with two).
-    int stages = teams_of(warps, 1) >= 2 * teams_of(warps, 2) ? 1 : 2;
-    // A team for each of the SM's tokens where they all fit: none waits for another (per head, 1560 tokens of 24 and 8
-    // heads 11.3 -> 8.6 us, 4680 of 2 x 1536 15.7 -> 13.5; over the token, 2600 of 2 x 1536 13.0 -> 10.6).
-    const int64_t each = (p.n + sms - 1) / sms;
-    const int all = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({TEAM_WARPS, 32 / each, (steps + 1) / 2})));
-    const bool at_once = teams_of(all, 1) >= each;
-    if (at_once) warps = all, stages = 1;
-    const int teams = at_once ? static_cast<int>(each) : teams_of(warps, stages), token = token_bytes(stages);
+  const int32_t heads[2] = {p.rows[0].heads, p.rows[1].heads}, norms[2] = {p.rows[0].norm, p.rows[1].norm};
+  const RopeForm f = rope_form(p.n, p.n_rows, heads, norms, p.head_dim, p.pairs, p.lanes_per_head, HALF, sms);
+  if (f.stream) {
     const auto go = [&](auto kernel) {
       const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
       if (e != cudaSuccess) return e;
-      const int64_t per = std::max<int64_t>((p.n + sms - 1) / sms, teams);
-      return launch_pdl(kernel, dim3(static_cast<unsigned>((p.n + per - 1) / per)), dim3(32 * warps, teams),
-                        fixed + teams * token, s, p, static_cast<int>(per));
+      return launch_pdl(kernel, dim3(static_cast<unsigned>((p.n + f.tokens - 1) / f.tokens)),
+                        dim3(32 * f.warps, f.teams), f.smem, s, p, static_cast<int>(f.tokens));
     };
-    if (teams >= 1) {
-      const bool full = 2 * p.pairs == p.head_dim && 8 * p.lanes_per_head == p.head_dim;
-      const auto pick = [&](auto one, auto two) { return stages == 1 ? go(one) : go(two); };
-      if (token_norm)
-        return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 1>,
+    const auto pick = [&](auto one, auto two) { return f.stages == 1 ? go(one) : go(two); };
+    if (norms[0] == ISPA_QK_NORM_TOKEN)
+      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 1>,
                            rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 2>)
                     : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 1>,
                            rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 2>);
-      if (head_norm)
-        return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 1>,
+    if (norms[0] == ISPA_QK_NORM_HEAD)
+      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 1>,
                            rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 2>)
                     : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 1>,
                            rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 2>);
-      return full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 1>,
+    return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 1>,
                          rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 2>)
                   : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 1>,
                          rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 2>);
-    }
   }
-  const auto go = [&](auto kernel, int warps) {
-    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), p.n_rows), dim3(32 * warps), 0, s, p);
+  const auto go = [&](auto kernel) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), p.n_rows), dim3(32 * f.warps), 0, s, p);
   };
-  if (steps <= 16) return go(rope_kernel<1, HALF>, static_cast<int>(steps));
-  if (steps <= 32) return go(rope_kernel<2, HALF>, static_cast<int>((steps + 1) / 2));
-  return go(rope_kernel<4, HALF>, steps <= 64 ? static_cast<int>((steps + 3) / 4) : 16);
+  return f.vectors == 1 ? go(rope_kernel<1, HALF>) : f.vectors == 2 ? go(rope_kernel<2, HALF>) : go(rope_kernel<4, HALF>);
 }
 
 }  // namespace

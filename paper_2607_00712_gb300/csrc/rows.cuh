@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "forms.h"
 #include "ptx.cuh"
 
 namespace ispa {
@@ -106,8 +107,6 @@ __device__ __forceinline__ float block_reduce(float v, int warps, float (*red)[3
   for (int i = 1; i < warps; ++i) v = Op::of(v, red[slot][i]);
   return v;
 }
-
-constexpr int TEAM_WARPS = 8;   // at most
 
 // A team of `warps` warps with its own named barrier and its own part of shared memory.
 struct Team {
