@@ -686,6 +686,10 @@ ISPA_API ispa_status ispa_linear_w8a8(const uint8_t* a_q, const float* a_scale, 
  *   even, in [-127, 127].
  * A group with an infinity or a NaN has an infinite or NaN scale (its codes say nothing), so that what is
  * computed from it is no finite number.
+ *
+ * For checkpoints that hold integers: the 8 bits save the weights' memory and their way from HBM, not time on the
+ * tensor cores, which have no integer form, so that a chunk's product runs at the 16-bit rate.  ispa_linear_w8a8 takes
+ * about half the time (4680 x 1536 -> 1536 11.5 against 19.9 us, 5120 -> 5120 68 against 151).
  */
 
 /* Largest D of ispa_linear_i8: D * 128 * 128 stays below 2^31. */
@@ -724,7 +728,9 @@ ISPA_API ispa_status ispa_linear_i8(const int8_t* a_q, const float* a_scale, con
  *
  * Rows are dense [rows][dim].  dim a multiple of 8 up to 32768, rows below 2^31 (else
  * ISPA_ERR_UNSUPPORTED).
- * Statistics and all arithmetic between load and store in fp32.
+ * Statistics and all arithmetic between load and store in fp32, so a row whose squares sum to 2^128 or more has
+ * a norm of zeros.  Few rows and many go through different kernels: the last bits of a row's result may depend on
+ * how many rows the call has.
  */
 #define ISPA_NORM_NONE 0
 #define ISPA_NORM_RMS 1
@@ -794,6 +800,8 @@ ISPA_API ispa_status ispa_gate_residual(const void* x, int32_t x_type, const voi
  * Pair i of every head turns by pos * w_i radians at its axis's position:
  *   (u, v) -> factor * (u cos - v sin, u sin + v cos)
  * Features of a head past 2 * pairs pass unturned (but normed).  Negative positions turn back.
+ * Arithmetic in fp32; as with the norms, the last bits may depend on the number of tokens, and a head or token
+ * whose squares sum to 2^128 or more has a norm of zeros.
  */
 #define ISPA_ROPE_INTERLEAVED 0 /* pair i: features 2 i and 2 i + 1 */
 #define ISPA_ROPE_HALF 1        /* pair i: features i and i + pairs */

@@ -23,8 +23,8 @@ struct LinearForm {
   int split;              // CTAs that share a tile's contraction
 };
 
-// The tensor-core form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in L2)
-// of 9 to 9400 tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's
+// The tensor-core form with the shortest estimated run, and the estimate in ns.  Fitted to measured runs (weights in
+// L2) of 9 to 9400 tokens, 64 to 5120 codes and 256 to 8960 channels: waves of tiles x (blocks x time of one + a tile's
 // fixed part) + launch, fill and the last tile's way out.  A block of a pair of 192 columns costs little more than one
 // of 128, so those win where tiles fill whole waves (4680 x 1536 -> 1536: 19.7 against 22.4 us with pairs of 128 and
 // 23.6 with single CTAs); single CTAs win where there are few tiles (1000 x 1536 -> 1536: 10.0 against 10.9 and 10.3).

@@ -22,11 +22,11 @@
 // 4680 x 5120 -> 5120 150.8 us, 1627 TFLOP/s, with operands and result in L2, 162 from and to HBM; 4680 x 1536 -> 4608
 // 47.0 us; 61 x 5120 -> 640 9.1 us; one token of 1536 x 1536 1.9 us.  What bounds a long contraction is no single unit:
 // a block of 192 columns takes 0.25 us where its UMMAs take 0.19, a team 0.47 us for a block (there are three), and the
-// ring of four stages, from one block's conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out gave
-// 134 us, three quarters of the UMMAs 143.  On the way: one team of eight converter warps 405 us, four teams of two 218;
-// the hand-over without an unrestricted release of cluster scope a block 168; A in TMEM, so that shared memory moves a
-// third less, 225 in pairs of 192 with one lane in the TMA and UMMA roles; whole warps in these roles 159; twelve
-// converter warps 157; sums of two runs in fp32 155; running stage counters 150.
+// ring of four stages, from one block's conversion to the end of its UMMAs, 0.7 us; half of A's conversion left out
+// gave 134 us, three quarters of the UMMAs 143.  On the way: one team of eight converter warps 405 us, four teams of
+// two 218; the hand-over without an unrestricted release of cluster scope a block 168; A in TMEM, so that shared memory
+// moves a third less, 225 in pairs of 192 with one lane in the TMA and UMMA roles; whole warps in these roles 159;
+// twelve converter warps 157; sums of two runs in fp32 155; running stage counters 150.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

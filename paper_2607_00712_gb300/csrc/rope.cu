@@ -407,7 +407,9 @@ cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
   const auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), p.n_rows), dim3(32 * f.warps), 0, s, p);
   };
-  return f.vectors == 1 ? go(rope_kernel<1, HALF>) : f.vectors == 2 ? go(rope_kernel<2, HALF>) : go(rope_kernel<4, HALF>);
+  return f.vectors == 1   ? go(rope_kernel<1, HALF>)
+         : f.vectors == 2 ? go(rope_kernel<2, HALF>)
+                          : go(rope_kernel<4, HALF>);
 }
 
 }  // namespace

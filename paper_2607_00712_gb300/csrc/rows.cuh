@@ -67,8 +67,8 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(const float* h, float inv) {
   return pack_e4m3x4(__fmul_rn(h[0], inv), __fmul_rn(h[1], inv), __fmul_rn(h[2], inv), __fmul_rn(h[3], inv));
 }
 
-// The e4m3 quantisers keep every group whose quotient 448 / amax fp32 holds; up to 448 * 2^-128 it does not, and the zeros
-// of such a group would become NaN.
+// The e4m3 quantisers keep every group whose quotient 448 / amax fp32 holds; up to 448 * 2^-128 it does not, and the
+// zeros of such a group would become NaN.
 constexpr float kTinyE4M3Group = 1.316553672920962e-36f;   // 7 * 2^-122
 
 struct SumOp {
