@@ -42,10 +42,14 @@ int main() {
 """
 
 
+_dir = None
+
+
 @functools.cache
 def _program() -> str:
-    d = tempfile.mkdtemp()
-    src, exe = os.path.join(d, "forms.cc"), os.path.join(d, "forms")
+    global _dir
+    _dir = tempfile.TemporaryDirectory()      # as long as the module lives
+    src, exe = os.path.join(_dir.name, "forms.cc"), os.path.join(_dir.name, "forms")
     with open(src, "w") as f:
         f.write(_PROGRAM)
     subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I",
