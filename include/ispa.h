@@ -12,7 +12,9 @@
  *     the closed-form solve with its feasibility score (Eq. 5-6);
  *   - appending a finished chunk's K/V into a ring-buffer cache;
  *   - the rest of a DiT layer's attention block: its norms with modulation, gate and
- *     residual, and the rotary positions of q and k.
+ *     residual, and the rotary positions of q and k, also on their way into the ring;
+ *   - attention over the window and selected blocks of the history, with the mean keys
+ *     that blocks are scored by and the selection.
  *
  * Conventions (all entry points)
  *   - Every tensor argument is a DEVICE pointer owned by the caller, unless
@@ -873,6 +875,88 @@ typedef struct {
 /* Host-only: steps[i] = round(w_i / (2 pi) * 2^64) of one axis (host array of n_pairs, to be copied to the
  * device next to the other axes'), and *factor (nullable) for ispa_rope. */
 ISPA_API ispa_status ispa_rope_steps(const ispa_rope_frequencies* f, int32_t n_pairs, uint64_t* steps, float* factor);
+
+/* ------------------------------------------------------------ append with rotary positions */
+
+/*
+ * A finished chunk's keys and values from the projection into the ring, with the RMS norm and the rotary positions
+ * of the keys (and, where q is given, of the queries for the attention that follows) on the way: ispa_rope_apply and
+ * the ring's append in one pass, without the turned keys' way through memory.
+ *   k       : the chunk's keys as projected (k->out NULL; k->heads the ring's num_heads)
+ *   q       : the chunk's queries, or NULL; q->out takes the turned queries (bf16)
+ *   v       : bf16 values, token t's heads at v + t * v_stride, [num_heads][head_dim] dense
+ *   pos, pos0, rope : as in ispa_rope_apply, for the n_frames * P tokens; rope->head_dim the ring's
+ *   k_scale : fp32 [H] for a ring with e4m3 keys (the ring's), else NULL;  v_scale : the same for e4m3 values
+ * Strides as in ispa_rope_apply.  Keys are rounded once, from fp32 to the ring's type: bf16, or the code of
+ * k * (1 / scale) saturated at +-448.  q->out may be q->x with the same stride; else no output may overlap an input.
+ * Frame frames_written + i goes to its ring slot; frames_written advances by n_frames.  Errors as ispa_kv_append
+ * and ispa_rope_apply.
+ */
+ISPA_API ispa_status ispa_kv_append_rope(ispa_kv_ring* ring, const ispa_rope* rope, const ispa_rope_rows* k,
+                                         const ispa_rope_rows* q, const void* v, int64_t v_stride,
+                                         const int32_t* pos, int64_t pos0, int32_t n_frames, const float* k_scale,
+                                         const float* v_scale, ispa_stream stream);
+
+/* ------------------------------------------------------------ attention over selected blocks of the history */
+/*
+ * Between the F-layer's whole history and the L-layer's window: attention over the window, the chunk and, for every
+ * head and block of 128 queries, the top_k blocks of the history whose mean keys score highest.  (The paper keeps or
+ * drops a layer's history as a whole.)
+ *
+ * A frame's P tokens are cut into nb = ceil(P / block) blocks of `block` tokens (a multiple of 64, at most 2^20; the
+ * frame's last block has what is left).  Block b of the frame in ring slot s has the number s * nb + b, which names
+ * it in all that follows; capacity_frames * nb below 2^31.  Sizes off these are ISPA_ERR_UNSUPPORTED.
+ *
+ * A rollout keeps `means` next to the ring: after an append, ispa_key_means of the frames appended; before an
+ * attention, ispa_select_blocks with its queries and window.
+ */
+
+/*
+ * Mean key of every block of the resident frames first_frame .. first_frame + n_frames - 1 (logical frames):
+ *   means : fp32 [num_heads][capacity_frames * nb][head_dim]; the blocks of other frames are left as they are
+ *   k_scale : fp32 [H] (device) for a ring with e4m3 keys, whose means are of code * scale; NULL for a bf16 ring
+ * Sums in fp32.  Errors: ISPA_ERR_CAPACITY if a frame is not resident.
+ */
+ISPA_API ispa_status ispa_key_means(const ispa_kv_ring* ring, const float* k_scale, int64_t first_frame,
+                                    int32_t n_frames, int32_t block, float* means, ispa_stream stream);
+
+/* Workspace bytes of ispa_select_blocks (for any window); 0 for bad sizes. */
+ISPA_API size_t ispa_select_blocks_workspace_size(const ispa_kv_ring* ring, int32_t block, int32_t n_q);
+
+/*
+ * For head h and query block i (queries 128 i .. 128 i + 127 of the n_q): the history's blocks, those of resident
+ * frames outside the window, with the top_k highest scores
+ *   score(h, i, b) = sum over the block's queries of q . means[h][b]
+ * ranked in 64-bit arithmetic; equal scores go to the lower number, NaN ranks last.
+ *   q      : bf16 [n_q][num_heads][head_dim] (as given to the attention, or before its coding)
+ *   means  : fp32 [num_heads][capacity_frames * nb][head_dim] (16-byte aligned)
+ *   blocks : int32 [num_heads][ceil(n_q / 128)][top_k] (written): block numbers, ascending, then -1 where the
+ *            history has fewer than top_k blocks
+ * The ring's buffers and k_format are not used.  top_k >= 1.  Errors: ISPA_ERR_CAPACITY as ispa_window_resolve.
+ */
+ISPA_API ispa_status ispa_select_blocks(const ispa_kv_ring* ring, ispa_window win, int32_t block, const float* means,
+                                        const void* q, int32_t n_q, int32_t top_k, int32_t* blocks, void* workspace,
+                                        size_t ws_bytes, ispa_stream stream);
+
+/*
+ * The chunk attention of ispa_attn_local_ex with the listed blocks as further keys:
+ *   blocks : int32 [num_heads][ceil(n_q / 128)][top_k] (device), as ispa_select_blocks writes them or the caller's
+ *            own.  Of a list the first min(top_k, resident blocks) entries are read.  A number outside the resident
+ *            blocks names no key; a block named twice, or in the window too, counts twice.
+ *   k_cur, v_cur : both NULL where the call has no chunk (the new frames are in the ring already); then no flags
+ * Other arguments as in ispa_attn_local_ex.  A query that sees no key has out = 0 and lse = -inf.  Tokens behind a
+ * frame's last one are not read for listed blocks, whatever they hold.
+ */
+ISPA_API ispa_status ispa_attn_blocks(const ispa_kv_ring* ring, ispa_window win, int32_t block, const int32_t* blocks,
+                                      int32_t top_k, const void* q, const void* k_cur, const void* v_cur, int32_t n_q,
+                                      float scale, uint32_t flags, void* out, float* lse, ispa_stream stream);
+/* The same over a ring with e4m3 keys (ISPA_KV_K_E4M3); codes and scales as in ispa_attn_local_qk8.  k_cur_scale
+ * may be NULL where there is no chunk. */
+ISPA_API ispa_status ispa_attn_blocks_qk8(const ispa_kv_ring* ring, const float* k_ring_scale, ispa_window win,
+                                          int32_t block, const int32_t* blocks, int32_t top_k, const void* q8,
+                                          const float* q_scale, const void* k8_cur, const float* k_cur_scale,
+                                          const void* v_cur, int32_t n_q, float scale, void* out, float* lse,
+                                          ispa_stream stream);
 
 #ifdef __cplusplus
 }

@@ -188,6 +188,17 @@ _SIGS = {
     "ispa_gate_residual": (c_int32, [c_void_p, c_int32, c_void_p, c_int64, c_int32, POINTER(Norm), c_float, c_float,
                                      POINTER(Modulation), c_void_p, POINTER(Norm), POINTER(RowsOut), c_void_p]),
     "ispa_rope_apply": (c_int32, [POINTER(Rope), POINTER(RopeRows), c_int32, c_void_p, c_int64, c_int64, c_void_p]),
+    "ispa_kv_append_rope": (c_int32, [POINTER(KVRing), POINTER(Rope), POINTER(RopeRows), POINTER(RopeRows), c_void_p,
+                                      c_int64, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "ispa_key_means": (c_int32, [POINTER(KVRing), c_void_p, c_int64, c_int32, c_int32, c_void_p, c_void_p]),
+    "ispa_select_blocks_workspace_size": (c_size_t, [POINTER(KVRing), c_int32, c_int32]),
+    "ispa_select_blocks": (c_int32, [POINTER(KVRing), Window, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                                     c_void_p, c_size_t, c_void_p]),
+    "ispa_attn_blocks": (c_int32, [POINTER(KVRing), Window, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                   c_int32, c_float, c_uint32, c_void_p, c_void_p, c_void_p]),
+    "ispa_attn_blocks_qk8": (c_int32, [POINTER(KVRing), c_void_p, Window, c_int32, c_void_p, c_int32, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_float, c_void_p, c_void_p,
+                                       c_void_p]),
     "ispa_rope_steps": (c_int32, [POINTER(RopeFrequencies), c_int32, POINTER(c_uint64), POINTER(c_float)]),
     "ispa_ls_solve": (c_int32, [POINTER(LSState), c_void_p, c_int32, c_double, c_void_p, POINTER(c_double),
                                 c_void_p, c_size_t, c_void_p]),
@@ -601,3 +612,41 @@ def ispa_rope_steps(n_pairs: int, base: float = 10000.0, scaling: int = ISPA_ROP
     steps, factor = (c_uint64 * max(n_pairs, 1))(), c_float(0.0)
     _check(lib().ispa_rope_steps(ctypes.byref(f), n_pairs, steps, ctypes.byref(factor)), "ispa_rope_steps")
     return list(steps), factor.value
+
+
+# ---------------------------------------------------------------- append with rotary positions
+def ispa_kv_append_rope(ring: KVRing, rope: Rope, k: RopeRows, q: RopeRows | None, v, v_stride: int, pos, pos0: int,
+                        n_frames: int, k_scale=None, v_scale=None, stream=None) -> None:
+    """k: rope_rows with out None and out_stride 0 (the keys go into the ring)."""
+    _check(lib().ispa_kv_append_rope(ctypes.byref(ring), rope, k, q, _ptr(v), v_stride, _ptr(pos), pos0, n_frames,
+                                     _ptr(k_scale), _ptr(v_scale), _stream(stream)), "ispa_kv_append_rope")
+
+
+# ---------------------------------------------------------------- attention over selected blocks of the history
+def ispa_key_means(ring: KVRing, k_scale, first_frame: int, n_frames: int, block: int, means, stream=None) -> None:
+    _check(lib().ispa_key_means(ctypes.byref(ring), _ptr(k_scale), first_frame, n_frames, block, _ptr(means),
+                                _stream(stream)), "ispa_key_means")
+
+
+def ispa_select_blocks_workspace_size(ring: KVRing, block: int, n_q: int) -> int:
+    return lib().ispa_select_blocks_workspace_size(ctypes.byref(ring), block, n_q)
+
+
+def ispa_select_blocks(ring: KVRing, win: Window, block: int, means, q, n_q: int, top_k: int, blocks, workspace,
+                       ws_bytes: int, stream=None) -> None:
+    _check(lib().ispa_select_blocks(ctypes.byref(ring), win, block, _ptr(means), _ptr(q), n_q, top_k, _ptr(blocks),
+                                    _ptr(workspace), ws_bytes, _stream(stream)), "ispa_select_blocks")
+
+
+def ispa_attn_blocks(ring: KVRing, win: Window, block: int, blocks, top_k: int, q, k_cur, v_cur, n_q: int, scale: float,
+                     flags: int, out, lse=None, stream=None) -> None:
+    _check(lib().ispa_attn_blocks(ctypes.byref(ring), win, block, _ptr(blocks), top_k, _ptr(q), _ptr(k_cur),
+                                  _ptr(v_cur), n_q, scale, flags, _ptr(out), _ptr(lse), _stream(stream)),
+           "ispa_attn_blocks")
+
+
+def ispa_attn_blocks_qk8(ring: KVRing, k_ring_scale, win: Window, block: int, blocks, top_k: int, q8, q_scale, k8_cur,
+                         k_cur_scale, v_cur, n_q: int, scale: float, out, lse=None, stream=None) -> None:
+    _check(lib().ispa_attn_blocks_qk8(ctypes.byref(ring), _ptr(k_ring_scale), win, block, _ptr(blocks), top_k, _ptr(q8),
+                                      _ptr(q_scale), _ptr(k8_cur), _ptr(k_cur_scale), _ptr(v_cur), n_q, scale,
+                                      _ptr(out), _ptr(lse), _stream(stream)), "ispa_attn_blocks_qk8")

@@ -26,6 +26,7 @@ constexpr uint64_t kDefaultWaitLimitNs = 1000ull * 1000 * 1000;
 std::atomic<uint64_t> g_wait_limit{kDefaultWaitLimitNs};
 
 bool aligned16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                    const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -385,14 +386,37 @@ struct Qk8Scales {
   int64_t vt_ld = 0;
 };
 
+// Blocks of a frame of P tokens; 0: bad sizes.
+int64_t blocks_of(int32_t P, int32_t block) {
+  if (block < kPiece || block % kPiece != 0 || block > (1 << 20)) return 0;
+  return (static_cast<int64_t>(P) + block - 1) / block;
+}
+ispa_status check_blocks(const ispa_kv_ring* r, int32_t block) {
+  const int64_t nb = blocks_of(r->tokens_per_frame, block);
+  return nb > 0 && nb * r->capacity_frames <= INT32_MAX && r->num_heads <= 65535 ? ISPA_OK : ISPA_ERR_UNSUPPORTED;
+}
+
+// Lists of blocks beside the segments (MODE_LOCAL).
+struct BlockLists {
+  int32_t block;
+  const int32_t* ids;
+  int32_t top_k;
+};
+
 ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, const void* q,
                         const void* k_cur, const void* v_cur, int32_t n_q, float scale, uint32_t flags,
                         void* out, void* out_loc, float* lse, float* lse_loc, float* disc_part,
-                        cudaStream_t stream, const Qk8Scales* qk8 = nullptr) {
+                        cudaStream_t stream, const Qk8Scales* qk8 = nullptr, const BlockLists* blocks = nullptr) {
   ispa_status st = check_ring(ring);
   if (st != ISPA_OK) return st;
+  const bool has_chunk = !blocks || k_cur || v_cur;
+  if (!has_chunk) {   // stands in for the chunk's maps, which no tile uses
+    k_cur = ring->k;
+    v_cur = ring->v;
+    if (flags) return ISPA_ERR_INVALID_ARG;
+  }
   if ((ring->k_format != ISPA_KV_BF16) != (qk8 != nullptr)) return ISPA_ERR_INVALID_ARG;
-  if (qk8 && (!qk8->q || !qk8->k_cur || !qk8->k_ring)) return ISPA_ERR_INVALID_ARG;
+  if (qk8 && (!qk8->q || (!qk8->k_cur && has_chunk) || !qk8->k_ring)) return ISPA_ERR_INVALID_ARG;
   const bool kv8 = ring->k_format == ISPA_KV_KV_E4M3;
   if (kv8 && (!qk8->v || qk8->vt_ld < n_q || qk8->vt_ld % 16 != 0)) return ISPA_ERR_INVALID_ARG;
   if (!kv8 && qk8 && qk8->v) return ISPA_ERR_INVALID_ARG;   // 8-bit P V needs a ring with e4m3 values
@@ -403,6 +427,8 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
     return ISPA_ERR_INVALID_ARG;
   if (mode == MODE_DUAL && (!aligned16(out_loc) || !disc_part)) return ISPA_ERR_INVALID_ARG;
   if (!(scale >= 0.f) || !isfinite(scale)) return ISPA_ERR_INVALID_ARG;
+  if (blocks && (!aligned4(blocks->ids) || blocks->top_k < 1 || blocks->block < 1)) return ISPA_ERR_INVALID_ARG;
+  if (blocks && (st = check_blocks(ring, blocks->block)) != ISPA_OK) return st;
   ispa_key_sets ks;
   st = resolve(ring, mode == MODE_FULL ? ispa_window{0, 0} : win, &ks);
   if (st != ISPA_OK) return st;
@@ -428,12 +454,33 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
   } else {
     tiles += add_segs(p, 0, ks.local, ks.n_local, P, bn, al);
   }
-  if (mode != MODE_HIST) {
+  if (mode != MODE_HIST && has_chunk) {
     AttnSeg& s = p.seg[p.n_seg++];
     s.src = 1;
     s.start = 0;
     s.count = n_q;
     tiles += (n_q + bn - 1) / bn;
+  }
+  AttnLists lists = {};
+  if (blocks) {
+    lists.ids = blocks->ids;
+    lists.top_k = blocks->top_k;
+    lists.block = blocks->block;
+    lists.P = P;
+    lists.nb = static_cast<int32_t>(blocks_of(P, blocks->block));
+    lists.n_ids = static_cast<int32_t>(std::min<int64_t>(ring->frames_written, ring->capacity_frames)) * lists.nb;
+    lists.entries = std::min(lists.top_k, lists.n_ids);
+    lists.pieces = (std::min(blocks->block, P) + kPiece - 1) / kPiece;
+    // at most ring tokens / 64 + blocks pieces: as tiles of 192 keys below 2^31
+    const int64_t n = (static_cast<int64_t>(lists.entries) * lists.pieces + 2) / 3;
+    if ((n + tiles) * bn > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
+    if (n > 0) {
+      AttnSeg& s = p.seg[p.n_seg++];
+      s.src = 2;
+      s.count = static_cast<int32_t>(n) * bn;
+      tiles += static_cast<int>(n);
+    }
+    if (tiles == 0) return launch_empty_branch(out, lse, n_q, H, HD, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
   }
   if (mode != MODE_HIST) {
     p.n_local_tiles = tiles;
@@ -498,14 +545,25 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
          encode_tmap_4d(&tkc, k_cur, dims_c8, str_c8, box_k8, true) &&
          encode_tmap_4d(&tkr, ring->k, dims_r8, str_r8, box_k8, true);
     p.q_scale = qk8->q;
-    p.kc_scale = qk8->k_cur;
+    p.kc_scale = has_chunk ? qk8->k_cur : qk8->k_ring;
     p.kr_scale = qk8->k_ring;
   } else {
     ok = ok && encode_tmap_4d(&tq, q, dims_c, str_c, box_q) && encode_tmap_4d(&tkc, k_cur, dims_c, str_c, box_k) &&
          encode_tmap_4d(&tkr, ring->k, dims_r, str_r, box_k);
   }
+  if (ok && blocks) {
+    const auto frames = [&](CUtensorMap* m, const void* base, uint64_t row, bool u8) {
+      const uint64_t frame_b = row * static_cast<uint64_t>(P), cap = static_cast<uint64_t>(ring->capacity_frames);
+      const uint64_t dims[4] = {static_cast<uint64_t>(HD), static_cast<uint64_t>(P), cap, static_cast<uint64_t>(H)};
+      const uint64_t str[3] = {row, frame_b, frame_b * cap};
+      const uint32_t box[4] = {u8 ? 128u : 64u, kPiece, 1, 1};
+      return encode_tmap_4d(m, base, dims, str, box, u8);
+    };
+    ok = frames(&lists.k, ring->k, qk8 ? 128 : row_b, qk8 != nullptr) && frames(&lists.v, ring->v, row_b, false);
+  }
   if (!ok) return ISPA_ERR_CUDA;
-  if (launch_attention(HD, &tq, &tkr, &tvr, &tkc, &tvc, p, stream) != cudaSuccess) return ISPA_ERR_CUDA;
+  if (launch_attention(HD, &tq, &tkr, &tvr, &tkc, &tvc, p, stream, blocks ? &lists : nullptr) != cudaSuccess)
+    return ISPA_ERR_CUDA;
   return ISPA_OK;
 }
 
@@ -525,8 +583,6 @@ __global__ void wait_probe_kernel(uint64_t limit_ns, int* status) {
 }
 
 bool aligned16_or_null(const void* p) { return !p || aligned16(p); }
-bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
 bool good_norm(const ispa_norm* n) {
   return n->kind >= ISPA_NORM_NONE && n->kind <= ISPA_NORM_LAYER && n->eps >= 0.f && isfinite(n->eps) &&
          aligned16_or_null(n->weight) && aligned16_or_null(n->bias);
@@ -563,6 +619,58 @@ ispa_status norm_params(NormParams& p, const void* x, int32_t x_type, int64_t ro
     p.out_scale = out->scale;
     p.format = out->format;
   }
+  p.status = device_status_ptr();
+  p.wait_limit_ns = g_wait_limit.load();
+  return p.status ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+// Checks and parameters of the rotary entry points.  to_ring: the last of the rows has no `out`.
+ispa_status rope_params(RopeParams& p, const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows,
+                        const int32_t* pos, int64_t pos0, int64_t n, bool to_ring) {
+  if (!rope || !rows || !rope->steps || !pos || n_rows < 1 || n_rows > 2 || n <= 0 || rope->n_axes < 1 ||
+      rope->n_axes > ISPA_ROPE_MAX_AXES || rope->head_dim <= 0 || !isfinite(rope->factor) ||
+      (rope->layout != ISPA_ROPE_INTERLEAVED && rope->layout != ISPA_ROPE_HALF) ||
+      (reinterpret_cast<uintptr_t>(rope->steps) & 7u) || (reinterpret_cast<uintptr_t>(pos) & 3u))
+    return ISPA_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < rope->n_axes; ++a) {
+    if (rope->axis_pairs[a] < 0) return ISPA_ERR_INVALID_ARG;
+    pairs += rope->axis_pairs[a];
+  }
+  if (pairs < 1) return ISPA_ERR_INVALID_ARG;
+  for (int i = 0; i < n_rows; ++i) {
+    const ispa_rope_rows& r = rows[i];
+    const bool ring_row = to_ring && i == n_rows - 1;
+    if (!aligned16(r.x) || (!ring_row && !aligned16(r.out)) || (ring_row && (r.out || r.out_stride)) ||
+        r.heads <= 0 || r.norm < ISPA_QK_NORM_NONE || r.norm > ISPA_QK_NORM_TOKEN)
+      return ISPA_ERR_INVALID_ARG;
+    const int64_t width = static_cast<int64_t>(r.heads) * rope->head_dim;
+    if (r.x_stride < width || r.x_stride % 8 != 0 ||
+        (!ring_row && (r.out_stride < width || r.out_stride % 8 != 0 || (r.x == r.out && r.x_stride != r.out_stride))))
+      return ISPA_ERR_INVALID_ARG;
+    if (r.norm != ISPA_QK_NORM_NONE &&
+        ((r.norm_weight && !aligned16(r.norm_weight)) || !(r.eps >= 0.f) || !isfinite(r.eps)))
+      return ISPA_ERR_INVALID_ARG;
+    if (width > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
+  }
+  if (rope->head_dim % 8 != 0 || rope->head_dim > 256 || 2 * pairs > rope->head_dim ||
+      (rope->layout == ISPA_ROPE_HALF && pairs % 4 != 0) || n > INT32_MAX / 2)
+    return ISPA_ERR_UNSUPPORTED;
+  for (int i = 0; i < n_rows; ++i)
+    p.rows[i] = {rows[i].x, rows[i].out, rows[i].x_stride, rows[i].out_stride, rows[i].norm_weight, rows[i].eps,
+                 rows[i].heads, rows[i].norm};
+  p.n_rows = n_rows;
+  p.n = n;
+  p.pos0 = pos0;
+  p.pos = pos;
+  p.steps = rope->steps;
+  p.head_dim = rope->head_dim;
+  p.pairs = static_cast<int32_t>(pairs);
+  p.lanes_per_head = 1;
+  while (8 * p.lanes_per_head < rope->head_dim) p.lanes_per_head *= 2;
+  p.axis_end[0] = rope->axis_pairs[0];
+  p.axis_end[1] = p.axis_end[0] + (rope->n_axes > 1 ? rope->axis_pairs[1] : 0);
+  p.factor = rope->factor;
   p.status = device_status_ptr();
   p.wait_limit_ns = g_wait_limit.load();
   return p.status ? ISPA_OK : ISPA_ERR_CUDA;
@@ -934,54 +1042,133 @@ ispa_status ispa_gate_residual(const void* x, int32_t x_type, const void* y, int
 
 ispa_status ispa_rope_apply(const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows, const int32_t* pos,
                             int64_t pos0, int64_t n, ispa_stream stream) {
-  if (!rope || !rows || !rope->steps || !pos || n_rows < 1 || n_rows > 2 || n <= 0 || rope->n_axes < 1 ||
-      rope->n_axes > ISPA_ROPE_MAX_AXES || rope->head_dim <= 0 || !isfinite(rope->factor) ||
-      (rope->layout != ISPA_ROPE_INTERLEAVED && rope->layout != ISPA_ROPE_HALF) ||
-      (reinterpret_cast<uintptr_t>(rope->steps) & 7u) || (reinterpret_cast<uintptr_t>(pos) & 3u))
-    return ISPA_ERR_INVALID_ARG;
-  int64_t pairs = 0;
-  for (int a = 0; a < rope->n_axes; ++a) {
-    if (rope->axis_pairs[a] < 0) return ISPA_ERR_INVALID_ARG;
-    pairs += rope->axis_pairs[a];
-  }
-  if (pairs < 1) return ISPA_ERR_INVALID_ARG;
-  for (int i = 0; i < n_rows; ++i) {
-    const ispa_rope_rows& r = rows[i];
-    if (!aligned16(r.x) || !aligned16(r.out) || r.heads <= 0 || r.norm < ISPA_QK_NORM_NONE ||
-        r.norm > ISPA_QK_NORM_TOKEN)
-      return ISPA_ERR_INVALID_ARG;
-    const int64_t width = static_cast<int64_t>(r.heads) * rope->head_dim;
-    if (r.x_stride < width || r.out_stride < width || r.x_stride % 8 != 0 || r.out_stride % 8 != 0 ||
-        (r.x == r.out && r.x_stride != r.out_stride))
-      return ISPA_ERR_INVALID_ARG;
-    if (r.norm != ISPA_QK_NORM_NONE &&
-        ((r.norm_weight && !aligned16(r.norm_weight)) || !(r.eps >= 0.f) || !isfinite(r.eps)))
-      return ISPA_ERR_INVALID_ARG;
-    if (width > INT32_MAX) return ISPA_ERR_UNSUPPORTED;
-  }
-  if (rope->head_dim % 8 != 0 || rope->head_dim > 256 || 2 * pairs > rope->head_dim ||
-      (rope->layout == ISPA_ROPE_HALF && pairs % 4 != 0) || n > INT32_MAX / 2)
-    return ISPA_ERR_UNSUPPORTED;
   RopeParams p = {};
-  for (int i = 0; i < n_rows; ++i)
-    p.rows[i] = {rows[i].x, rows[i].out, rows[i].x_stride, rows[i].out_stride, rows[i].norm_weight, rows[i].eps,
-                 rows[i].heads, rows[i].norm};
-  p.n_rows = n_rows;
-  p.n = n;
-  p.pos0 = pos0;
-  p.pos = pos;
-  p.steps = rope->steps;
-  p.head_dim = rope->head_dim;
-  p.pairs = static_cast<int32_t>(pairs);
-  p.lanes_per_head = 1;
-  while (8 * p.lanes_per_head < rope->head_dim) p.lanes_per_head *= 2;
-  p.axis_end[0] = rope->axis_pairs[0];
-  p.axis_end[1] = p.axis_end[0] + (rope->n_axes > 1 ? rope->axis_pairs[1] : 0);
-  p.factor = rope->factor;
-  p.status = device_status_ptr();
-  p.wait_limit_ns = g_wait_limit.load();
-  if (!p.status) return ISPA_ERR_CUDA;
+  const ispa_status st = rope_params(p, rope, rows, n_rows, pos, pos0, n, false);
+  if (st != ISPA_OK) return st;
   return launch_rope(p, rope->layout == ISPA_ROPE_HALF, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+ispa_status ispa_kv_append_rope(ispa_kv_ring* ring, const ispa_rope* rope, const ispa_rope_rows* k,
+                                const ispa_rope_rows* q, const void* v, int64_t v_stride, const int32_t* pos,
+                                int64_t pos0, int32_t n_frames, const float* k_scale, const float* v_scale,
+                                ispa_stream stream) {
+  ispa_status st = check_ring(ring);
+  if (st != ISPA_OK) return st;
+  const bool k8 = ring->k_format != ISPA_KV_BF16, v8 = ring->k_format == ISPA_KV_KV_E4M3;
+  const int32_t H = ring->num_heads, d = ring->head_dim, P = ring->tokens_per_frame;
+  if (!rope || !k || n_frames <= 0 || k->heads != H || rope->head_dim != d || !aligned16(v) || v_stride % 8 != 0 ||
+      v_stride < static_cast<int64_t>(H) * d || !aligned16(ring->k) || !aligned16(ring->v) ||
+      (k8 ? !aligned4(k_scale) : k_scale != nullptr) || (v8 ? !aligned4(v_scale) : v_scale != nullptr))
+    return ISPA_ERR_INVALID_ARG;
+  if (n_frames > kMaxAppendFrames || n_frames > ring->capacity_frames - ring->n_sink_frames) return ISPA_ERR_CAPACITY;
+  if (H > 65535) return ISPA_ERR_UNSUPPORTED;
+  ispa_rope_rows rows[2] = {q ? *q : *k, *k};
+  RopeAppendParams p = {};
+  st = rope_params(p, rope, rows, q ? 2 : 1, pos, pos0, static_cast<int64_t>(n_frames) * P, true);
+  if (st != ISPA_OK) return st;
+  p.k_ring = ring->k;
+  p.k_scale = k_scale;
+  p.v = v8 ? nullptr : static_cast<const __nv_bfloat16*>(v);
+  p.v_stride = v_stride;
+  p.v_ring = static_cast<__nv_bfloat16*>(ring->v);
+  p.ring_tok = static_cast<int64_t>(ring->capacity_frames) * P;
+  p.P = P;
+  for (int i = 0; i < n_frames; ++i) p.slot[i] = slot_of(ring, ring->frames_written + i);
+  if (launch_rope_append(p, rope->layout == ISPA_ROPE_HALF, stream) != cudaSuccess) return ISPA_ERR_CUDA;
+  if (v8 && launch_append_vt(p.slot, n_frames, P, H, v, v_stride, ring->v, v_scale, ispa_ring_vt_stride(ring),
+                             stream) != cudaSuccess)
+    return ISPA_ERR_CUDA;
+  ring->frames_written += n_frames;
+  return ISPA_OK;
+}
+
+// ------------------------------------------------------------ blocks of the history
+
+ispa_status ispa_key_means(const ispa_kv_ring* ring, const float* k_scale, int64_t first_frame, int32_t n_frames,
+                           int32_t block, float* means, ispa_stream stream) {
+  ispa_status st = check_ring(ring);
+  if (st != ISPA_OK) return st;
+  const bool k8 = ring->k_format != ISPA_KV_BF16;
+  if (n_frames <= 0 || block <= 0 || !aligned16(ring->k) || !aligned16(means) ||
+      (k8 ? !aligned4(k_scale) : k_scale != nullptr))
+    return ISPA_ERR_INVALID_ARG;
+  if ((st = check_blocks(ring, block)) != ISPA_OK) return st;
+  // the resident frames are the sinks and a run up to the last one
+  if (first_frame < 0 || first_frame > ring->frames_written - n_frames) return ISPA_ERR_CAPACITY;
+  for (int32_t i = 0; i < n_frames; ++i)
+    if (!resident(ring, first_frame + i)) return ISPA_ERR_CAPACITY;
+  MeansParams p = {};
+  p.k = ring->k;
+  p.k_scale = k_scale;
+  p.means = means;
+  p.first_frame = first_frame;
+  p.n_sink = ring->n_sink_frames;
+  p.capacity = ring->capacity_frames;
+  p.P = ring->tokens_per_frame;
+  p.block = block;
+  p.nb = static_cast<int32_t>(blocks_of(p.P, block));
+  p.H = ring->num_heads;
+  p.d = ring->head_dim;
+  p.units = static_cast<int64_t>(n_frames) * p.nb;
+  return launch_key_means(p, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+size_t ispa_select_blocks_workspace_size(const ispa_kv_ring* ring, int32_t block, int32_t n_q) {
+  if (check_ring(ring) != ISPA_OK || n_q <= 0 || check_blocks(ring, block) != ISPA_OK) return 0;
+  return select_ws_bytes(ring->num_heads, (static_cast<int64_t>(n_q) + kSelectQueries - 1) / kSelectQueries,
+                         ring->head_dim, blocks_of(ring->tokens_per_frame, block) * ring->capacity_frames);
+}
+
+ispa_status ispa_select_blocks(const ispa_kv_ring* ring, ispa_window win, int32_t block, const float* means,
+                               const void* q, int32_t n_q, int32_t top_k, int32_t* blocks, void* workspace,
+                               size_t ws_bytes, ispa_stream stream) {
+  ispa_status st = check_ring(ring);
+  if (st != ISPA_OK) return st;
+  if (n_q <= 0 || top_k <= 0 || block <= 0 || !aligned16(means) || !aligned16(q) || !aligned4(blocks))
+    return ISPA_ERR_INVALID_ARG;
+  if ((st = check_blocks(ring, block)) != ISPA_OK) return st;
+  ispa_key_sets ks;
+  if ((st = resolve(ring, win, &ks)) != ISPA_OK) return st;
+  if (!aligned16(workspace) || ws_bytes < ispa_select_blocks_workspace_size(ring, block, n_q))
+    return ISPA_ERR_WORKSPACE;
+  SelectParams p = {};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.means = means;
+  p.blocks = blocks;
+  p.ws = workspace;
+  p.n_q = n_q;
+  p.n_qt = static_cast<int32_t>((static_cast<int64_t>(n_q) + kSelectQueries - 1) / kSelectQueries);
+  p.H = ring->num_heads;
+  p.d = ring->head_dim;
+  p.top_k = top_k;
+  const int32_t nb = static_cast<int32_t>(blocks_of(ring->tokens_per_frame, block));
+  p.ids = static_cast<int64_t>(ring->capacity_frames) * nb;
+  p.n_runs = ks.n_hist;
+  for (int r = 0; r < ks.n_hist; ++r) {
+    p.run_shift[r] = ks.hist[r].first_slot * nb - p.n_cand;
+    p.n_cand += ks.hist[r].n_slots * nb;
+    p.run_end[r] = p.n_cand;
+  }
+  return launch_select(p, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
+}
+
+ispa_status ispa_attn_blocks(const ispa_kv_ring* ring, ispa_window win, int32_t block, const int32_t* blocks,
+                             int32_t top_k, const void* q, const void* k_cur, const void* v_cur, int32_t n_q,
+                             float scale, uint32_t flags, void* out, float* lse, ispa_stream stream) {
+  const BlockLists lists{block, blocks, top_k};
+  return attn_common(MODE_LOCAL, ring, win, q, k_cur, v_cur, n_q, scale, flags, out, nullptr, lse, nullptr, nullptr,
+                     stream, nullptr, &lists);
+}
+
+ispa_status ispa_attn_blocks_qk8(const ispa_kv_ring* ring, const float* k_ring_scale, ispa_window win, int32_t block,
+                                 const int32_t* blocks, int32_t top_k, const void* q8, const float* q_scale,
+                                 const void* k8_cur, const float* k_cur_scale, const void* v_cur, int32_t n_q,
+                                 float scale, void* out, float* lse, ispa_stream stream) {
+  if (ring && ring->k_format != ISPA_KV_K_E4M3) return ISPA_ERR_INVALID_ARG;
+  const BlockLists lists{block, blocks, top_k};
+  const Qk8Scales sc{q_scale, k_cur_scale, k_ring_scale};
+  return attn_common(MODE_LOCAL, ring, win, q8, k8_cur, v_cur, n_q, scale, 0u, out, nullptr, lse, nullptr, nullptr,
+                     stream, &sc, &lists);
 }
 
 ispa_status ispa_rope_steps(const ispa_rope_frequencies* f, int32_t n_pairs, uint64_t* steps, float* factor) {

@@ -52,6 +52,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "internal.h"
 #include "pdl.cuh"
@@ -196,8 +197,30 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// Piece u of a list: its frame's slot, its first token in the frame (P where the piece does not exist: a box there
+// arrives as zeros) and how many tokens it has.
+struct Piece {
+  int frame, row, count;
+};
+__device__ __forceinline__ Piece piece_of(const AttnLists& l, const int32_t* list, int u) {
+  Piece r{0, l.P, 0};
+  const int e = u / l.pieces;
+  if (e < l.entries) {
+    const int id = __ldg(list + e);
+    if (id >= 0 && id < l.n_ids) {
+      r.frame = id / l.nb;
+      r.row = (id - r.frame * l.nb) * l.block + kPiece * (u - e * l.pieces);
+      r.count = max(0, min(kPiece, l.P - r.row));
+    }
+  }
+  return r;
+}
+
 }  // namespace
 
+// Params = AttnBlocksParams (BLOCKS): the instances for listed blocks.  Their tiles come after the dense segments' as three boxes of 64
+// tokens each, so that a 64-token block costs a third of a tile wherever it lies.
+//
 // SPLIT: the instance for items that leave SMs idle (see split_plan).  A cluster works on one item:
 // rank r of c visits the key tiles [n r / c, n (r + 1) / c), and at the end each CTA leaves its
 // unnormalised O, m and l in its shared memory (the stages are free by then) and merges 128 / c
@@ -221,12 +244,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // epilogue's reads of O.
 // The TMA thread asks for the next item a few tiles before the end of the current one and
 // publishes it (or "none") to the UMMA thread and the softmax warps through a two-slot mailbox.
-template <int HD, bool QK8, bool PV8, bool TRACE, bool SPLIT>
+template <int HD, bool QK8, bool PV8, bool TRACE, bool SPLIT, typename Params = AttnParams>
 __global__ void __launch_bounds__(NTHREADS, 1)
     attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kr,
                 const __grid_constant__ CUtensorMap tm_vr, const __grid_constant__ CUtensorMap tm_kc,
-                const __grid_constant__ CUtensorMap tm_vc, const AttnParams p) {
+                const __grid_constant__ CUtensorMap tm_vc, const __grid_constant__ Params p) {
   using C = Cfg<HD, QK8, PV8>;
+  constexpr bool BLOCKS = !std::is_same_v<Params, AttnParams>;
+  static_assert(!BLOCKS || (!PV8 && !TRACE), "instances for listed blocks");
   // The dynamic shared window must start on a 1 KB boundary (the swizzle atoms of the
   // TMA boxes); the declaration asks for it and the check below enforces it.
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -296,6 +321,10 @@ __global__ void __launch_bounds__(NTHREADS, 1)
     tma_prefetch_desc(&tm_vr);
     tma_prefetch_desc(&tm_kc);
     tma_prefetch_desc(&tm_vc);
+    if constexpr (BLOCKS) {
+      tma_prefetch_desc(&p.lists.k);
+      tma_prefetch_desc(&p.lists.v);
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -361,6 +390,9 @@ __global__ void __launch_bounds__(NTHREADS, 1)
       int vk = 0, vj = 0, vseg = seg0, voff = off0;   // V cursor
       int t = 0, tv = 0;                        // global K and V tiles issued
       bool k_live = true, ok = true;
+      // listed blocks: where the pieces of the K cursor's last two tiles lie, for their values (V trails K by at most
+      // one tile)
+      int2 at[2][3] = {};
       load_q();
       if (req_at == 0) request();
       // Loads are issued in the order their stages free up: inside an item the UMMA stream is
@@ -369,11 +401,20 @@ __global__ void __launch_bounds__(NTHREADS, 1)
       auto issue_v = [&]() -> bool {
         const int vs = tv % C::VST;
         if (!mbar_wait(b.v_empty0 + 8 * vs, ((tv / C::VST) & 1) ^ 1, wc, 2, tv)) return false;
-        const bool chunk = p.seg[vseg].src != 0;
+        const bool chunk = p.seg[vseg].src == 1;
         mbar_arrive_expect_tx(b.v_full0 + 8 * vs, C::V_TILE);
         const uint32_t sV = sbase + C::OFF_V + vs * C::V_TILE;
         const int vhead = vk == kk ? kh : prev_h;
-        if constexpr (PV8) {
+        if (BLOCKS && p.seg[vseg].src == 2) {
+          if constexpr (BLOCKS) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+#pragma unroll
+              for (int c = 0; c < C::NBOX; ++c)
+                tma_load_4d(sV + c * C::KBOX + i * kPiece * 128, &p.lists.v, b.v_full0 + 8 * vs, 64 * c,
+                            at[tv & 1][i].y, at[tv & 1][i].x, vhead);
+          }
+        } else if constexpr (PV8) {
           // d-major e4m3 V: the tile's first key is a multiple of 16 (segments start aligned)
           const int x0 = p.seg[vseg].start + voff;
           tma_load_3d(sV, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, x0, 0, vhead);
@@ -406,10 +447,30 @@ __global__ void __launch_bounds__(NTHREADS, 1)
           // K_t's stage held K_t-KST; S_t-2 complete means K_t-2 (and every older K) has been
           // read.  S_t cannot complete before K_t lands, so this barrier is never a phase ahead.
           if (t >= 2 && !mbar_wait(b.s_full0 + 8 * ((t - 2) & 1), ((t - 2) >> 1) & 1, wc, 1, t)) break;
-          const bool chunk = p.seg[kseg].src != 0;
-          mbar_arrive_expect_tx(b.k_full0 + 8 * ks, C::K_TILE);
-          tma_load_4d(sbase + C::OFF_K + ks * C::K_TILE, chunk ? &tm_kc : &tm_kr, b.k_full0 + 8 * ks, 0,
-                      p.seg[kseg].start + koff, 0, kh);
+          const bool chunk = p.seg[kseg].src == 1;
+          if (BLOCKS && p.seg[kseg].src == 2) {
+            if constexpr (BLOCKS) {
+              const AttnLists& l = p.lists;
+              const int32_t* list = l.ids + (static_cast<int64_t>(kh) * p.n_qt + kq) * l.top_k;
+#pragma unroll
+              for (int i = 0; i < 3; ++i) {
+                const Piece w = piece_of(l, list, 3 * (koff / BN) + i);
+                at[t & 1][i] = make_int2(w.frame, w.row);
+              }
+              mbar_arrive_expect_tx(b.k_full0 + 8 * ks, C::K_TILE);
+              constexpr int kCols = QK8 ? 1 : C::NBOX;   // boxes of 128 bytes across a key
+#pragma unroll
+              for (int i = 0; i < 3; ++i)
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                  tma_load_4d(sbase + C::OFF_K + ks * C::K_TILE + c * C::KBOX + i * kPiece * 128, &l.k,
+                              b.k_full0 + 8 * ks, 64 * c, at[t & 1][i].y, at[t & 1][i].x, kh);
+            }
+          } else {
+            mbar_arrive_expect_tx(b.k_full0 + 8 * ks, C::K_TILE);
+            tma_load_4d(sbase + C::OFF_K + ks * C::K_TILE, chunk ? &tm_kc : &tm_kr, b.k_full0 + 8 * ks, 0,
+                        p.seg[kseg].start + koff, 0, kh);
+          }
           tr(t, 6);
           ++t;
           if (++kj == req_at && req_at > 0) request();
@@ -650,7 +711,7 @@ __global__ void __launch_bounds__(NTHREADS, 1)
       float* x_sq = x_max + 2 * BM;   // [half][row]
       float sq = 0.f;
       if (live) {
-        const float inv = (PV8 ? p.v_scale[head] : 1.f) / l_row;
+        const float inv = BLOCKS && l_row == 0.f ? 0.f : (PV8 ? p.v_scale[head] : 1.f) / l_row;   // 0: no key
         const int c0 = half * C::O_HALF;
         __nv_bfloat16* drow = dst + static_cast<size_t>(qrow) * D + head * HD + c0;
         const __nv_bfloat16* lrow = p.out_loc + static_cast<size_t>(qrow) * D + head * HD + c0;
@@ -808,12 +869,30 @@ __global__ void __launch_bounds__(NTHREADS, 1)
         if (threadIdx.x == 0) tr(g, 0);
         if (lane == 0) tr(g, 24 + warp);
         int vloc = min(BN, p.seg[seg].count - off) - half * HALF_COLS;   // valid columns of this half
-        if (p.causal_p != 0 && p.seg[seg].src != 0) {
+        int first = 0, second = 0, cut = 0;   // listed blocks: valid columns of the half's two pieces, where they meet
+        bool whole = true;
+        if constexpr (BLOCKS) {
+          if (p.seg[seg].src == 2) {
+            // lane i < 3 looks up piece i; their counts side by side in one word
+            const AttnLists& l = p.lists;
+            const int32_t* list = l.ids + (static_cast<int64_t>(head) * p.n_qt + q_tile) * l.top_k;
+            uint32_t n = 0;
+            if (lane < 3) n = static_cast<uint32_t>(piece_of(l, list, 3 * (off / BN) + lane).count) << (8 * lane);
+            n = __reduce_or_sync(0xffffffffu, n);
+            vloc = BN;
+            const int c1 = n >> 8 & 255;
+            cut = half ? 32 : 64;
+            first = half ? c1 - 32 : n & 255;
+            second = cut + (half ? n >> 16 : c1);
+            whole = n == 0x404040u;
+          }
+        }
+        if (p.causal_p != 0 && p.seg[seg].src == 1) {
           // frame-causal chunk: this row sees chunk keys below the end of its own frame
           const int kc0 = p.seg[seg].start + off + half * HALF_COLS;   // chunk index of column 0
           vloc = min(vloc, (qrow / p.causal_p + 1) * p.causal_p - kc0);
         }
-        const float sl2 = p.seg[seg].src != 0 ? sl2_chunk : sl2_ring;
+        const float sl2 = p.seg[seg].src == 1 ? sl2_chunk : sl2_ring;
         const uint32_t scol = trow + C::COL_S0 + sb * BN + half * HALF_COLS;
         // load this half's scores (masked columns -inf)
         auto load_s = [&](uint32_t* s) {
@@ -826,6 +905,13 @@ __global__ void __launch_bounds__(NTHREADS, 1)
 #pragma unroll
             for (int i = 0; i < HALF_COLS; ++i)
               if (i >= vloc) s[i] = __float_as_uint(-INFINITY);
+          }
+          if constexpr (BLOCKS) {
+            if (!whole) {
+#pragma unroll
+              for (int i = 0; i < HALF_COLS; ++i)
+                if (i >= (i < cut ? first : second)) s[i] = __float_as_uint(-INFINITY);
+            }
           }
           if constexpr (PV8) {
             // keys before the run at the start of an aligned segment
@@ -852,7 +938,8 @@ __global__ void __launch_bounds__(NTHREADS, 1)
           // first tile: the row max comes from both halves
           float mo;
           ok = pair_exchange(mx, mo);
-          m_run = fmaxf(mx, mo) * sl2;
+          mo = fmaxf(mx, mo);
+          m_run = BLOCKS && mo == -INFINITY ? mo : mo * sl2;
         } else {
           // the running max stands unless the tile's max exceeds it by more than 2^8 somewhere in
           // the pair's rows (rare); then O is rescaled first
@@ -966,7 +1053,8 @@ __global__ void __launch_bounds__(NTHREADS, 1)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int i = 0; i < c; ++i) {
           // a CTA none of whose keys the row sees (frame-causal) has m = -inf and zeros
-          const float w = ex2_approx(cluster_ld1(cluster_map(xm, i)) - m);
+          // (and with listed blocks the row may have none anywhere)
+          const float w = ex2_approx(cluster_ld1(cluster_map(xm, i)) - (BLOCKS && m == -INFINITY ? 0.f : m));
           l = fmaf(w, cluster_ld1(cluster_map(xm + BM * 4, i)), l);
           const float4 v = cluster_ld4(cluster_map(xo, i));
           o.x = fmaf(w, v.x, o.x);
@@ -974,7 +1062,7 @@ __global__ void __launch_bounds__(NTHREADS, 1)
           o.z = fmaf(w, v.z, o.z);
           o.w = fmaf(w, v.w, o.w);
         }
-        const float inv = vs / l;
+        const float inv = BLOCKS && l == 0.f ? 0.f : vs / l;
         const size_t qrow = static_cast<size_t>(q_tile) * BM + r;
         if (lane < HD / 4)
           reinterpret_cast<uint2*>(p.out + (qrow * p.num_heads + head) * HD)[lane] =
@@ -1047,15 +1135,15 @@ static SplitPlan split_plan(int items, int n_tiles, int sms, F&& clusters) {
   return best;
 }
 
-template <int HD, bool QK8, bool TRACE = false, bool PV8 = false>
+template <int HD, bool QK8, bool TRACE = false, bool PV8 = false, typename Params>
 static cudaError_t launch_hd(const CUtensorMap* tq, const CUtensorMap* tkr, const CUtensorMap* tvr,
-                             const CUtensorMap* tkc, const CUtensorMap* tvc, AttnParams p, cudaStream_t s) {
+                             const CUtensorMap* tkc, const CUtensorMap* tvc, Params p, cudaStream_t s) {
   using C = Cfg<HD, QK8, PV8>;
-  const auto whole = attn_kernel<HD, QK8, PV8, TRACE, false>;
+  const auto whole = attn_kernel<HD, QK8, PV8, TRACE, false, Params>;
   // Not with 8-bit P V: its probabilities are rounded to e4m3 against the running maximum, and a
   // CTA's own maximum would round them otherwise (within the same bound, but 2.6 % of the output).
   // Not in the dual pass: its discrepancy is a difference of outputs and would move with them.
-  const auto split = attn_kernel<HD, QK8, false, TRACE, true>;
+  const auto split = attn_kernel<HD, QK8, false, TRACE, true, Params>;
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -1110,7 +1198,13 @@ static cudaError_t launch_hd(const CUtensorMap* tq, const CUtensorMap* tkr, cons
 
 cudaError_t launch_attention(int head_dim, const CUtensorMap* tq, const CUtensorMap* tkr,
                              const CUtensorMap* tvr, const CUtensorMap* tkc,
-                             const CUtensorMap* tvc, const AttnParams& p, cudaStream_t s) {
+                             const CUtensorMap* tvc, const AttnParams& p, cudaStream_t s, const AttnLists* lists) {
+  if (lists) {
+    const AttnBlocksParams b{p, *lists};
+    if (p.q_scale) return launch_hd<128, true>(tq, tkr, tvr, tkc, tvc, b, s);
+    if (head_dim == 128) return launch_hd<128, false>(tq, tkr, tvr, tkc, tvc, b, s);
+    return launch_hd<64, false>(tq, tkr, tvr, tkc, tvc, b, s);
+  }
   if (p.q_scale) {
     if (head_dim == 128 && p.v_scale) return launch_hd<128, true, false, true>(tq, tkr, tvr, tkc, tvc, p, s);
     if (head_dim == 128) return launch_hd<128, true>(tq, tkr, tvr, tkc, tvc, p, s);

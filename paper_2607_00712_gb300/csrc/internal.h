@@ -13,7 +13,8 @@ namespace ispa {
 
 // ------------------------------------------------------------ attention
 // One contiguous run of keys.  src 0 = the KV ring ([H][cap*P][d]), src 1 = the
-// chunk's own k_cur/v_cur ([n_q][H][d]).  start/count are token rows.
+// chunk's own k_cur/v_cur ([n_q][H][d]).  start/count are token rows.  src 2 (the last
+// segment of a call with lists) = the listed blocks: count = tiles * kAttnBN.
 struct AttnSeg {
   int32_t src;
   int32_t start;
@@ -59,6 +60,24 @@ struct AttnParams {
   const float* v_scale;
 };
 
+// Listed blocks (the *_blocks entry points): a list's blocks are cut into pieces of kPiece tokens, three to a
+// key tile.  The maps view the ring as (columns, tokens of a frame, frames, heads), so that what a piece's box
+// has behind its frame's last token arrives as zeros.
+constexpr int kPiece = 64;
+struct AttnLists {
+  CUtensorMap k, v;
+  const int32_t* ids;   // [H][query tiles][top_k]
+  int32_t top_k;
+  int32_t entries;      // of a list that are read
+  int32_t pieces;       // of a block
+  int32_t nb;           // blocks of a frame
+  int32_t n_ids;        // block numbers below this are resident
+  int32_t block, P;     // tokens of a block, of a frame
+};
+struct AttnBlocksParams : AttnParams {
+  AttnLists lists;
+};
+
 // Raise the dynamic shared-memory limit of `func` to `bytes` on the current device, once
 // per (device, kernel); safe to call from several host threads.
 cudaError_t set_smem_limit_once(const void* func, int bytes);
@@ -66,7 +85,8 @@ cudaError_t set_smem_limit_once(const void* func, int bytes);
 // Launch the attention kernel.  tensor maps are encoded by the caller.
 cudaError_t launch_attention(int head_dim, const CUtensorMap* tm_q, const CUtensorMap* tm_kr,
                              const CUtensorMap* tm_vr, const CUtensorMap* tm_kc,
-                             const CUtensorMap* tm_vc, const AttnParams& p, cudaStream_t s);
+                             const CUtensorMap* tm_vc, const AttnParams& p, cudaStream_t s,
+                             const AttnLists* lists = nullptr);
 // disc[t] = sqrt(sum_h part[h][t]); *disc_sq_sum += sum_t sum_h part[h][t]
 cudaError_t launch_disc_reduce(const float* part, int32_t H, int32_t n_q, float* disc,
                                float* disc_sq_sum, cudaStream_t s);
@@ -168,6 +188,18 @@ struct RopeParams {
   uint64_t wait_limit_ns;
 };
 cudaError_t launch_rope(const RopeParams& p, bool half, cudaStream_t s);
+// The same with the last tensor (the keys) going into a ring, and the values beside it.
+struct RopeAppendParams : RopeParams {
+  void* k_ring;                   // bf16, or e4m3 codes if k_scale: [H][ring_tok][head_dim]
+  const float* k_scale;           // [H]
+  const __nv_bfloat16* v;         // token t's heads at v + t * v_stride; null: the values are not copied here
+  int64_t v_stride;
+  __nv_bfloat16* v_ring;          // [H][ring_tok][head_dim]
+  int64_t ring_tok;               // capacity_frames * P
+  int32_t P;
+  int32_t slot[kMaxAppendFrames]; // ring slot of each frame
+};
+cudaError_t launch_rope_append(const RopeAppendParams& p, bool half, cudaStream_t s);
 // Turns per position of n_pairs pairs (64-bit fractions) and the factor on the rotated features; false: bad arguments.
 bool rope_steps(const ispa_rope_frequencies& f, int32_t n_pairs, uint64_t* steps, float* factor);
 
@@ -183,9 +215,40 @@ cudaError_t launch_quant_vt(const void* x, int64_t n, int32_t H, const float* sc
                             cudaStream_t s);
 // vt_scale: null (values copied as bf16), or the values' per-head scales: v_dst then takes d-major codes
 // of row stride vt_ld in the frames' slots (d = 128, P % 4 == 0).
+// Values alone, as d-major codes in the frames' slots; token t's heads at v + t * v_stride.
+cudaError_t launch_append_vt(const int32_t* slots, int32_t n_frames, int32_t P, int32_t H, const void* v,
+                             int64_t v_stride, void* v_dst, const float* vt_scale, int64_t vt_ld, cudaStream_t s);
 cudaError_t launch_append_qk8(const int32_t* slots, int32_t n_frames, int32_t P, int32_t H, int32_t d,
                               int64_t ring_tok, const void* k_src, const void* v_src, void* k_dst, void* v_dst,
                               const float* k_scale, const float* vt_scale, int64_t vt_ld, cudaStream_t s);
+
+// ------------------------------------------------------------ blocks of the history
+struct MeansParams {
+  const void* k;            // [H][capacity * P][d]
+  const float* k_scale;     // e4m3 codes, or null: bf16
+  float* means;             // [H][capacity * nb][d]
+  int64_t first_frame;      // logical
+  int32_t n_sink, capacity;
+  int32_t P, block, nb, H, d;
+  int64_t units;            // frames * nb
+};
+cudaError_t launch_key_means(const MeansParams& p, cudaStream_t s);
+
+constexpr int kSelectQueries = 128;   // that share a selection
+struct SelectParams {
+  const __nv_bfloat16* q;   // [n_q][H][d]
+  const float* means;       // [H][ids][d]
+  int32_t* blocks;          // [H][n_qt][top_k]
+  void* ws;
+  int32_t n_q, n_qt, H, d, top_k;
+  int64_t ids;              // capacity * nb
+  int32_t n_cand;           // candidates, numbered through the runs
+  int32_t n_runs;
+  int32_t run_end[ISPA_MAX_RANGES];     // candidates up to the end of the run
+  int32_t run_shift[ISPA_MAX_RANGES];   // block number - candidate
+};
+size_t select_ws_bytes(int64_t H, int64_t n_qt, int64_t d, int64_t ids);
+cudaError_t launch_select(const SelectParams& p, cudaStream_t s);
 
 // ------------------------------------------------------------ misc
 int* device_status_ptr();  // library status word in the current context (nullptr on error)

@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(256) quant_given_kernel(const uint4* __restric
 constexpr int VT_TOK = 128;
 struct QuantVtParams {
   const uint4* v;        // bf16 [n][H][128]
-  int64_t n;
+  int64_t n, row;        // tokens, 16-byte words from one token to the next
   int32_t H;
   const float* scale;    // [H]
   uint8_t* out;          // [H][128][ld]
@@ -208,7 +208,7 @@ __device__ __forceinline__ void quant_vt_block(const QuantVtParams& p, int64_t t
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       x[i][r] = make_uint4(0, 0, 0, 0);
-      if (4 * t4 + r < rows) x[i][r] = p.v[((t0 + 4 * t4 + r) * p.H + h) * 16 + c8];
+      if (4 * t4 + r < rows) x[i][r] = p.v[(t0 + 4 * t4 + r) * p.row + h * 16 + c8];
     }
   }
   const float inv = inv_of_scale(p.scale[h]);
@@ -338,6 +338,7 @@ static QuantVtParams vt_params(const void* x, int64_t n, int32_t H, const float*
   QuantVtParams p{};
   p.v = static_cast<const uint4*>(x);
   p.n = n;
+  p.row = static_cast<int64_t>(H) * 16;
   p.H = H;
   p.scale = scale;
   p.out = out;
@@ -375,6 +376,15 @@ cudaError_t launch_append_qk8(const int32_t* slots, int32_t n_frames, int32_t P,
   const dim3 grid(static_cast<unsigned>(kb + vb));
   return total < (int64_t{1} << 31) - 1024 ? launch_pdl(append_qk8_kernel<uint32_t>, grid, dim3(256), 0, s, p)
                                            : launch_pdl(append_qk8_kernel<int64_t>, grid, dim3(256), 0, s, p);
+}
+
+cudaError_t launch_append_vt(const int32_t* slots, int32_t n_frames, int32_t P, int32_t H, const void* v,
+                             int64_t v_stride, void* v_dst, const float* vt_scale, int64_t vt_ld, cudaStream_t s) {
+  const int64_t tokens = static_cast<int64_t>(n_frames) * P;
+  QuantVtParams p = vt_params(v, tokens, H, vt_scale, static_cast<uint8_t*>(v_dst), vt_ld, P, n_frames, slots);
+  p.row = v_stride / 8;
+  const dim3 grid(static_cast<unsigned>((tokens + VT_TOK - 1) / VT_TOK), static_cast<unsigned>(H));
+  return launch_pdl(quant_vt_kernel, grid, dim3(256), 0, s, p);
 }
 
 cudaError_t launch_quant_vt(const void* x, int64_t n, int32_t H, const float* scale, uint8_t* out, int64_t ld,

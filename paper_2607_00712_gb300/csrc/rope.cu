@@ -28,6 +28,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "forms.h"
 #include "internal.h"
@@ -90,6 +91,48 @@ struct Lane {
   }
 };
 
+// Ring: the kernel whose last tensor goes into a ring (RopeAppendParams).
+template <typename Params>
+constexpr bool kRing = !std::is_same_v<Params, RopeParams>;
+
+// A token's place in the ring: row of head 0.
+__device__ __forceinline__ int64_t ring_row(const RopeAppendParams& p, int64_t tok) {
+  const int f = static_cast<int>(tok / p.P);
+  return static_cast<int64_t>(p.slot[f]) * p.P + (tok - static_cast<int64_t>(f) * p.P);
+}
+// Eight features of head h to ring row `row`, as bf16 or as codes of f * (1 / scale).
+template <bool HALF>
+__device__ __forceinline__ void ring_store(const RopeAppendParams& p, const Lane<HALF>& ln, int64_t row, int h,
+                                           const float* f) {
+  const int64_t at = (static_cast<int64_t>(h) * p.ring_tok + row) * p.head_dim;
+  if (!p.k_scale) {
+    ln.store(static_cast<__nv_bfloat16*>(p.k_ring) + at, f);
+  } else {
+    const float inv = __fdiv_rn(1.f, __ldg(p.k_scale + h));
+    uint8_t* const head = static_cast<uint8_t*>(p.k_ring) + at;
+    *reinterpret_cast<uint32_t*>(head + ln.at0) = pack_e4m3x4(f, inv);
+    *reinterpret_cast<uint32_t*>(head + ln.at1) = pack_e4m3x4(f + 4, inv);
+  }
+}
+// A token's values, by `threads` threads of which this is number t.
+__device__ __forceinline__ void ring_values(const RopeAppendParams& p, int64_t tok, int64_t row, int heads, int t,
+                                            int threads) {
+  const int wph = p.head_dim / 8, words = heads * wph;
+  const uint4* from = reinterpret_cast<const uint4*>(p.v + tok * p.v_stride);
+  uint4* to = reinterpret_cast<uint4*>(p.v_ring) + row * wph;
+  for (int i0 = t; i0 < words; i0 += 4 * threads) {
+    uint4 w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * threads < words) w[u] = __ldcs(from + i0 + u * threads);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * threads;
+      if (i < words) to[i / wph * p.ring_tok * wph + i % wph] = w[u];
+    }
+  }
+}
+
 __device__ __forceinline__ float sum_squares(const uint4& w, float s) {
   float f[8];
   unpack8(w, f);
@@ -111,18 +154,28 @@ __device__ __forceinline__ int axis_of(int pair, const RopeParams& p) {
 
 // ------------------------------------------------------------ few rows
 // A block a row (a token's queries or keys); V: vectors a thread holds at once.  blockIdx.y: which of the two.
-template <int V, bool HALF>
-__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeParams p) {
+template <int V, bool HALF, typename Params>
+__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ Params p) {
   __shared__ float2 table[128];
   __shared__ float red[2][32];
   const int64_t tok = blockIdx.x;
-  const RopeRowsParams& o = p.rows[blockIdx.y];
+  const RopeRowsParams& o = p.rows[kRing<Params> ? min(static_cast<int>(blockIdx.y), p.n_rows - 1) : blockIdx.y];
   const int lph = p.lanes_per_head, d = p.head_dim;
   const Lane<HALF> ln(threadIdx.x, p);
   const int heads_step = blockDim.x / lph, head0 = threadIdx.x / lph;
   pdl_wait();
   pdl_trigger();
 
+  int64_t row = 0;       // ring row of the keys
+  bool keys = false;
+  if constexpr (kRing<Params>) {
+    row = ring_row(p, tok);
+    keys = static_cast<int>(blockIdx.y) == p.n_rows - 1;
+    if (static_cast<int>(blockIdx.y) == p.n_rows) {
+      ring_values(p, tok, row, p.rows[p.n_rows - 1].heads, threadIdx.x, blockDim.x);
+      return;
+    }
+  }
   const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(o.x) + tok * o.x_stride;
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride;
   uint4 raw[V];
@@ -161,7 +214,13 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeP
       for (int e = 0; e < 8; ++e) f[e] *= r * w[e];
     }
     ln.turn(f, cs);
-    if (ln.live && h < o.heads) ln.store(out + static_cast<int64_t>(h) * d, f);
+    if (ln.live && h < o.heads) {
+      if (kRing<Params> && keys) {
+        if constexpr (kRing<Params>) ring_store(p, ln, row, h, f);
+      } else {
+        ln.store(out + static_cast<int64_t>(h) * d, f);
+      }
+    }
   };
   // Every lane of a warp goes round alike (the head's sum needs all of them): the step counts from the first head.
 #pragma unroll
@@ -184,8 +243,8 @@ constexpr uint64_t R_DRAIN_NS = 200ull * 1000 * 1000;
 // weights of a norm over the token's heads stand there too, the eight of a lane in two planes, so that a warp reads
 // whole lines.  NORM: of queries and keys alike.  FULL: every feature turns and a head's lanes are a power of two.
 // STAGES: tokens of a team in shared memory, one where all of the block's tokens fit at once.
-template <bool HALF, int NORM, bool FULL, int STAGES>
-__global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_constant__ RopeParams p, int per_block) {
+template <bool HALF, int NORM, bool FULL, int STAGES, typename Params>
+__global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_constant__ Params p, int per_block) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int abort_word;
   const int t = threadIdx.x, threads = blockDim.x, teams = blockDim.y, d = p.head_dim, lph = p.lanes_per_head;
@@ -272,8 +331,11 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   };
   // norm, rotation and way out of a tensor; cs: the pairs' cosines and sines, with 1 / root of a norm over the token in
   // them, r that factor for what passes
-  auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs,
-                    float r) {
+  auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs, float r,
+                    bool keys) {
+    int64_t row = 0;
+    if constexpr (kRing<Params>)
+      if (keys) row = ring_row(p, tok);
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride + head0 * d;
     const float4* wp = planes + head0 * vecs + ln.c;
@@ -319,7 +381,12 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
           f[b] *= r;
         }
       }
-      if (here) ln.store(out, f);
+      if (kRing<Params> && keys) {
+        if constexpr (kRing<Params>)
+          if (here) ring_store(p, ln, row, h, f);
+      } else {
+        if (here) ln.store(out, f);
+      }
       h += heads_step;
       x += heads_step * d;
       out += heads_step * d;
@@ -363,12 +430,14 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
         c1[j] = make_float2(cs[j].x * r0, cs[j].y * r0);
         cs[j] = make_float2(cs[j].x * r1, cs[j].y * r1);
       }
-      finish(src, p.rows[0], reinterpret_cast<const float4*>(smem), n0, c1, r0);
-      if (n1) finish(src + 2 * n0, p.rows[1], reinterpret_cast<const float4*>(smem + 4 * n0), n1, cs, r1);
+      finish(src, p.rows[0], reinterpret_cast<const float4*>(smem), n0, c1, r0, n1 == 0);
+      if (n1) finish(src + 2 * n0, p.rows[1], reinterpret_cast<const float4*>(smem + 4 * n0), n1, cs, r1, true);
     } else {
-      finish(src, p.rows[0], nullptr, n0, cs, 1.f);
-      if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f);
+      finish(src, p.rows[0], nullptr, n0, cs, 1.f, n1 == 0);
+      if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f, true);
     }
+    if constexpr (kRing<Params>)
+      if (p.v) ring_values(p, tok, ring_row(p, tok), p.rows[p.n_rows - 1].heads, t, threads);
     tm.sync();   // the token's stage and the table are free
     if (STAGES == 1 && t == 0 && ok && last - tok > teams) fetch(tok + teams, stage_of(issued++));
   }
@@ -377,8 +446,8 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
       mbar_wait_drain(full + 8 * stage_of(i), parity_of(i), R_DRAIN_NS);
 }
 
-template <bool HALF>
-cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
+template <bool HALF, typename Params>
+cudaError_t launch_layout(const Params& p, int sms, cudaStream_t s) {
   const int32_t heads[2] = {p.rows[0].heads, p.rows[1].heads}, norms[2] = {p.rows[0].norm, p.rows[1].norm};
   const RopeForm f = rope_form(p.n, p.n_rows, heads, norms, p.head_dim, p.pairs, p.lanes_per_head, HALF, sms);
   if (f.stream) {
@@ -390,31 +459,40 @@ cudaError_t launch_layout(const RopeParams& p, int sms, cudaStream_t s) {
     };
     const auto pick = [&](auto one, auto two) { return f.stages == 1 ? go(one) : go(two); };
     if (norms[0] == ISPA_QK_NORM_TOKEN)
-      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 1>,
-                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 2>)
-                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 1>,
-                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 2>);
+      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 1, Params>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, true, 2, Params>)
+                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 1, Params>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_TOKEN, false, 2, Params>);
     if (norms[0] == ISPA_QK_NORM_HEAD)
-      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 1>,
-                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 2>)
-                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 1>,
-                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 2>);
-    return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 1>,
-                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 2>)
-                  : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 1>,
-                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 2>);
+      return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 1, Params>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, true, 2, Params>)
+                    : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 1, Params>,
+                           rope_stream_kernel<HALF, ISPA_QK_NORM_HEAD, false, 2, Params>);
+    return f.full ? pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 1, Params>,
+                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, true, 2, Params>)
+                  : pick(rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 1, Params>,
+                         rope_stream_kernel<HALF, ISPA_QK_NORM_NONE, false, 2, Params>);
   }
   const auto go = [&](auto kernel) {
-    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), p.n_rows), dim3(32 * f.warps), 0, s, p);
+    int parts = p.n_rows;
+    if constexpr (kRing<Params>) parts += p.v != nullptr;
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(p.n), parts), dim3(32 * f.warps), 0, s, p);
   };
-  return f.vectors == 1   ? go(rope_kernel<1, HALF>)
-         : f.vectors == 2 ? go(rope_kernel<2, HALF>)
-                          : go(rope_kernel<4, HALF>);
+  return f.vectors == 1   ? go(rope_kernel<1, HALF, Params>)
+         : f.vectors == 2 ? go(rope_kernel<2, HALF, Params>)
+                          : go(rope_kernel<4, HALF, Params>);
 }
 
 }  // namespace
 
 cudaError_t launch_rope(const RopeParams& p, bool half, cudaStream_t s) {
+  int dev = 0, sms = 152;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return half ? launch_layout<true>(p, sms, s) : launch_layout<false>(p, sms, s);
+}
+
+cudaError_t launch_rope_append(const RopeAppendParams& p, bool half, cudaStream_t s) {
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
