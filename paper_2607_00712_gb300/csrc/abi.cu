@@ -471,6 +471,9 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
     lists.n_ids = static_cast<int32_t>(std::min<int64_t>(ring->frames_written, ring->capacity_frames)) * lists.nb;
     lists.entries = std::min(lists.top_k, lists.n_ids);
     lists.pieces = (std::min(blocks->block, P) + kPiece - 1) / kPiece;
+    lists.by_nb = divisor(lists.nb);
+    lists.by_pieces = divisor(lists.pieces);
+    lists.first_tile = tiles;
     // at most ring tokens / 64 + blocks pieces: as tiles of 192 keys below 2^31
     const int64_t n = (static_cast<int64_t>(lists.entries) * lists.pieces + 2) / 3;
     if ((n + tiles) * bn > INT32_MAX) return ISPA_ERR_UNSUPPORTED;

@@ -197,29 +197,33 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Piece u of a list: its frame's slot, its first token in the frame (P where the piece does not exist: a box there
-// arrives as zeros) and how many tokens it has.
+__device__ __forceinline__ int quotient(int x, const Divisor& d) {
+  return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(x)) * d.m >> d.s);
+}
+// A piece (tokens `first` on of block `id`, a multiple of kPiece): its frame (slot), its first token in the frame (P
+// where the piece does not exist: a box there arrives as zeros) and how many tokens it has.
 struct Piece {
   int frame, row, count;
 };
-__device__ __forceinline__ Piece piece_of(const AttnLists& l, const int32_t* list, int u) {
+__device__ __forceinline__ Piece piece_of(const AttnLists& l, int id, int first) {
   Piece r{0, l.P, 0};
-  const int e = u / l.pieces;
-  if (e < l.entries) {
-    const int id = __ldg(list + e);
-    if (id >= 0 && id < l.n_ids) {
-      r.frame = id / l.nb;
-      r.row = (id - r.frame * l.nb) * l.block + kPiece * (u - e * l.pieces);
-      r.count = max(0, min(kPiece, l.P - r.row));
-    }
+  if (static_cast<uint32_t>(id) < static_cast<uint32_t>(l.n_ids)) {
+    r.frame = quotient(id, l.by_nb);
+    r.row = (id - r.frame * l.nb) * l.block + first;
+    r.count = max(0, min(kPiece, l.P - r.row));
   }
   return r;
 }
+__device__ __forceinline__ int dense_tiles(const AttnParams& p) { return p.n_tiles; }
+__device__ __forceinline__ int dense_tiles(const AttnBlocksParams& p) { return p.lists.first_tile; }
 
 }  // namespace
 
-// Params = AttnBlocksParams (BLOCKS): the instances for listed blocks.  Their tiles come after the dense segments' as three boxes of 64
-// tokens each, so that a 64-token block costs a third of a tile wherever it lies.
+// Params = AttnBlocksParams (BLOCKS): the instances for listed blocks.  Their tiles come after the dense segments', as
+// three pieces of 64 tokens each, so that a 64-token block costs a third of a tile wherever it lies.  A piece's K and V
+// come in one box per 128 bytes of a row, into the dense tiles' layout.  (One box a piece for both column blocks, with
+// the layout that it leaves and other descriptors for it, took 9 % longer: what the descriptors cost the issuing
+// thread.  Boxes of L2 prefetch three tiles ahead took 25 % longer.)
 //
 // SPLIT: the instance for items that leave SMs idle (see split_plan).  A cluster works on one item:
 // rank r of c visits the key tiles [n r / c, n (r + 1) / c), and at the end each CTA leaves its
@@ -350,6 +354,7 @@ __global__ void __launch_bounds__(NTHREADS, 1)
     for (int n; skip >= (n = (p.seg[seg0].count + BN - 1) / BN); ++seg0) skip -= n;
     off0 = skip * BN;
   }
+  const int n_dense = dense_tiles(p) - tile0;   // tiles of this CTA's share of an item before listed ones
   // tile events of the CTA's first item (global tile index = item tile index there)
   auto tr = [&](int g, int ev) {
     if constexpr (TRACE) {
@@ -390,10 +395,47 @@ __global__ void __launch_bounds__(NTHREADS, 1)
       int vk = 0, vj = 0, vseg = seg0, voff = off0;   // V cursor
       int t = 0, tv = 0;                        // global K and V tiles issued
       bool k_live = true, ok = true;
-      // listed blocks: where the pieces of the K cursor's last two tiles lie, for their values (V trails K by at most
-      // one tile)
-      int2 at[2][3] = {};
+      // Listed blocks: where the K cursor's tile lies (`at`: frame, token), and for their values (V trails K by at most
+      // one tile) the last two listed tiles issued; the numbers of the tile after the K cursor's.  All of it is ready
+      // when a stage gets free, but for the first list tile of an item without dense ones.
+      int2 at[3] = {}, last[3] = {}, before[3] = {};
+      int ids[3] = {}, in_block[3] = {};        // numbers, first tokens in their blocks
+      const int32_t* list = nullptr;
+      int entry = 0, sub = 0;                   // of the list: the next piece to be looked up
+      auto send_ids = [&]() {
+        if constexpr (BLOCKS) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) {
+            ids[i] = entry < p.lists.entries ? __ldg(list + entry) : -1;
+            in_block[i] = kPiece * sub;
+            if (++sub == p.lists.pieces) {
+              sub = 0;
+              ++entry;
+            }
+          }
+        }
+      };
+      auto locate = [&](bool start) {   // for the K cursor's tile, and on the way for the one after it
+        if constexpr (BLOCKS) {
+          const int j = kj - n_dense;
+          if (start) {
+            list = p.lists.ids + (static_cast<int64_t>(kh) * p.n_qt + kq) * p.lists.top_k;
+            entry = quotient(3 * max(j, 0), p.lists.by_pieces);
+            sub = 3 * max(j, 0) - entry * p.lists.pieces;
+            if (j >= 0) send_ids();
+          }
+          if (j >= 0) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              const Piece w = piece_of(p.lists, ids[i], in_block[i]);
+              at[i] = make_int2(w.frame, w.row);
+            }
+          }
+          if (j >= -1) send_ids();
+        }
+      };
       load_q();
+      locate(true);
       if (req_at == 0) request();
       // Loads are issued in the order their stages free up: inside an item the UMMA stream is
       // S_0 S_1 PV_0 S_2 PV_1 S_3 ..., so K_t goes out once S_t-2 has completed and V_t-1 once
@@ -405,14 +447,16 @@ __global__ void __launch_bounds__(NTHREADS, 1)
         mbar_arrive_expect_tx(b.v_full0 + 8 * vs, C::V_TILE);
         const uint32_t sV = sbase + C::OFF_V + vs * C::V_TILE;
         const int vhead = vk == kk ? kh : prev_h;
-        if (BLOCKS && p.seg[vseg].src == 2) {
+        if (BLOCKS && vj >= n_dense) {
           if constexpr (BLOCKS) {
 #pragma unroll
-            for (int i = 0; i < 3; ++i)
+            for (int i = 0; i < 3; ++i) {
+              const int2 w = tv == t - 1 ? last[i] : before[i];
 #pragma unroll
               for (int c = 0; c < C::NBOX; ++c)
-                tma_load_4d(sV + c * C::KBOX + i * kPiece * 128, &p.lists.v, b.v_full0 + 8 * vs, 64 * c,
-                            at[tv & 1][i].y, at[tv & 1][i].x, vhead);
+                tma_load_4d(sV + c * C::KBOX + i * kPiece * 128, &p.lists.v, b.v_full0 + 8 * vs, 64 * c, w.y, w.x,
+                            vhead);
+            }
           }
         } else if constexpr (PV8) {
           // d-major e4m3 V: the tile's first key is a multiple of 16 (segments start aligned)
@@ -448,23 +492,21 @@ __global__ void __launch_bounds__(NTHREADS, 1)
           // read.  S_t cannot complete before K_t lands, so this barrier is never a phase ahead.
           if (t >= 2 && !mbar_wait(b.s_full0 + 8 * ((t - 2) & 1), ((t - 2) >> 1) & 1, wc, 1, t)) break;
           const bool chunk = p.seg[kseg].src == 1;
-          if (BLOCKS && p.seg[kseg].src == 2) {
+          if (BLOCKS && kj >= n_dense) {
             if constexpr (BLOCKS) {
-              const AttnLists& l = p.lists;
-              const int32_t* list = l.ids + (static_cast<int64_t>(kh) * p.n_qt + kq) * l.top_k;
 #pragma unroll
               for (int i = 0; i < 3; ++i) {
-                const Piece w = piece_of(l, list, 3 * (koff / BN) + i);
-                at[t & 1][i] = make_int2(w.frame, w.row);
+                before[i] = last[i];
+                last[i] = at[i];
               }
               mbar_arrive_expect_tx(b.k_full0 + 8 * ks, C::K_TILE);
-              constexpr int kCols = QK8 ? 1 : C::NBOX;   // boxes of 128 bytes across a key
+              const uint32_t sK = sbase + C::OFF_K + ks * C::K_TILE, bar = b.k_full0 + 8 * ks;
 #pragma unroll
-              for (int i = 0; i < 3; ++i)
+              for (int i = 0; i < 3; ++i) {
 #pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                  tma_load_4d(sbase + C::OFF_K + ks * C::K_TILE + c * C::KBOX + i * kPiece * 128, &l.k,
-                              b.k_full0 + 8 * ks, 64 * c, at[t & 1][i].y, at[t & 1][i].x, kh);
+                for (int c = 0; c < (QK8 ? 1 : C::NBOX); ++c)   // boxes of 128 bytes across a key
+                  tma_load_4d(sK + c * C::KBOX + i * kPiece * 128, &p.lists.k, bar, 64 * c, at[i].y, at[i].x, kh);
+              }
             }
           } else {
             mbar_arrive_expect_tx(b.k_full0 + 8 * ks, C::K_TILE);
@@ -506,6 +548,8 @@ __global__ void __launch_bounds__(NTHREADS, 1)
           } else {
             next_tile(p, kseg, koff);
           }
+          // between the tile's keys and the last one's values: behind both it would stand in the way of the next keys
+          if (BLOCKS && k_live) locate(kj == 0);
         }
         if (tv < t - (k_live ? 1 : 0)) {
           if (!issue_v()) break;
@@ -855,138 +899,173 @@ __global__ void __launch_bounds__(NTHREADS, 1)
       l_run = 0.f;
       seg = seg0;
       off = off0;
-      for (int j = 0; j < n_tiles; ++j) {
-        const int g = base + j;
-        const int sb = g & 1;
-        if (!SPLIT && p.dual && j == p.n_local_tiles && j > 0) {
-          // A_loc snapshot: O and l hold exactly the local tiles 0..j-1.
-          const float l_loc = row_l();
-          if (ok) ok = wait_o(g - 1, 7);
-          if (ok) tc_fence_after();
-          emit(ok, l_loc, p.out_loc, p.lse_loc, false);
-        }
-        if (ok) ok = warp_ok(mbar_wait(b.s_full0 + 8 * sb, (g >> 1) & 1, wc, 8, g));
-        if (threadIdx.x == 0) tr(g, 0);
-        if (lane == 0) tr(g, 24 + warp);
-        int vloc = min(BN, p.seg[seg].count - off) - half * HALF_COLS;   // valid columns of this half
-        int first = 0, second = 0, cut = 0;   // listed blocks: valid columns of the half's two pieces, where they meet
-        bool whole = true;
-        if constexpr (BLOCKS) {
-          if (p.seg[seg].src == 2) {
-            // lane i < 3 looks up piece i; their counts side by side in one word
-            const AttnLists& l = p.lists;
-            const int32_t* list = l.ids + (static_cast<int64_t>(head) * p.n_qt + q_tile) * l.top_k;
-            uint32_t n = 0;
-            if (lane < 3) n = static_cast<uint32_t>(piece_of(l, list, 3 * (off / BN) + lane).count) << (8 * lane);
-            n = __reduce_or_sync(0xffffffffu, n);
-            vloc = BN;
-            const int c1 = n >> 8 & 255;
-            cut = half ? 32 : 64;
-            first = half ? c1 - 32 : n & 255;
-            second = cut + (half ? n >> 16 : c1);
-            whole = n == 0x404040u;
-          }
-        }
-        if (p.causal_p != 0 && p.seg[seg].src == 1) {
-          // frame-causal chunk: this row sees chunk keys below the end of its own frame
-          const int kc0 = p.seg[seg].start + off + half * HALF_COLS;   // chunk index of column 0
-          vloc = min(vloc, (qrow / p.causal_p + 1) * p.causal_p - kc0);
-        }
-        const float sl2 = p.seg[seg].src == 1 ? sl2_chunk : sl2_ring;
-        const uint32_t scol = trow + C::COL_S0 + sb * BN + half * HALF_COLS;
-        // load this half's scores (masked columns -inf)
-        auto load_s = [&](uint32_t* s) {
-          tc_fence_after();
+      // Once for dense tiles and once for listed ones: with what listed tiles need in the same loop, every tile of a
+      // call took 10 to 18 % longer.
 #pragma unroll
-          for (int i = 0; i < HALF_COLS / 8; ++i) tmem_ld8(scol + 8 * i, s + 8 * i);
-#pragma unroll
-          for (int i = 0; i < HALF_COLS / 8; ++i) tmem_wait_ld8(s + 8 * i);
-          if (vloc < HALF_COLS) {
-#pragma unroll
-            for (int i = 0; i < HALF_COLS; ++i)
-              if (i >= vloc) s[i] = __float_as_uint(-INFINITY);
-          }
+      for (int part = 0; part < (BLOCKS ? 2 : 1); ++part) {
+        const bool listed = BLOCKS && part == 1;
+        int count = 0, list_at = 30;   // listed blocks: tokens of a piece (a lane's), the tile's first lane
+        uint32_t whole_pieces = 0;     // lanes whose piece is whole
+        int number = -1, in_block = 0; // of this lane's piece in the ten tiles that come next
+        auto look_up = [&](int u) {
           if constexpr (BLOCKS) {
-            if (!whole) {
-#pragma unroll
-              for (int i = 0; i < HALF_COLS; ++i)
-                if (i >= (i < cut ? first : second)) s[i] = __float_as_uint(-INFINITY);
-            }
-          }
-          if constexpr (PV8) {
-            // keys before the run at the start of an aligned segment
-            const int vfirst = (off == 0 ? p.seg[seg].skip : 0) - half * HALF_COLS;
-            if (vfirst > 0) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (i < vfirst) s[i] = __float_as_uint(-INFINITY);
-            }
+            const int e = quotient(u, p.lists.by_pieces);
+            in_block = kPiece * (u - e * p.lists.pieces);
+            number = e < p.lists.entries
+                         ? __ldg(p.lists.ids + (static_cast<int64_t>(head) * p.n_qt + q_tile) * p.lists.top_k + e)
+                         : -1;
           }
         };
-        // P_j overwrites the first 96 columns of S_j (this half's 48 packed columns), so both
-        // halves of the pair must have read their scores first: the pair barrier below orders it.
-        const uint32_t pcol = trow + C::COL_S0 + sb * BN + half * P_HALF;
-        uint32_t s[HALF_COLS];
-        float mx = -INFINITY;
-        if (ok) {
-          load_s(s);
-          if (threadIdx.x == 0) tr(g, 8);
-          mx = raw_max(s);
-        }
-        if (threadIdx.x == 0) tr(g, 9);
-        if (j == 0) {
-          // first tile: the row max comes from both halves
-          float mo;
-          ok = pair_exchange(mx, mo);
-          mo = fmaxf(mx, mo);
-          m_run = BLOCKS && mo == -INFINITY ? mo : mo * sl2;
-        } else {
-          // the running max stands unless the tile's max exceeds it by more than 2^8 somewhere in
-          // the pair's rows (rare); then O is rescaled first
-          const bool need = ok && mx * sl2 > m_run + C::RESCALE;
-          if (pair_or(pair_id, need || !ok)) {
-            float mo;
-            ok = pair_exchange(mx, mo);
-            // O holds PV of tiles 0..j-1 once PV_j-1 has completed; lanes whose max did not grow
-            // keep alpha = 1.
-            if (ok) ok = wait_o(g - 1, 9);
-            if (ok) {
-              tc_fence_after();
-              const float m_new = fmaxf(m_run, fmaxf(mx, mo) * sl2);
-              const float alpha = m_new == m_run ? 1.f : ex2_approx(m_run - m_new);
-              l_run *= alpha;
-#pragma unroll 1
-              for (int c = 0; c < C::O_HALF / 8; ++c) {
-                uint32_t r[8];
-                const uint32_t ocol = trow + C::COL_O + half * C::O_HALF + 8 * c;
-                tmem_ld8(ocol, r);
-                tmem_wait_ld8(r);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                tmem_st4(ocol, r);
-                tmem_st4(ocol + 4, r + 4);
+        if (listed) look_up(3 * max(0, -n_dense) + lane);
+        const int j_end = BLOCKS && part == 0 ? min(n_dense, n_tiles) : n_tiles;
+        for (int j = part == 0 ? 0 : max(0, n_dense); j < j_end; ++j) {
+          const int g = base + j;
+          const int sb = g & 1;
+          if (!SPLIT && p.dual && j == p.n_local_tiles && j > 0) {
+            // A_loc snapshot: O and l hold exactly the local tiles 0..j-1.
+            const float l_loc = row_l();
+            if (ok) ok = wait_o(g - 1, 7);
+            if (ok) tc_fence_after();
+            emit(ok, l_loc, p.out_loc, p.lse_loc, false);
+          }
+          if constexpr (BLOCKS) {
+            if (listed) {
+              if (list_at >= 30) {   // lane i < 30 has a piece of this tile and the next nine
+                count = lane < 30 ? piece_of(p.lists, number, in_block).count : 0;
+                whole_pieces = __ballot_sync(0xffffffffu, count == kPiece);
+                list_at = 0;
+                look_up(3 * (j - n_dense) + 30 + lane);
               }
-              tmem_wait_st();
-              m_run = m_new;
             }
           }
-        }
-        if (threadIdx.x == 0) tr(g, 1);
-        if (ok) {
-          if constexpr (PV8) {
-            // e4m3 P: this half's 96 keys are 24 columns of S_j's buffer
-            l_run += exps_store8(s, sl2, m_run, trow + C::COL_S0 + sb * BN + 24 * half);
-          } else {
-            l_run += exps_store(s, sl2, m_run, pcol);
+          if (ok) ok = warp_ok(mbar_wait(b.s_full0 + 8 * sb, (g >> 1) & 1, wc, 8, g));
+          if (threadIdx.x == 0) tr(g, 0);
+          if (lane == 0) tr(g, 24 + warp);
+          int vloc = min(BN, p.seg[seg].count - off) - half * HALF_COLS;   // valid columns of this half
+          if (!listed && p.causal_p != 0 && p.seg[seg].src == 1) {
+            // frame-causal chunk: this row sees chunk keys below the end of its own frame
+            const int kc0 = p.seg[seg].start + off + half * HALF_COLS;   // chunk index of column 0
+            vloc = min(vloc, (qrow / p.causal_p + 1) * p.causal_p - kc0);
           }
-          if (threadIdx.x == 0) tr(g, 10);
-          tmem_wait_st();
-          tc_fence_before();
-          mbar_arrive(b.p_full0 + 8 * sb);
-          if (threadIdx.x == 0) tr(g, 2);
-          if (lane == 0) tr(g, 16 + warp);
+          const float sl2 = !listed && p.seg[seg].src == 1 ? sl2_chunk : sl2_ring;
+          const uint32_t scol = trow + C::COL_S0 + sb * BN + half * HALF_COLS;
+          // load this half's scores (masked columns -inf)
+          auto load_s = [&](uint32_t* s) {
+            tc_fence_after();
+#pragma unroll
+            for (int i = 0; i < HALF_COLS / 8; ++i) tmem_ld8(scol + 8 * i, s + 8 * i);
+#pragma unroll
+            for (int i = 0; i < HALF_COLS / 8; ++i) tmem_wait_ld8(s + 8 * i);
+            if (vloc < HALF_COLS) {
+#pragma unroll
+              for (int i = 0; i < HALF_COLS; ++i)
+                if (i >= vloc) s[i] = __float_as_uint(-INFINITY);
+            }
+            if constexpr (PV8) {
+              // keys before the run at the start of an aligned segment
+              const int vfirst = (off == 0 ? p.seg[seg].skip : 0) - half * HALF_COLS;
+              if (vfirst > 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                  if (i < vfirst) s[i] = __float_as_uint(-INFINITY);
+              }
+            }
+          };
+          // P_j overwrites the first 96 columns of S_j (this half's 48 packed columns), so both
+          // halves of the pair must have read their scores first: the pair barrier below orders it.
+          const uint32_t pcol = trow + C::COL_S0 + sb * BN + half * P_HALF;
+          uint32_t s[HALF_COLS];
+          float mx = -INFINITY;
+          if constexpr (BLOCKS) {
+            if (ok && listed) {
+              // A tile with a piece that is not whole, or none: its columns are masked where they lie, in TMEM, so that
+              // the other tiles have nothing to do with it.
+              if ((whole_pieces >> list_at & 7) != 7) {
+                const int c0 = __shfl_sync(0xffffffffu, count, list_at);
+                const int c1 = __shfl_sync(0xffffffffu, count, list_at + 1);
+                const int c2 = __shfl_sync(0xffffffffu, count, list_at + 2);
+                tc_fence_after();
+#pragma unroll 1
+                for (int i = 0; i < HALF_COLS; i += 8) {   // eight columns of one piece
+                  const int at = half * HALF_COLS + i, n = (at < 64 ? c0 : at < 128 ? c1 : c2) - (at & 63);
+                  if (n >= 8) continue;
+                  uint32_t r[8];
+                  tmem_ld8(scol + i, r);
+                  tmem_wait_ld8(r);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e)
+                    if (e >= n) r[e] = __float_as_uint(-INFINITY);
+                  tmem_st4(scol + i, r);
+                  tmem_st4(scol + i + 4, r + 4);
+                }
+                tmem_wait_st();
+              }
+            }
+            if (listed) {
+              list_at += 3;
+              vloc = BN;
+            }
+          }
+          if (ok) {
+            load_s(s);
+            if (threadIdx.x == 0) tr(g, 8);
+            mx = raw_max(s);
+          }
+          if (threadIdx.x == 0) tr(g, 9);
+          if (j == 0) {
+            // first tile: the row max comes from both halves
+            float mo;
+            ok = pair_exchange(mx, mo);
+            mo = fmaxf(mx, mo);
+            m_run = BLOCKS && mo == -INFINITY ? mo : mo * sl2;
+          } else {
+            // the running max stands unless the tile's max exceeds it by more than 2^8 somewhere in
+            // the pair's rows (rare); then O is rescaled first
+            const bool need = ok && mx * sl2 > m_run + C::RESCALE;
+            if (pair_or(pair_id, need || !ok)) {
+              float mo;
+              ok = pair_exchange(mx, mo);
+              // O holds PV of tiles 0..j-1 once PV_j-1 has completed; lanes whose max did not grow
+              // keep alpha = 1.
+              if (ok) ok = wait_o(g - 1, 9);
+              if (ok) {
+                tc_fence_after();
+                const float m_new = fmaxf(m_run, fmaxf(mx, mo) * sl2);
+                const float alpha = m_new == m_run ? 1.f : ex2_approx(m_run - m_new);
+                l_run *= alpha;
+#pragma unroll 1
+                for (int c = 0; c < C::O_HALF / 8; ++c) {
+                  uint32_t r[8];
+                  const uint32_t ocol = trow + C::COL_O + half * C::O_HALF + 8 * c;
+                  tmem_ld8(ocol, r);
+                  tmem_wait_ld8(r);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                  tmem_st4(ocol, r);
+                  tmem_st4(ocol + 4, r + 4);
+                }
+                tmem_wait_st();
+                m_run = m_new;
+              }
+            }
+          }
+          if (threadIdx.x == 0) tr(g, 1);
+          if (ok) {
+            if constexpr (PV8) {
+              // e4m3 P: this half's 96 keys are 24 columns of S_j's buffer
+              l_run += exps_store8(s, sl2, m_run, trow + C::COL_S0 + sb * BN + 24 * half);
+            } else {
+              l_run += exps_store(s, sl2, m_run, pcol);
+            }
+            if (threadIdx.x == 0) tr(g, 10);
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(b.p_full0 + 8 * sb);
+            if (threadIdx.x == 0) tr(g, 2);
+            if (lane == 0) tr(g, 16 + warp);
+          }
+          if (!listed) next_tile(p, seg, off);
         }
-        next_tile(p, seg, off);
       }
       {
         const float l_row = row_l();   // overlaps the last P V

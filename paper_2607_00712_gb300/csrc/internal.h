@@ -64,6 +64,16 @@ struct AttnParams {
 // key tile.  The maps view the ring as (columns, tokens of a frame, frames, heads), so that what a piece's box
 // has behind its frame's last token arrives as zeros.
 constexpr int kPiece = 64;
+// x / n = x m >> s for 0 <= x < 2^31: with 2^k >= n, s = 31 + k and m = ceil(2^s / n), x m / 2^s exceeds x / n by less
+// than 2^31 n / (2^s n) <= 1 / n.
+struct Divisor {
+  uint32_t m, s;
+};
+inline Divisor divisor(int32_t n) {
+  uint32_t k = 0;
+  while ((int64_t{1} << k) < n) ++k;
+  return {static_cast<uint32_t>(((uint64_t{1} << (31 + k)) + n - 1) / n), 31 + k};
+}
 struct AttnLists {
   CUtensorMap k, v;
   const int32_t* ids;   // [H][query tiles][top_k]
@@ -73,6 +83,8 @@ struct AttnLists {
   int32_t nb;           // blocks of a frame
   int32_t n_ids;        // block numbers below this are resident
   int32_t block, P;     // tokens of a block, of a frame
+  int32_t first_tile;   // key tiles before the lists'
+  Divisor by_nb, by_pieces;
 };
 struct AttnBlocksParams : AttnParams {
   AttnLists lists;
