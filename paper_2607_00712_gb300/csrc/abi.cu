@@ -627,7 +627,7 @@ ispa_status norm_params(NormParams& p, const void* x, int32_t x_type, int64_t ro
   return p.status ? ISPA_OK : ISPA_ERR_CUDA;
 }
 
-// Checks and parameters of the rotary entry points.  to_ring: the last of the rows has no `out`.
+// Checks and parameters of the rotary entry points.  to_ring: the first of the rows has no `out`.
 ispa_status rope_params(RopeParams& p, const ispa_rope* rope, const ispa_rope_rows* rows, int32_t n_rows,
                         const int32_t* pos, int64_t pos0, int64_t n, bool to_ring) {
   if (!rope || !rows || !rope->steps || !pos || n_rows < 1 || n_rows > 2 || n <= 0 || rope->n_axes < 1 ||
@@ -643,7 +643,7 @@ ispa_status rope_params(RopeParams& p, const ispa_rope* rope, const ispa_rope_ro
   if (pairs < 1) return ISPA_ERR_INVALID_ARG;
   for (int i = 0; i < n_rows; ++i) {
     const ispa_rope_rows& r = rows[i];
-    const bool ring_row = to_ring && i == n_rows - 1;
+    const bool ring_row = to_ring && i == 0;
     if (!aligned16(r.x) || (!ring_row && !aligned16(r.out)) || (ring_row && (r.out || r.out_stride)) ||
         r.heads <= 0 || r.norm < ISPA_QK_NORM_NONE || r.norm > ISPA_QK_NORM_TOKEN)
       return ISPA_ERR_INVALID_ARG;
@@ -1065,7 +1065,7 @@ ispa_status ispa_kv_append_rope(ispa_kv_ring* ring, const ispa_rope* rope, const
     return ISPA_ERR_INVALID_ARG;
   if (n_frames > kMaxAppendFrames || n_frames > ring->capacity_frames - ring->n_sink_frames) return ISPA_ERR_CAPACITY;
   if (H > 65535) return ISPA_ERR_UNSUPPORTED;
-  ispa_rope_rows rows[2] = {q ? *q : *k, *k};
+  const ispa_rope_rows rows[2] = {*k, q ? *q : *k};
   RopeAppendParams p = {};
   st = rope_params(p, rope, rows, q ? 2 : 1, pos, pos0, static_cast<int64_t>(n_frames) * P, true);
   if (st != ISPA_OK) return st;
@@ -1076,6 +1076,8 @@ ispa_status ispa_kv_append_rope(ispa_kv_ring* ring, const ispa_rope* rope, const
   p.v_ring = static_cast<__nv_bfloat16*>(ring->v);
   p.ring_tok = static_cast<int64_t>(ring->capacity_frames) * P;
   p.P = P;
+  p.by_P = divisor(P);
+  p.by_words = divisor(H * d / 8);
   for (int i = 0; i < n_frames; ++i) p.slot[i] = slot_of(ring, ring->frames_written + i);
   if (launch_rope_append(p, rope->layout == ISPA_ROPE_HALF, stream) != cudaSuccess) return ISPA_ERR_CUDA;
   if (v8 && launch_append_vt(p.slot, n_frames, P, H, v, v_stride, ring->v, v_scale, ispa_ring_vt_stride(ring),

@@ -197,9 +197,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-__device__ __forceinline__ int quotient(int x, const Divisor& d) {
-  return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(x)) * d.m >> d.s);
-}
 // A piece (tokens `first` on of block `id`, a multiple of kPiece): its frame (slot), its first token in the frame (P
 // where the piece does not exist: a box there arrives as zeros) and how many tokens it has.
 struct Piece {

@@ -11,6 +11,22 @@
 
 namespace ispa {
 
+// x / n = x m >> s for 0 <= x < 2^31: with 2^k >= n, s = 31 + k and m = ceil(2^s / n), x m / 2^s exceeds x / n by less
+// than 2^31 n / (2^s n) <= 1 / n.
+struct Divisor {
+  uint32_t m, s;
+};
+#ifdef __CUDACC__
+__device__ __forceinline__ int quotient(int x, const Divisor& d) {
+  return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(x)) * d.m >> d.s);
+}
+#endif
+inline Divisor divisor(int32_t n) {
+  uint32_t k = 0;
+  while ((int64_t{1} << k) < n) ++k;
+  return {static_cast<uint32_t>(((uint64_t{1} << (31 + k)) + n - 1) / n), 31 + k};
+}
+
 // ------------------------------------------------------------ attention
 // One contiguous run of keys.  src 0 = the KV ring ([H][cap*P][d]), src 1 = the
 // chunk's own k_cur/v_cur ([n_q][H][d]).  start/count are token rows.  src 2 (the last
@@ -64,16 +80,6 @@ struct AttnParams {
 // key tile.  The maps view the ring as (columns, tokens of a frame, frames, heads), so that what a piece's box
 // has behind its frame's last token arrives as zeros.
 constexpr int kPiece = 64;
-// x / n = x m >> s for 0 <= x < 2^31: with 2^k >= n, s = 31 + k and m = ceil(2^s / n), x m / 2^s exceeds x / n by less
-// than 2^31 n / (2^s n) <= 1 / n.
-struct Divisor {
-  uint32_t m, s;
-};
-inline Divisor divisor(int32_t n) {
-  uint32_t k = 0;
-  while ((int64_t{1} << k) < n) ++k;
-  return {static_cast<uint32_t>(((uint64_t{1} << (31 + k)) + n - 1) / n), 31 + k};
-}
 struct AttnLists {
   CUtensorMap k, v;
   const int32_t* ids;   // [H][query tiles][top_k]
@@ -200,7 +206,7 @@ struct RopeParams {
   uint64_t wait_limit_ns;
 };
 cudaError_t launch_rope(const RopeParams& p, bool half, cudaStream_t s);
-// The same with the last tensor (the keys) going into a ring, and the values beside it.
+// The same with the first tensor (the keys) going into a ring, and the values beside it.
 struct RopeAppendParams : RopeParams {
   void* k_ring;                   // bf16, or e4m3 codes if k_scale: [H][ring_tok][head_dim]
   const float* k_scale;           // [H]
@@ -209,6 +215,8 @@ struct RopeAppendParams : RopeParams {
   __nv_bfloat16* v_ring;          // [H][ring_tok][head_dim]
   int64_t ring_tok;               // capacity_frames * P
   int32_t P;
+  Divisor by_P, by_words;         // by_words: 16-byte words of a token's values
+  int32_t wait_first;             // 1: wait for the kernel before at the start; 0: at the end (see values_kernel)
   int32_t slot[kMaxAppendFrames]; // ring slot of each frame
 };
 cudaError_t launch_rope_append(const RopeAppendParams& p, bool half, cudaStream_t s);

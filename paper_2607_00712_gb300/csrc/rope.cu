@@ -91,45 +91,49 @@ struct Lane {
   }
 };
 
-// Ring: the kernel whose last tensor goes into a ring (RopeAppendParams).
+// The kernels whose first tensor, the keys, goes into a ring, as codes or as bf16.
+struct RopeCodesParams : RopeAppendParams {};
 template <typename Params>
 constexpr bool kRing = !std::is_same_v<Params, RopeParams>;
+template <typename Params>
+constexpr bool kCodes = std::is_same_v<Params, RopeCodesParams>;
 
 // A token's place in the ring: row of head 0.
-__device__ __forceinline__ int64_t ring_row(const RopeAppendParams& p, int64_t tok) {
-  const int f = static_cast<int>(tok / p.P);
-  return static_cast<int64_t>(p.slot[f]) * p.P + (tok - static_cast<int64_t>(f) * p.P);
+__device__ __forceinline__ int64_t ring_row(const RopeAppendParams& p, int tok) {
+  const int f = quotient(tok, p.by_P);
+  return static_cast<int64_t>(p.slot[f]) * p.P + (tok - f * p.P);
 }
-// Eight features of head h to ring row `row`, as bf16 or as codes of f * (1 / scale).
+// Eight features of a head as codes of f * inv.
 template <bool HALF>
-__device__ __forceinline__ void ring_store(const RopeAppendParams& p, const Lane<HALF>& ln, int64_t row, int h,
-                                           const float* f) {
-  const int64_t at = (static_cast<int64_t>(h) * p.ring_tok + row) * p.head_dim;
-  if (!p.k_scale) {
-    ln.store(static_cast<__nv_bfloat16*>(p.k_ring) + at, f);
+__device__ __forceinline__ void store_codes(uint8_t* head, const Lane<HALF>& ln, const float* f, float inv) {
+  const uint32_t a = pack_e4m3x4(f, inv), b = pack_e4m3x4(f + 4, inv);
+  if constexpr (!HALF) {
+    *reinterpret_cast<uint2*>(head + ln.at0) = make_uint2(a, b);
   } else {
-    const float inv = __fdiv_rn(1.f, __ldg(p.k_scale + h));
-    uint8_t* const head = static_cast<uint8_t*>(p.k_ring) + at;
-    *reinterpret_cast<uint32_t*>(head + ln.at0) = pack_e4m3x4(f, inv);
-    *reinterpret_cast<uint32_t*>(head + ln.at1) = pack_e4m3x4(f + 4, inv);
+    *reinterpret_cast<uint32_t*>(head + ln.at0) = a;
+    *reinterpret_cast<uint32_t*>(head + ln.at1) = b;
   }
 }
-// A token's values, by `threads` threads of which this is number t.
-__device__ __forceinline__ void ring_values(const RopeAppendParams& p, int64_t tok, int64_t row, int heads, int t,
-                                            int threads) {
-  const int wph = p.head_dim / 8, words = heads * wph;
-  const uint4* from = reinterpret_cast<const uint4*>(p.v + tok * p.v_stride);
-  uint4* to = reinterpret_cast<uint4*>(p.v_ring) + row * wph;
-  for (int i0 = t; i0 < words; i0 += 4 * threads) {
+// Tokens first .. last - 1 of the values into the ring, by all threads of the block.
+__device__ __forceinline__ void copy_values(const RopeAppendParams& p, int first, int last) {
+  const int wph = p.head_dim / 8, shift = p.head_dim == 128 ? 4 : 3, words = p.rows[0].heads * wph;
+  const int total = (last - first) * words;
+  const uint4* from = reinterpret_cast<const uint4*>(p.v) + first * (p.v_stride / 8);
+  uint4* to = reinterpret_cast<uint4*>(p.v_ring);
+  for (int i0 = threadIdx.x; i0 < total; i0 += 4 * blockDim.x) {
     uint4 w[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i0 + u * threads < words) w[u] = __ldcs(from + i0 + u * threads);
+    int64_t at[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * threads;
-      if (i < words) to[i / wph * p.ring_tok * wph + i % wph] = w[u];
+      const int i = i0 + u * blockDim.x, tok = quotient(i, p.by_words), c = i - tok * words, h = c >> shift;
+      at[u] = -1;
+      if (i >= total) continue;
+      w[u] = __ldcs(from + tok * (p.v_stride / 8) + c);
+      at[u] = (h * p.ring_tok + ring_row(p, first + tok)) * wph + (c & (wph - 1));
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at[u] >= 0) to[at[u]] = w[u];
   }
 }
 
@@ -169,10 +173,10 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ Param
   int64_t row = 0;       // ring row of the keys
   bool keys = false;
   if constexpr (kRing<Params>) {
-    row = ring_row(p, tok);
-    keys = static_cast<int>(blockIdx.y) == p.n_rows - 1;
+    row = ring_row(p, static_cast<int>(tok));
+    keys = blockIdx.y == 0;
     if (static_cast<int>(blockIdx.y) == p.n_rows) {
-      ring_values(p, tok, row, p.rows[p.n_rows - 1].heads, threadIdx.x, blockDim.x);
+      copy_values(p, static_cast<int>(tok), static_cast<int>(tok) + 1);
       return;
     }
   }
@@ -216,7 +220,13 @@ __global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ Param
     ln.turn(f, cs);
     if (ln.live && h < o.heads) {
       if (kRing<Params> && keys) {
-        if constexpr (kRing<Params>) ring_store(p, ln, row, h, f);
+        if constexpr (kRing<Params>) {
+          const int64_t at = (static_cast<int64_t>(h) * p.ring_tok + row) * d;
+          if constexpr (kCodes<Params>)
+            store_codes(static_cast<uint8_t*>(p.k_ring) + at, ln, f, __fdiv_rn(1.f, __ldg(p.k_scale + h)));
+          else
+            ln.store(static_cast<__nv_bfloat16*>(p.k_ring) + at, f);
+        }
       } else {
         ln.store(out + static_cast<int64_t>(h) * d, f);
       }
@@ -272,7 +282,11 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
     fence_mbar_init();
   }
   __syncthreads();
-  pdl_wait();
+  if constexpr (kRing<Params>) {
+    if (p.wait_first) pdl_wait();
+  } else {
+    pdl_wait();
+  }
   pdl_trigger();
   const WaitCtx wc{&abort_word, p.status, p.wait_limit_ns};
   const int first = blockIdx.x * per_block;   // tokens are fewer than 2^30
@@ -332,12 +346,20 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   // norm, rotation and way out of a tensor; cs: the pairs' cosines and sines, with 1 / root of a norm over the token in
   // them, r that factor for what passes
   auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs, float r,
-                    bool keys) {
-    int64_t row = 0;
-    if constexpr (kRing<Params>)
-      if (keys) row = ring_row(p, tok);
+                    bool first) {
+    // keys (the first tensor) that go into the ring: head 0 of the token, and the step from one head to the next (values, or codes)
+    uint8_t* codes = nullptr;
+    int64_t step_out = heads_step * d;
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.out) + tok * o.out_stride + head0 * d;
+    if constexpr (kRing<Params>) {
+      if (first) {
+        const int64_t at = (head0 * p.ring_tok + ring_row(p, tok)) * d;
+        step_out = heads_step * p.ring_tok * d;
+        if constexpr (kCodes<Params>) codes = static_cast<uint8_t*>(p.k_ring) + at;
+        else out = static_cast<__nv_bfloat16*>(p.k_ring) + at;
+      }
+    }
     const float4* wp = planes + head0 * vecs + ln.c;
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     if (NORM == ISPA_QK_NORM_HEAD && o.weight && live) ln.weight(o.weight, w);
@@ -381,15 +403,16 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
           f[b] *= r;
         }
       }
-      if (kRing<Params> && keys) {
-        if constexpr (kRing<Params>)
-          if (here) ring_store(p, ln, row, h, f);
+      if (kCodes<Params> && first) {
+        if constexpr (kCodes<Params>)
+          if (here) store_codes(codes, ln, f, __fdiv_rn(1.f, __ldg(p.k_scale + h)));
+        codes += step_out;
       } else {
         if (here) ln.store(out, f);
+        out += step_out;
       }
       h += heads_step;
       x += heads_step * d;
-      out += heads_step * d;
       wp += heads_step * vecs;
     }
   };
@@ -428,22 +451,40 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         c1[j] = make_float2(cs[j].x * r0, cs[j].y * r0);
-        cs[j] = make_float2(cs[j].x * r1, cs[j].y * r1);
+        if constexpr (!kRing<Params>) cs[j] = make_float2(cs[j].x * r1, cs[j].y * r1);
       }
-      finish(src, p.rows[0], reinterpret_cast<const float4*>(smem), n0, c1, r0, n1 == 0);
-      if (n1) finish(src + 2 * n0, p.rows[1], reinterpret_cast<const float4*>(smem + 4 * n0), n1, cs, r1, true);
+      finish(src, p.rows[0], reinterpret_cast<const float4*>(smem), n0, c1, r0, true);
+      if constexpr (kRing<Params>) {   // from the table once more: the first tensor needs the registers
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = FULL || j < ln.turned ? table[4 * ln.c + j] : make_float2(1.f, 0.f);
+          cs[j] = make_float2(v.x * r1, v.y * r1);
+        }
+      }
+      if (n1) finish(src + 2 * n0, p.rows[1], reinterpret_cast<const float4*>(smem + 4 * n0), n1, cs, r1, false);
     } else {
-      finish(src, p.rows[0], nullptr, n0, cs, 1.f, n1 == 0);
-      if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f, true);
+      finish(src, p.rows[0], nullptr, n0, cs, 1.f, true);
+      if (n1) finish(src + 2 * n0, p.rows[1], nullptr, n1, cs, 1.f, false);
     }
-    if constexpr (kRing<Params>)
-      if (p.v) ring_values(p, tok, ring_row(p, tok), p.rows[p.n_rows - 1].heads, t, threads);
     tm.sync();   // the token's stage and the table are free
     if (STAGES == 1 && t == 0 && ok && last - tok > teams) fetch(tok + teams, stage_of(issued++));
   }
   if (t == 0 && !ok)   // after a timeout: nothing in flight when the block leaves
     for (uint32_t i = issued < STAGES ? 0 : issued - STAGES; i < issued; ++i)
       mbar_wait_drain(full + 8 * stage_of(i), parity_of(i), R_DRAIN_NS);
+  if constexpr (kRing<Params>)
+    if (!p.wait_first) pdl_wait();   // the values' launch completes before this one does
+}
+
+// The values of many tokens, in a launch of their own in front of the keys', which starts as soon as this one's blocks
+// have the kernel before behind them and runs beside it.  In the teams' loop the copies cost their registers: 4680
+// tokens of 3 x 5120 with 8-bit keys 83 us against 62, of 3 x 1536 25.6 against 20.
+__global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ RopeAppendParams p, int per_block) {
+  pdl_wait();
+  pdl_trigger();
+  const int first = blockIdx.x * per_block;
+  copy_values(p, first, static_cast<int>(min(static_cast<int64_t>(first) + per_block, p.n)));
 }
 
 template <bool HALF, typename Params>
@@ -452,10 +493,19 @@ cudaError_t launch_layout(const Params& p, int sms, cudaStream_t s) {
   const RopeForm f = rope_form(p.n, p.n_rows, heads, norms, p.head_dim, p.pairs, p.lanes_per_head, HALF, sms);
   if (f.stream) {
     const auto go = [&](auto kernel) {
-      const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
+      cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
       if (e != cudaSuccess) return e;
+      Params q = p;
+      if constexpr (kRing<Params>) {
+        q.wait_first = p.v == nullptr;
+        if (p.v) {
+          const int per = static_cast<int>((p.n + 8 * sms - 1) / (8 * sms));
+          e = launch_pdl(values_kernel, dim3(static_cast<unsigned>((p.n + per - 1) / per)), dim3(256), 0, s, p, per);
+          if (e != cudaSuccess) return e;
+        }
+      }
       return launch_pdl(kernel, dim3(static_cast<unsigned>((p.n + f.tokens - 1) / f.tokens)),
-                        dim3(32 * f.warps, f.teams), f.smem, s, p, static_cast<int>(f.tokens));
+                        dim3(32 * f.warps, f.teams), f.smem, s, q, static_cast<int>(f.tokens));
     };
     const auto pick = [&](auto one, auto two) { return f.stages == 1 ? go(one) : go(two); };
     if (norms[0] == ISPA_QK_NORM_TOKEN)
@@ -496,6 +546,10 @@ cudaError_t launch_rope_append(const RopeAppendParams& p, bool half, cudaStream_
   int dev = 0, sms = 152;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (p.k_scale) {
+    const RopeCodesParams c{p};
+    return half ? launch_layout<true>(c, sms, s) : launch_layout<false>(c, sms, s);
+  }
   return half ? launch_layout<true>(p, sms, s) : launch_layout<false>(p, sms, s);
 }
 
