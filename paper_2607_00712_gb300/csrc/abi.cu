@@ -1148,12 +1148,12 @@ ispa_status ispa_select_blocks(const ispa_kv_ring* ring, ispa_window win, int32_
   p.top_k = top_k;
   const int32_t nb = static_cast<int32_t>(blocks_of(ring->tokens_per_frame, block));
   p.ids = static_cast<int64_t>(ring->capacity_frames) * nb;
-  p.n_runs = ks.n_hist;
   for (int r = 0; r < ks.n_hist; ++r) {
     p.run_shift[r] = ks.hist[r].first_slot * nb - p.n_cand;
     p.n_cand += ks.hist[r].n_slots * nb;
     p.run_end[r] = p.n_cand;
   }
+  for (int r = ks.n_hist; r < ISPA_MAX_RANGES; ++r) p.run_end[r] = INT32_MAX;
   return launch_select(p, stream) == cudaSuccess ? ISPA_OK : ISPA_ERR_CUDA;
 }
 

@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
   pdl_wait();
   pdl_trigger();
   const uint4* from = static_cast<const uint4*>(p.k) +
-                      ((static_cast<int64_t>(h) * p.capacity + slot) * p.P + static_cast<int64_t>(b) * p.block) * LPR + lane;
+                      ((static_cast<int64_t>(h) * p.capacity + slot) * p.P + static_cast<int64_t>(b) * p.block) * LPR +
+                      lane;
   float s[VALS];
 #pragma unroll
   for (int e = 0; e < VALS; ++e) s[e] = 0.f;
@@ -94,131 +95,194 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------ selection
-// Workspace: per head and query block the sum of the queries as two floats a feature, then per head, query block and
-// candidate the 32-bit score, per head and candidate the mean's norm, and room for 64-bit scores.
+// Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
+// 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
+// multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
 struct SelectWs {
-  float2* qsum;    // [H][n_qt][d]
-  double* exact;   // [H][n_qt][n_cand]
-  float* score;    // [H][n_qt][n_cand]
-  float* norm;     // [H][n_cand]
+  float* hi;          // [H][n_qt][d]
+  float* lo;
+  double* exact;      // [H][n_qt][n_cand]
+  float* score;       // [H][n_qt][n_cand]
+  float* norm;        // [H][n_qt]
+  float* largest;     // [H][tiles]
 };
 __host__ __device__ __forceinline__ SelectWs ws_of(void* ws, int64_t H, int64_t n_qt, int64_t d, int64_t n_cand) {
   SelectWs w;
-  w.qsum = static_cast<float2*>(ws);
-  w.exact = reinterpret_cast<double*>(w.qsum + H * n_qt * d);
+  w.hi = static_cast<float*>(ws);
+  w.lo = w.hi + H * n_qt * d;
+  w.exact = reinterpret_cast<double*>(w.lo + H * n_qt * d);
   w.score = reinterpret_cast<float*>(w.exact + H * n_qt * n_cand);
   w.norm = w.score + H * n_qt * n_cand;
+  w.largest = w.norm + H * n_qt;
   return w;
 }
 
+// Block number of a candidate.  The runs behind the last one end at INT32_MAX.
 __device__ __forceinline__ int id_of(const SelectParams& p, int cand) {
-  int r = 0;
-  while (r + 1 < p.n_runs && cand >= p.run_end[r]) ++r;
-  return cand + p.run_shift[r];
+  int shift = p.run_shift[ISPA_MAX_RANGES - 1];
+#pragma unroll
+  for (int r = ISPA_MAX_RANGES - 2; r >= 0; --r)
+    if (cand < p.run_end[r]) shift = p.run_shift[r];
+  return cand + shift;
 }
 
-// hi + lo = the sum of a and b, hi rounded to nearest (Knuth's TwoSum); lo collects.
+// hi + lo = the sum of hi and x, hi rounded to nearest (Knuth's TwoSum); lo collects.
 __device__ __forceinline__ void two_sum(float& hi, float& lo, float x) {
   const float s = __fadd_rn(hi, x), t = __fsub_rn(s, hi);
   lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fsub_rn(x, t)));
   hi = s;
 }
 
-// Sum of a query block's queries of one head: rows over the threads, then over the block.  Of 2^-7 of the queries, exact
-// for every bf16 value, so that the sum of finite ones stays finite; the order of the scores is the same.
-template <int D>
-__global__ void __launch_bounds__(256) qsum_kernel(const __grid_constant__ SelectParams p) {
-  constexpr int LPR = D / 8, ROWS = 256 / LPR;
-  __shared__ float2 part[ROWS][D];
-  const int qt = blockIdx.x, h = blockIdx.y, lane = threadIdx.x % LPR, r0 = threadIdx.x / LPR;
-  const int n = min(kSelectQueries, p.n_q - qt * kSelectQueries);
-  pdl_wait();
-  pdl_trigger();
-  const int64_t row = static_cast<int64_t>(p.H) * LPR;
-  const uint4* from = reinterpret_cast<const uint4*>(p.q) + (static_cast<int64_t>(qt) * kSelectQueries) * row +
-                      h * LPR + lane;
-  float hi[8] = {}, lo[8] = {};
-  uint4 w[kSelectQueries / ROWS];
+// Sum of a query block's queries of one head, by THREADS threads: rows over the threads, then over the block.  Of 2^-7
+// of the queries, exact for every bf16 value, so that the sum of finite ones stays finite; the order of the scores is
+// the same.  Feature c's sum (hi, lo) to thread c < D; a barrier has passed since the last use of `part` by others.
+template <int D, int THREADS>
+struct QSum {
+  static constexpr int LPR = D / 8, ROWS = THREADS / LPR;
+  float2 part[ROWS][D];
+  __device__ __forceinline__ float2 of(const SelectParams& p, int h, int qt) {
+    const int lane = threadIdx.x % LPR, r0 = threadIdx.x / LPR;
+    const int n = min(kSelectQueries, p.n_q - qt * kSelectQueries);
+    const int64_t row = static_cast<int64_t>(p.H) * LPR;
+    const uint4* from = reinterpret_cast<const uint4*>(p.q) + (static_cast<int64_t>(qt) * kSelectQueries) * row +
+                        h * LPR + lane;
+    float hi[8] = {}, lo[8] = {};
+    for (int u0 = 0; u0 * ROWS < n; u0 += 8) {
+      uint4 w[8];
 #pragma unroll
-  for (int u = 0; u < kSelectQueries / ROWS; ++u)
-    w[u] = r0 + u * ROWS < n ? __ldg(from + (r0 + u * ROWS) * row) : make_uint4(0, 0, 0, 0);
+      for (int u = 0; u < 8; ++u) {
+        const int r = r0 + (u0 + u) * ROWS;
+        w[u] = r < n ? __ldg(from + r * row) : make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
-  for (int u = 0; u < kSelectQueries / ROWS; ++u) {
-    float f[8];
-    unpack8(w[u], f);
+      for (int u = 0; u < 8; ++u) {
+        float f[8];
+        unpack8(w[u], f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) two_sum(hi[e], lo[e], 0.0078125f * f[e]);
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) part[r0][lane * 8 + e] = make_float2(hi[e], lo[e]);
-  __syncthreads();
-  const int c = threadIdx.x;
-  if (c < D) {
-    float a = part[0][c].x, b = part[0][c].y;
-    for (int r = 1; r < ROWS; ++r) {
-      two_sum(a, b, part[r][c].x);
-      b += part[r][c].y;
+        for (int e = 0; e < 8; ++e) two_sum(hi[e], lo[e], 0.0078125f * f[e]);
+      }
     }
-    const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, p.n_cand);
-    ws.qsum[(static_cast<int64_t>(h) * p.n_qt + qt) * D + c] = make_float2(a, fabsf(a) < INFINITY ? b : 0.f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[r0][lane * 8 + e] = make_float2(hi[e], lo[e]);
+    __syncthreads();
+    float a = 0.f, b = 0.f;
+    if (threadIdx.x < D) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const float2 v = part[r][threadIdx.x];
+        two_sum(a, b, v.x);
+        b += v.y;
+      }
+    }
+    return make_float2(a, fabsf(a) < INFINITY ? b : 0.f);
   }
+};
+// The sum to the workspace, with its norm; all threads of the block.
+template <int D>
+__device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float2 v, float (*red)[32], int warps) {
+  if (threadIdx.x < D) {
+    ws.hi[list * D + threadIdx.x] = v.x;
+    ws.lo[list * D + threadIdx.x] = v.y;
+  }
+  const float s = block_reduce<SumOp>(threadIdx.x < D ? v.x * v.x : 0.f, warps, red, 0);
+  if (threadIdx.x == 0) ws.norm[list] = sqrtf(s);
 }
 
-// 32-bit scores: a tile of 64 candidates x 32 query blocks of one head, 2 x 4 a thread.
-constexpr int S_CAND = 64, S_QT = 32;
 template <int D>
-__global__ void __launch_bounds__(256) score_kernel(const __grid_constant__ SelectParams p) {
-  extern __shared__ float4 sm4[];
-  float* const m = reinterpret_cast<float*>(sm4);   // [S_CAND][D + 4]
-  float* const q = m + S_CAND * (D + 4);            // [S_QT][D + 4]
-  const int c0 = blockIdx.x * S_CAND, h = blockIdx.y;
-  const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, p.n_cand);
+__global__ void __launch_bounds__(256) qsum_kernel(const __grid_constant__ SelectParams p) {
+  __shared__ QSum<D, 256> sum;
+  __shared__ float red[2][32];
+  const int qt = blockIdx.x, h = blockIdx.y;
   pdl_wait();
   pdl_trigger();
-  for (int i = threadIdx.x; i < S_CAND * (D / 4); i += 256) {
-    const int r = i / (D / 4), c = i % (D / 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c0 + r < p.n_cand)
-      v = __ldg(reinterpret_cast<const float4*>(p.means + (h * p.ids + id_of(p, c0 + r)) * D) + c);
-    *reinterpret_cast<float4*>(m + r * (D + 4) + 4 * c) = v;
+  keep_sum<D>(ws_of(p.ws, p.H, p.n_qt, D, p.n_cand), static_cast<int64_t>(h) * p.n_qt + qt, sum.of(p, h, qt), red, 8);
+}
+
+// 32-bit scores: a tile of 64 candidates x 8 J query blocks of one head in shared memory, 2 x J a thread.  A warp's
+// lanes read 16 candidates' words and two query blocks' at a time, with J = 5 in 9 cycles of shared memory for 10 of
+// products.  OWN: one query block, whose sum every block of the grid takes for itself.
+constexpr int S_CAND = 64, S_THREADS = 256;
+template <int D, int J>
+constexpr int kScoreSmem = (S_CAND + 8 * J) * (D + 4) * 4;
+__device__ __forceinline__ void copy16(uint32_t dst, const float4* src, bool here) {   // else zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(here ? 16 : 0) : "memory");
+}
+template <int D, int J, bool OWN>
+__global__ void __launch_bounds__(S_THREADS) score_kernel(const __grid_constant__ SelectParams p) {
+  static_assert(!OWN || J == 1, "one query block");
+  constexpr int LD = D + 4, QT = 8 * J, VPR = D / 4;   // rows 4 banks apart; a row's float4
+  extern __shared__ float4 tile[];
+  float* const m = reinterpret_cast<float*>(tile);   // [S_CAND][LD]
+  float* const q = m + S_CAND * LD;                  // [QT][LD]
+  __shared__ float red[2][32];
+  const int c0 = blockIdx.x * S_CAND, h = blockIdx.y;
+  const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, p.n_cand);
+  // Behind qsum_kernel this starts when all its blocks have the kernels before behind them, so the means can be read
+  // while it works.
+  if constexpr (OWN) pdl_wait();
+  const uint32_t m_at = smem_u32(m), q_at = smem_u32(q);
+  const float4* const means = reinterpret_cast<const float4*>(p.means) + h * p.ids * VPR;
+#pragma unroll
+  for (int i = threadIdx.x; i < S_CAND * VPR; i += S_THREADS) {
+    const int r = i / VPR, c = i % VPR;
+    const bool here = c0 + r < p.n_cand;
+    copy16(m_at + (r * LD + 4 * c) * 4, means + (here ? static_cast<int64_t>(id_of(p, c0 + r)) * VPR + c : 0), here);
   }
-  const int tc = threadIdx.x % 16, tq = threadIdx.x / 16;   // candidates tc + 16 i, query blocks tq + 16 j
-  for (int q0 = 0; q0 < p.n_qt; q0 += S_QT) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < S_QT * D; i += 256) {
-      const int r = i / D, c = i % D;
-      q[r * (D + 4) + c] = q0 + r < p.n_qt ? ws.qsum[(static_cast<int64_t>(h) * p.n_qt + q0 + r) * D + c].x : 0.f;
+  if constexpr (!OWN) pdl_wait();
+  pdl_trigger();
+  if constexpr (OWN) {
+    __shared__ QSum<D, S_THREADS> sum;
+    const float2 v = sum.of(p, h, 0);
+    if (threadIdx.x < D) q[threadIdx.x] = v.x;
+#pragma unroll
+    for (int i = threadIdx.x; i < 7 * D; i += S_THREADS) q[(1 + i / D) * LD + i % D] = 0.f;
+    if (blockIdx.x == 0) keep_sum<D>(ws, h, v, red, S_THREADS / 32);
+  }
+  // candidates tc + 32 i, query blocks tq + 8 j: a warp has 16 of the one and two of the other
+  const int tc = threadIdx.x % 16 + 16 * (threadIdx.x / 128), tq = threadIdx.x / 16 % 8;
+  for (int q0 = 0; q0 < p.n_qt; q0 += QT) {
+    const int rows = min(QT, p.n_qt - q0);
+    if constexpr (!OWN) {
+      const float4* from = reinterpret_cast<const float4*>(ws.hi + (static_cast<int64_t>(h) * p.n_qt + q0) * D);
+      if (q0 > 0) __syncthreads();
+#pragma unroll
+      for (int i = threadIdx.x; i < QT * VPR; i += S_THREADS) {
+        const bool here = i < rows * VPR;
+        copy16(q_at + (i / VPR * LD + 4 * (i % VPR)) * 4, from + (here ? i : 0), here);
+      }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    float acc[4][2] = {};
+    float acc[2][J] = {};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
-      float4 a[4], b[2];
+      float4 a[2], b[J];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(m + (tc + 16 * i) * (D + 4) + c);
+      for (int i = 0; i < 2; ++i) a[i] = *reinterpret_cast<const float4*>(m + (tc + 32 * i) * LD + c);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b[j] = *reinterpret_cast<const float4*>(q + (tq + 16 * j) * (D + 4) + c);
+      for (int j = 0; j < J; ++j) b[j] = *reinterpret_cast<const float4*>(q + (tq + 8 * j) * LD + c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < J; ++j)
           acc[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, acc[i][j]))));
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (c0 + tc + 16 * i < p.n_cand && q0 + tq + 16 * j < p.n_qt)
-          ws.score[(static_cast<int64_t>(h) * p.n_qt + q0 + tq + 16 * j) * p.n_cand + c0 + tc + 16 * i] = acc[i][j];
+      for (int j = 0; j < J; ++j)
+        if (c0 + tc + 32 * i < p.n_cand && tq + 8 * j < rows)
+          ws.score[(static_cast<int64_t>(h) * p.n_qt + q0 + tq + 8 * j) * p.n_cand + c0 + tc + 32 * i] = acc[i][j];
   }
-  if (threadIdx.x < S_CAND && c0 + threadIdx.x < p.n_cand) {
-    float s = 0.f;
-    for (int c = 0; c < D; ++c) {
-      const float v = m[threadIdx.x * (D + 4) + c];
-      s = fmaf(v, v, s);
-    }
-    ws.norm[static_cast<int64_t>(h) * p.n_cand + c0 + threadIdx.x] = sqrtf(s);
+  // the largest of the tile's norms: four threads a mean
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    const float4 v = *reinterpret_cast<const float4*>(m + threadIdx.x / 4 * LD + 4 * (4 * c + threadIdx.x % 4));
+    s = fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, fmaf(v.w, v.w, s))));
   }
+  s = block_reduce<MaxOp>(group_reduce<SumOp>(s, 4), S_THREADS / 32, red, 1);
+  if (threadIdx.x == 0) ws.largest[h * gridDim.x + blockIdx.x] = sqrtf(s);
 }
 
 // Keys whose order as integers is that of the scores; both zeros alike, NaN below all.
@@ -232,26 +296,88 @@ __device__ __forceinline__ uint64_t order_key(double f) {
   const uint64_t u = static_cast<uint64_t>(__double_as_longlong(f + 0.0));
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
-__device__ __forceinline__ float score_of(uint32_t key) {   // of the last key but NaN's: finite or infinite
+__device__ __forceinline__ float score_of(uint32_t key) {   // of any key but NaN's
   return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
 }
 
-constexpr int P_THREADS = 256, P_WARPS = P_THREADS / 32;
 constexpr int kFew = 64;   // candidates that are ranked one against one
 
-// The k-th largest (1 <= k <= how many count) of the keys key(i), i < n, among those with live(i), and how many of
-// those equal to it are among the k largest.  Digit by digit from the top.
-template <typename Key, typename Get, typename Live>
-__device__ Key kth_largest(int n, int k, Get&& key, Live&& live, int* hist, int& ties) {
-  Key known = 0;
-#pragma unroll 1
-  for (int shift = 8 * sizeof(Key) - 8; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += P_THREADS) hist[i] = 0;
+template <int W>
+struct PickShared {
+  int4 hist[2][64];           // 256 counts, of the highest digit first; used in turn
+  uint32_t list[kFew];
+  uint32_t lo[W], hi[W];
+  float norms[W];
+  uint64_t counts[2][W];
+  int few[kFew];
+  uint64_t few_key[kFew], few_least;
+  int n_list, n_few, few_ties;
+  int wide[258];
+};
+
+// Two counts in a word: their sum over the warps before this one, and over all.
+template <int W>
+__device__ __forceinline__ uint64_t warps_before(uint64_t* of, uint64_t v, uint64_t& all) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  uint64_t s = 0;
+  all = v;
+  if constexpr (W > 1) {
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) of[warp] = v;
     __syncthreads();
-    const Key above = shift == 8 * static_cast<int>(sizeof(Key)) - 8 ? Key{0} : ~Key{0} << (shift + 8);
-    for (int i = threadIdx.x; i < n; i += P_THREADS) {
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const uint64_t x = of[w];
+      if (w < warp) s += x;
+      all += x;
+    }
+  }
+  return s;
+}
+
+// Of 256 counts, of the highest digit first: the digit where they add up to k, how many lie above it, how many at it.
+// Every warp by itself.
+__device__ __forceinline__ int digit_of(const int4* hist, int k, int& above, int& at) {
+  const int lane = threadIdx.x & 31;
+  const int4 x = hist[2 * lane], y = hist[2 * lane + 1];
+  const int v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  int sum = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum += v[j];
+  int before = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int u = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += u;
+  }
+  const int from = __ffs(__ballot_sync(0xffffffffu, before >= k)) - 1;
+  before -= sum;
+  int digit = 0, n = 0, b = before;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (b < k) digit = 8 * lane + j, before = b, n = v[j];
+    b += v[j];
+  }
+  above = __shfl_sync(0xffffffffu, before, from);
+  at = __shfl_sync(0xffffffffu, n, from);
+  return 255 - __shfl_sync(0xffffffffu, digit, from);
+}
+
+// The k-th largest (1 <= k <= how many count) of the 64-bit keys key(i), i < n, among those with live(i), and how many
+// of those equal to it are among the k largest.  Digit by digit from the top.
+template <int THREADS, typename Get, typename Live>
+__device__ uint64_t kth_largest(int n, int k, Get&& key, Live&& live, int* hist, int& ties) {
+  uint64_t known = 0;
+#pragma unroll 1
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += THREADS) hist[i] = 0;
+    __syncthreads();
+    const uint64_t above = shift == 56 ? 0 : ~uint64_t{0} << (shift + 8);
+    for (int i = threadIdx.x; i < n; i += THREADS) {
       if (!live(i)) continue;
-      const Key x = key(i);
+      const uint64_t x = key(i);
       if ((x & above) == known) atomicAdd(hist + (x >> shift & 255), 1);
     }
     __syncthreads();
@@ -274,7 +400,7 @@ __device__ Key kth_largest(int n, int k, Get&& key, Live&& live, int* hist, int&
       }
     }
     __syncthreads();
-    known |= static_cast<Key>(hist[256]) << shift;
+    known |= static_cast<uint64_t>(hist[256]) << shift;
     k -= hist[257];
   }
   __syncthreads();
@@ -282,161 +408,284 @@ __device__ Key kth_largest(int n, int k, Get&& key, Live&& live, int* hist, int&
   return known;
 }
 
-// One block a list.
-template <int D>
-__global__ void __launch_bounds__(P_THREADS) pick_kernel(const __grid_constant__ SelectParams p) {
-  __shared__ int hist[258];
-  __shared__ float red[2][32];
-  __shared__ int counts[2][P_WARPS + 2];
-  __shared__ int few[kFew];
-  __shared__ uint64_t few_key[kFew], few_least;
-  __shared__ int n_few, above_window;
+// One block of W warps a list.  Warp w takes the candidates from w 32 steps on, a step of 32 neighbours at a time.
+// PER: the steps, with their keys in registers; 0: any number, read again for each pass.  Latency bounds it (the passes
+// over the keys, with a barrier each): 1250 candidates in two warps 3 us longer than in eight.
+template <int D, int W, int PER>
+__global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ SelectParams p) {
+  constexpr int THREADS = 32 * W;
+  __shared__ PickShared<W> sh;
   const int qt = blockIdx.x, h = blockIdx.y, n = p.n_cand, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int64_t list = static_cast<int64_t>(h) * p.n_qt + qt;
   int32_t* const out = p.blocks + list * p.top_k;
+#pragma unroll
+  for (int i = threadIdx.x; i < 128; i += THREADS) sh.hist[i / 64][i % 64] = make_int4(0, 0, 0, 0);
+  if (threadIdx.x == 0) sh.n_list = sh.n_few = 0;
   pdl_wait();
   pdl_trigger();
   if (n <= p.top_k) {   // everything there is
-    for (int i = threadIdx.x; i < p.top_k; i += P_THREADS) out[i] = i < n ? id_of(p, i) : -1;
+    for (int i = threadIdx.x; i < p.top_k; i += THREADS) out[i] = i < n ? id_of(p, i) : -1;
     return;
   }
   const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, n);
   const float* score = ws.score + list * n;
-  const float2* qs = ws.qsum + list * D;
   double* exact = ws.exact + list * n;
-
-  // The bound: a product's sum in 32 bits over d terms is off by at most (d + 2) 2^-24 |q| |m| (Cauchy-Schwarz; q's
-  // rounding to 32 bits among it); the rest covers the roundings of |q|, |m| and of T +- 2 E themselves, 2^-126
-  // products that underflow.
-  float mm = 0.f, qq = 0.f;
-  for (int i = threadIdx.x; i < n; i += P_THREADS) mm = max_nan(mm, ws.norm[static_cast<int64_t>(h) * n + i]);
-  if (threadIdx.x < D) qq = qs[threadIdx.x].x * qs[threadIdx.x].x;
-  mm = block_reduce<MaxOp>(mm, P_WARPS, red, 0);
-  qq = block_reduce<SumOp>(qq, P_WARPS, red, 1);
-  const float E = (D + 24) * 5.9604645e-8f * sqrtf(qq) * mm + 1.1754944e-38f;
-
-  int ties;
-  const auto key = [&](int i) { return order_key(score[i]); };
-  const uint32_t t_key = kth_largest<uint32_t>(n, p.top_k, key, [](int) { return true; }, hist, ties);
-  const float T = score_of(t_key);
+  const int steps = PER ? PER : (n + THREADS - 1) / THREADS, first = warp * 32 * steps + lane;
+  const int tiles = (n + S_CAND - 1) / S_CAND;
+  float f[PER ? PER : 1];
+  if constexpr (PER != 0) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) f[j] = first + 32 * j < n ? __ldcg(score + first + 32 * j) : 0.f;
+  }
+  const float q_norm = __ldcg(ws.norm + list);
+  float m_norm = 0.f;
+  for (int i = threadIdx.x; i < tiles; i += THREADS) m_norm = max_nan(m_norm, __ldcg(ws.largest + h * tiles + i));
+  uint32_t keys[PER ? PER : 1];
+  if constexpr (PER != 0) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) keys[j] = order_key(f[j]);
+  }
+  const auto each = [&](auto&& f) {   // f(candidate, key, there is one), all lanes alike
+    if constexpr (PER != 0) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) f(first + 32 * j, keys[j], first + 32 * j < n);
+    } else {
+      for (int j = 0; j < steps; ++j) {
+        const int i = first + 32 * j;
+        f(i, i < n ? order_key(__ldcg(score + i)) : 0, i < n);
+      }
+    }
+  };
+  // T, the top_k-th largest 32-bit score, by counts.
+  uint32_t lo = 0xffffffffu, hi = 0;
+  each([&](int, uint32_t x, bool here) {
+    if (here) lo = min(lo, x), hi = max(hi, x);
+  });
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  m_norm = warp_max(m_norm);
+  if (W > 1 && lane == 0) sh.lo[warp] = lo, sh.hi[warp] = hi, sh.norms[warp] = m_norm;
+  __syncthreads();
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      lo = min(lo, sh.lo[w]);
+      hi = max(hi, sh.hi[w]);
+      m_norm = max_nan(m_norm, sh.norms[w]);
+    }
+  }
+  int bits = 32 - __clz(lo ^ hi);                       // of the keys, not known yet
+  uint32_t known = bits == 32 ? 0 : hi >> bits << bits;
+  int k = p.top_k, left = n;                            // wanted and there among those that it can be
+  // 256 steps of one size from the smallest to the largest: mostly few candidates are in the one that T is in.  (The
+  // keys' digits, which differ little in front, made their lanes wait for one another's counts.)
+  const float base = score_of(lo), scale = 256.f / (score_of(hi) - base);
+  const auto step_of = [&](uint32_t x) {                // never smaller for a larger key
+    return max(0, min(255, static_cast<int>((score_of(x) - base) * scale)));
+  };
+  int step = -1;                                        // that T is in, if it is known so
+  if (left > kFew && bits > 0 && lo && fabsf(base) < INFINITY && score_of(hi) < INFINITY) {
+    each([&](int, uint32_t x, bool here) {
+      if (here) atomicAdd(reinterpret_cast<int*>(sh.hist[0]) + (255 - step_of(x)), 1);
+    });
+    __syncthreads();
+    int above, at;
+    const int s = digit_of(sh.hist[0], k, above, at);
+    if (at <= kFew) {
+      step = s;
+      k -= above;
+      left = at;
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int i = threadIdx.x; i < 64; i += THREADS) sh.hist[0][i] = make_int4(0, 0, 0, 0);
+      __syncthreads();
+    }
+  }
+  // Else its key digit by digit, from the highest of the bits that the keys do not share, until few have the digits
+  // found so far.
+  const auto among = [&](uint32_t x) { return bits == 32 || x - known < 1u << bits; };
+  for (int turn = 0; bits > 0 && left > kFew; ++turn) {
+    int4* const hist = sh.hist[turn & 1];
+    const int shift = max(0, bits - 8);
+    each([&](int, uint32_t x, bool here) {
+      if (here && among(x)) atomicAdd(reinterpret_cast<int*>(hist) + (255 - ((x - known) >> shift)), 1);
+    });
+    __syncthreads();
+    int above;
+    known |= static_cast<uint32_t>(digit_of(hist, k, above, left)) << shift;
+    k -= above;
+    bits = shift;
+    if (turn > 0 && bits > 0 && left > kFew) {          // the other counts, which all have read
+#pragma unroll
+      for (int i = threadIdx.x; i < 64; i += THREADS) sh.hist[(turn & 1) ^ 1][i] = make_int4(0, 0, 0, 0);
+      __syncthreads();
+    }
+  }
+  // Those are ranked one against one.
+  uint32_t t_key = known;
+  if (bits > 0) {
+    if (step >= 0) {
+      each([&](int, uint32_t x, bool here) {
+        if (here && step_of(x) == step) sh.list[atomicAdd(&sh.n_list, 1)] = x;
+      });
+    } else {
+      each([&](int, uint32_t x, bool here) {
+        if (here && among(x)) sh.list[atomicAdd(&sh.n_list, 1)] = x;
+      });
+    }
+    __syncthreads();
+    // every warp by itself: of a lane's two, one that less than k are above of and k or more at or above
+    const uint32_t a = lane < left ? sh.list[lane] : 0, b = lane + 32 < left ? sh.list[lane + 32] : 0;
+    int a_above = 0, a_at = 0, b_above = 0, b_at = 0;
+    for (int i = 0; i < left; ++i) {
+      const uint32_t x = sh.list[i];
+      a_above += x > a;
+      a_at += x >= a;
+      b_above += x > b;
+      b_at += x >= b;
+    }
+    const bool a_is = lane < left && a_above < k && a_at >= k, b_is = lane + 32 < left && b_above < k && b_at >= k;
+    const uint32_t found = __ballot_sync(0xffffffffu, a_is || b_is);
+    t_key = __shfl_sync(0xffffffffu, a_is ? a : b, __ffs(found) - 1);
+  }
+  // The bound: a product's sum in 32 bits over d terms is off by at most (d + 1) 2^-24 |q| |m| (Cauchy-Schwarz; q's
+  // rounding to 32 bits among it), besides what underflows, 2^-150 a product; the other 23 steps are for the roundings
+  // of |q|, |m| and of T +- 2 E.
+  const float E = (D + 24) * 5.9604645e-8f * q_norm * m_norm + 1.1754944e-38f;
+  const float T = t_key ? score_of(t_key) : INFINITY;
   // without a finite bound everything is scored again
   const bool bounded = E < INFINITY && fabsf(T) < INFINITY;
-  const float low = T - 2.f * E - 1e-6f * fabsf(T) * 0.25f, high = T + 2.f * E + 1e-6f * fabsf(T) * 0.25f;
-  const auto sure = [&](int i) { return bounded && score[i] > high; };
-  const auto open = [&](int i) { return !bounded || (score[i] >= low && score[i] <= high); };
-  if (threadIdx.x == 0) n_few = above_window = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += P_THREADS) {
-    if (sure(i)) atomicAdd(&above_window, 1);
-    else if (open(i)) {
-      const int at = atomicAdd(&n_few, 1);
-      if (at < kFew) few[at] = i;
-    }
+  const float low = T - 2.f * E - 2.5e-7f * fabsf(T), high = T + 2.f * E + 2.5e-7f * fabsf(T);
+  const uint32_t low_key = bounded ? order_key(low) : 0, high_key = bounded ? order_key(high) : 0xffffffffu;
+  // sure: key above high_key; open: from low_key to high_key
+  uint32_t n_sure = 0, n_in = 0;
+  each([&](int, uint32_t x, bool here) {
+    n_sure += here && x > high_key;
+    n_in += here && x >= low_key;
+  });
+  uint64_t all;
+  const uint64_t before = warps_before<W>(sh.counts[0], static_cast<uint64_t>(n_sure) << 32 | n_in, all);
+  const int need = p.top_k - static_cast<int>(all >> 32);   // of the open ones
+  const int n_open = static_cast<int>(all) - static_cast<int>(all >> 32);
+  const uint32_t lower_lanes = (1u << lane) - 1u;
+  int at = static_cast<int>(before);
+  if (need >= n_open) {   // all of them
+    each([&](int i, uint32_t x, bool here) {
+      const bool in = here && x >= low_key;
+      const uint32_t mask = __ballot_sync(0xffffffffu, in);
+      if (in) out[at + __popc(mask & lower_lanes)] = id_of(p, i);
+      at += __popc(mask);
+    });
+    return;
   }
-  __syncthreads();
-  const int need = p.top_k - above_window, n_open = n_few;   // of the open ones
-  uint64_t least = 0;   // open candidates are taken above this key, `ties` of those at it
-  ties = n_open;
-  if (need < n_open) {
-    // 64-bit scores, a warp a candidate, every one's terms in the same order
-    double q[D / 32];
+  // 64-bit scores, a warp a candidate, every one's terms in the same order
+  uint64_t least;   // open candidates are taken above this key, `ties` of those at it
+  int ties;
+  double q[D / 32];
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      const float2 v = qs[lane + 32 * j];
-      q[j] = static_cast<double>(v.x) + static_cast<double>(v.y);
+  for (int j = 0; j < D / 32; ++j) {
+    const int64_t c = list * D + lane + 32 * j;
+    q[j] = static_cast<double>(ws.hi[c]) + static_cast<double>(ws.lo[c]);
+  }
+  const auto score64 = [&](int cand) {
+    const float* m = p.means + (h * p.ids + id_of(p, cand)) * D + lane;
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) s = fma(q[j], static_cast<double>(__ldg(m + 32 * j)), s);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+  };
+  if (n_open <= kFew) {
+    each([&](int i, uint32_t x, bool here) {
+      if (here && x >= low_key && x <= high_key) sh.few[atomicAdd(&sh.n_few, 1)] = i;
+    });
+    __syncthreads();
+    for (int i = warp; i < n_open; i += W) {
+      const double s = score64(sh.few[i]);
+      if (lane == 0) sh.few_key[i] = order_key(s), exact[sh.few[i]] = s;
     }
-    const auto score64 = [&](int cand) {
-      const float* m = p.means + (h * p.ids + id_of(p, cand)) * D + lane;
-      double s = 0.0;
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) s = fma(q[j], static_cast<double>(__ldg(m + 32 * j)), s);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      return s;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n_open; i += THREADS) {   // those that less than `need` are above of, and so on
+      const uint64_t x = sh.few_key[i];
+      int ahead = 0, equal = 0;
+      for (int j = 0; j < n_open; ++j) {
+        ahead += sh.few_key[j] > x;
+        equal += sh.few_key[j] == x;
+      }
+      if (ahead < need && ahead + equal >= need) {   // equal ones write the same
+        sh.few_least = x;
+        sh.few_ties = need - ahead;
+      }
+    }
+    __syncthreads();
+    least = sh.few_least;
+    ties = sh.few_ties;
+  } else {
+    const auto open = [&](int i) {
+      const uint32_t x = order_key(__ldcg(score + i));
+      return x >= low_key && x <= high_key;
     };
-    if (n_open <= kFew) {
-      for (int i = warp; i < n_open; i += P_WARPS) {
-        const double s = score64(few[i]);
-        if (lane == 0) few_key[i] = order_key(s), exact[few[i]] = s;
+    for (int i = warp; i < n; i += W)
+      if (open(i)) {
+        const double s = score64(i);
+        if (lane == 0) exact[i] = s;
       }
-      __syncthreads();
-      if (threadIdx.x < n_open) {   // the one with `need - 1` ahead of it is the last one taken
-        int ahead = 0, equal = 0;
-        for (int j = 0; j < n_open; ++j) {
-          ahead += few_key[j] > few_key[threadIdx.x];
-          equal += few_key[j] == few_key[threadIdx.x];
-        }
-        if (ahead < need && ahead + equal >= need) {
-          few_least = few_key[threadIdx.x];   // equal ones write the same
-          hist[0] = need - ahead;
-        }
-      }
-      __syncthreads();
-      least = few_least;
-      ties = hist[0];
-    } else {
-      for (int i = warp; i < n; i += P_WARPS)
-        if (open(i)) {
-          const double s = score64(i);
-          if (lane == 0) exact[i] = s;
-        }
-      __syncthreads();
-      least = kth_largest<uint64_t>(n, need, [&](int i) { return order_key(exact[i]); }, open, hist, ties);
-    }
+    __syncthreads();
+    least = kth_largest<THREADS>(n, need, [&](int i) { return order_key(exact[i]); }, open, sh.wide, ties);
   }
   // In the order of their numbers: the sure ones, the open ones above `least` and the first `ties` of those at it.
-  const bool all_open = need >= n_open;
-  int done = 0, tied = 0;   // written, and ties met so far
-  for (int i0 = 0; i0 < n; i0 += P_THREADS) {
-    const int i = i0 + threadIdx.x;
-    bool in = false, tie = false;
-    if (i < n) {
-      if (sure(i)) in = true;
-      else if (open(i)) {
-        if (all_open) in = true;
-        else {
-          const uint64_t x = order_key(exact[i]);
-          in = x > least;
-          tie = x == least;
-        }
-      }
-    }
+  const auto key64 = [&](int i, uint32_t x, bool here) {   // 0: not in question (a NaN's, too, where `least` is more)
+    return !here || x < low_key ? 0 : x > high_key ? ~uint64_t{0} : order_key(exact[i]);
+  };
+  const auto asked = [&](uint32_t x, bool here) { return here && x >= low_key; };
+  uint32_t n_above = 0, n_tied = 0;
+  each([&](int i, uint32_t x, bool here) {
+    const uint64_t e = key64(i, x, here);
+    n_above += asked(x, here) && e > least;
+    n_tied += asked(x, here) && e == least;
+  });
+  const uint64_t ahead = warps_before<W>(sh.counts[1], static_cast<uint64_t>(n_tied) << 32 | n_above, all);
+  int tied = static_cast<int>(ahead >> 32);   // ties before this step
+  at = static_cast<int>(ahead) + min(tied, ties);
+  each([&](int i, uint32_t x, bool here) {
+    const uint64_t e = key64(i, x, here);
+    const bool tie = asked(x, here) && e == least;
     const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) counts[0][warp] = __popc(tie_mask);
-    __syncthreads();
-    int rank = tied + __popc(tie_mask & ((1u << lane) - 1u));
-    for (int w = 0; w < P_WARPS; ++w) {
-      if (w < warp) rank += counts[0][w];
-      tied += counts[0][w];
-    }
-    in = in || (tie && rank < ties);
+    const bool in = asked(x, here) && (e > least || (tie && tied + __popc(tie_mask & lower_lanes) < ties));
     const uint32_t mask = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) counts[1][warp] = __popc(mask);
-    __syncthreads();
-    int at = done + __popc(mask & ((1u << lane) - 1u));
-    for (int w = 0; w < P_WARPS; ++w) {
-      if (w < warp) at += counts[1][w];
-      done += counts[1][w];
-    }
-    if (in) out[at] = id_of(p, i);
-  }
+    if (in) out[at + __popc(mask & lower_lanes)] = id_of(p, i);
+    at += __popc(mask);
+    tied += __popc(tie_mask);
+  });
 }
 
 template <int D>
 cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   const dim3 lists(static_cast<unsigned>(p.n_qt), static_cast<unsigned>(p.H));
   if (p.n_cand > p.top_k) {
-    cudaError_t e = launch_pdl(qsum_kernel<D>, lists, dim3(256), 0, s, p);
+    const dim3 tiles(static_cast<unsigned>((p.n_cand + S_CAND - 1) / S_CAND), static_cast<unsigned>(p.H));
+    const auto score = [&](auto kernel, int smem) {
+      const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), smem);
+      return e != cudaSuccess ? e : launch_pdl(kernel, tiles, dim3(S_THREADS), smem, s, p);
+    };
+    cudaError_t e = p.n_qt == 1 ? cudaSuccess : launch_pdl(qsum_kernel<D>, lists, dim3(256), 0, s, p);
     if (e != cudaSuccess) return e;
-    constexpr int smem = (S_CAND + S_QT) * (D + 4) * 4;
-    e = set_smem_limit_once(reinterpret_cast<const void*>(score_kernel<D>), smem);
-    if (e != cudaSuccess) return e;
-    e = launch_pdl(score_kernel<D>, dim3(static_cast<unsigned>((p.n_cand + S_CAND - 1) / S_CAND),
-                                         static_cast<unsigned>(p.H)),
-                   dim3(256), smem, s, p);
+    e = p.n_qt == 1    ? score(score_kernel<D, 1, true>, kScoreSmem<D, 1>)
+        : p.n_qt <= 8  ? score(score_kernel<D, 1, false>, kScoreSmem<D, 1>)
+        : p.n_qt <= 16 ? score(score_kernel<D, 2, false>, kScoreSmem<D, 2>)
+                       : score(score_kernel<D, 5, false>, kScoreSmem<D, 5>);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(pick_kernel<D>, lists, dim3(P_THREADS), 0, s, p);
+  const auto pick = [&](auto kernel, int warps) { return launch_pdl(kernel, lists, dim3(32 * warps), 0, s, p); };
+  const int n = p.n_cand;
+  return n <= 128    ? pick(pick_kernel<D, 1, 4>, 1)
+         : n <= 640  ? pick(pick_kernel<D, 4, 5>, 4)
+         : n <= 1280 ? pick(pick_kernel<D, 8, 5>, 8)
+         : n <= 2560 ? pick(pick_kernel<D, 8, 10>, 8)
+         : n <= 5120 ? pick(pick_kernel<D, 8, 20>, 8)
+                     : pick(pick_kernel<D, 8, 0>, 8);
 }
 
 }  // namespace
@@ -449,7 +698,7 @@ cudaError_t launch_key_means(const MeansParams& p, cudaStream_t s) {
 }
 
 size_t select_ws_bytes(int64_t H, int64_t n_qt, int64_t d, int64_t ids) {
-  return static_cast<size_t>(H) * (n_qt * d * 8 + n_qt * ids * 12 + ids * 4);
+  return static_cast<size_t>(H) * (n_qt * ids * 12 + n_qt * d * 8 + n_qt * 4 + (ids + S_CAND - 1) / S_CAND * 4);
 }
 
 cudaError_t launch_select(const SelectParams& p, cudaStream_t s) {

@@ -263,8 +263,7 @@ struct SelectParams {
   int32_t n_q, n_qt, H, d, top_k;
   int64_t ids;              // capacity * nb
   int32_t n_cand;           // candidates, numbered through the runs
-  int32_t n_runs;
-  int32_t run_end[ISPA_MAX_RANGES];     // candidates up to the end of the run
+  int32_t run_end[ISPA_MAX_RANGES];     // candidates up to the end of the run; INT32_MAX where there is none
   int32_t run_shift[ISPA_MAX_RANGES];   // block number - candidate
 };
 size_t select_ws_bytes(int64_t H, int64_t n_qt, int64_t d, int64_t ids);
