@@ -316,18 +316,32 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 #pragma unroll
   for (int j = 0; j < 4; ++j) step[j] = t + j * threads < p.pairs ? p.steps[t + j * threads] : 0;
   positions(tok);
-  auto copy_weights = [&](const float* from, float4* to, int n) {
+  // codes: with 1 / scale of the key's head in its weights, and none behind the rotation
+  auto copy_weights = [&](const float* from, float4* to, int n, bool codes) {
     for (int k = threadIdx.y * threads + t; k < n / 8; k += threads * teams) {   // vector k of a row
       const int c = k % vecs;
       const Lane<HALF> of(c, p);
       const float* w = from + (k - c) * 8;
-      to[k] = from ? __ldg(reinterpret_cast<const float4*>(w + of.at0)) : make_float4(1.f, 1.f, 1.f, 1.f);
-      to[n / 8 + k] = from ? __ldg(reinterpret_cast<const float4*>(w + of.at1)) : make_float4(1.f, 1.f, 1.f, 1.f);
+      float4 a = from ? __ldg(reinterpret_cast<const float4*>(w + of.at0)) : make_float4(1.f, 1.f, 1.f, 1.f);
+      float4 b = from ? __ldg(reinterpret_cast<const float4*>(w + of.at1)) : make_float4(1.f, 1.f, 1.f, 1.f);
+      if constexpr (kCodes<Params>) {
+        if (codes) {
+          const float inv = __fdiv_rn(1.f, __ldg(p.k_scale + k / vecs));
+          const auto by = [&](float v) {   // finite, so that a key of zero stays one
+            v *= inv;
+            return fabsf(v) == INFINITY ? copysignf(3.402823466e38f, v) : v;
+          };
+          a = make_float4(by(a.x), by(a.y), by(a.z), by(a.w));
+          b = make_float4(by(b.x), by(b.y), by(b.z), by(b.w));
+        }
+      }
+      to[k] = a;
+      to[n / 8 + k] = b;
     }
   };
   if constexpr (kWeights) {
-    copy_weights(p.rows[0].weight, reinterpret_cast<float4*>(smem), n0);
-    if (n1) copy_weights(p.rows[1].weight, reinterpret_cast<float4*>(smem + 4 * n0), n1);
+    copy_weights(p.rows[0].weight, reinterpret_cast<float4*>(smem), n0, true);
+    if (n1) copy_weights(p.rows[1].weight, reinterpret_cast<float4*>(smem + 4 * n0), n1, false);
   }
   __syncthreads();
   const float inv_n0 = 1.f / static_cast<float>(n0), inv_n1 = n1 ? 1.f / static_cast<float>(n1) : 0.f;
@@ -347,7 +361,7 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
   // them, r that factor for what passes
   auto finish = [&](const uint8_t* src, const RopeRowsParams& o, const float4* planes, int n, const float2* cs, float r,
                     bool first) {
-    // keys (the first tensor) that go into the ring: head 0 of the token, and the step from one head to the next (values, or codes)
+    // keys (the first tensor) that go into the ring: head 0 of the token, and the step from one head to the next
     uint8_t* codes = nullptr;
     int64_t step_out = heads_step * d;
     const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(src) + head0 * d;
@@ -405,7 +419,7 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
       }
       if (kCodes<Params> && first) {
         if constexpr (kCodes<Params>)
-          if (here) store_codes(codes, ln, f, __fdiv_rn(1.f, __ldg(p.k_scale + h)));
+          if (here) store_codes(codes, ln, f, kWeights ? 1.f : __fdiv_rn(1.f, __ldg(p.k_scale + h)));
         codes += step_out;
       } else {
         if (here) ln.store(out, f);
@@ -479,7 +493,7 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 
 // The values of many tokens, in a launch of their own in front of the keys', which starts as soon as this one's blocks
 // have the kernel before behind them and runs beside it.  In the teams' loop the copies cost their registers: 4680
-// tokens of 3 x 5120 with 8-bit keys 83 us against 62, of 3 x 1536 25.6 against 20.
+// tokens of 3 x 5120 with 8-bit keys 83 us against 57, of 3 x 1536 25.6 against 20.
 __global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ RopeAppendParams p, int per_block) {
   pdl_wait();
   pdl_trigger();
