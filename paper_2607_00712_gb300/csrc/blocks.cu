@@ -188,14 +188,16 @@ __device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float
   if (threadIdx.x == 0) ws.norm[list] = sqrtf(s);
 }
 
+constexpr int Q_THREADS = 256;
 template <int D>
-__global__ void __launch_bounds__(256) qsum_kernel(const __grid_constant__ SelectParams p) {
-  __shared__ QSum<D, 256> sum;
+__global__ void __launch_bounds__(Q_THREADS) qsum_kernel(const __grid_constant__ SelectParams p) {
+  __shared__ QSum<D, Q_THREADS> sum;
   __shared__ float red[2][32];
   const int qt = blockIdx.x, h = blockIdx.y;
   pdl_wait();
   pdl_trigger();
-  keep_sum<D>(ws_of(p.ws, p.H, p.n_qt, D, p.n_cand), static_cast<int64_t>(h) * p.n_qt + qt, sum.of(p, h, qt), red, 8);
+  keep_sum<D>(ws_of(p.ws, p.H, p.n_qt, D, p.n_cand), static_cast<int64_t>(h) * p.n_qt + qt, sum.of(p, h, qt), red,
+              Q_THREADS / 32);
 }
 
 // 32-bit scores: a tile of 64 candidates x 8 J query blocks of one head in shared memory, 2 x J a thread.  A warp's
@@ -670,7 +672,7 @@ cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
       const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), smem);
       return e != cudaSuccess ? e : launch_pdl(kernel, tiles, dim3(S_THREADS), smem, s, p);
     };
-    cudaError_t e = p.n_qt == 1 ? cudaSuccess : launch_pdl(qsum_kernel<D>, lists, dim3(256), 0, s, p);
+    cudaError_t e = p.n_qt == 1 ? cudaSuccess : launch_pdl(qsum_kernel<D>, lists, dim3(Q_THREADS), 0, s, p);
     if (e != cudaSuccess) return e;
     e = p.n_qt == 1    ? score(score_kernel<D, 1, true>, kScoreSmem<D, 1>)
         : p.n_qt <= 8  ? score(score_kernel<D, 1, false>, kScoreSmem<D, 1>)
@@ -681,7 +683,7 @@ cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   const auto pick = [&](auto kernel, int warps) { return launch_pdl(kernel, lists, dim3(32 * warps), 0, s, p); };
   const int n = p.n_cand;
   return n <= 128    ? pick(pick_kernel<D, 1, 4>, 1)
-         : n <= 640  ? pick(pick_kernel<D, 4, 5>, 4)
+         : n <= 768  ? pick(pick_kernel<D, 4, 6>, 4)
          : n <= 1280 ? pick(pick_kernel<D, 8, 5>, 8)
          : n <= 2560 ? pick(pick_kernel<D, 8, 10>, 8)
          : n <= 5120 ? pick(pick_kernel<D, 8, 20>, 8)
