@@ -218,7 +218,7 @@ ISPA_API ispa_status ispa_debug_set_heartbeat(uint32_t* counters, int32_t n_slot
  *   16 + w, 24 + w     softmax warp w (0-7): P_j arrived, S_j seen;
  *   12-15 of tile 0    once: kernel entry, TMEM allocated, Q tile landed,
  *                      epilogue stored.
- * NULL / 0 turns it off (the default). */
+ * Calls with listed blocks record nothing.  NULL / 0 turns it off (the default). */
 ISPA_API ispa_status ispa_debug_set_trace(uint64_t* buf, int32_t n_tiles);
 
 /* Debug aid for the timeout path: while tile >= 0, the TMA thread of every attention CTA

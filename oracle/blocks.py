@@ -54,12 +54,14 @@ def select(score, candidates, top_k):
     return out
 
 
-def attend(q, k, v, slots, lists, P, block, k_cur=None, v_cur=None, scale=None, frame_causal=False, residents=None):
+def attend(q, k, v, slots, lists, P, block, k_cur=None, v_cur=None, scale=None, frame_causal=False, residents=None,
+           queries=None):
     """q [n][H][d]; k, v [H][slots * P][d]; slots of the window; lists [H][query blocks][top_k].
 
     residents: block numbers below this name keys (the ring's resident ones); the first min(top_k, residents) entries
-    of a list count.  Returns out [n][H][d], lse [H][n], and for error bounds spread [n][H][d] = sum_i w_i |v_i|,
-    reach [H][n] = the largest sum_c |q_c k_c| scale of a row's keys, and the number of keys [H][n].
+    of a list count.  queries: those that are wanted (the others' results stay zero); None: all.  Returns
+    out [n][H][d], lse [H][n], and for error bounds spread [n][H][d] = sum_i w_i |v_i|, reach [H][n] = the largest
+    sum_c |q_c k_c| scale of a row's keys, and the number of keys [H][n].
     """
     q = np.asarray(q, np.float64)
     k, v = np.asarray(k, np.float64), np.asarray(v, np.float64)
@@ -78,6 +80,8 @@ def attend(q, k, v, slots, lists, P, block, k_cur=None, v_cur=None, scale=None, 
             here = slice(i * QUERIES, min(n, (i + 1) * QUERIES))
             kk, vv = k[h, rows], v[h, rows]
             for t in range(here.start, here.stop):
+                if queries is not None and t not in queries:
+                    continue
                 kt, vt = kk, vv
                 if k_cur is not None:
                     end = (t // P + 1) * P if frame_causal else len(k_cur)

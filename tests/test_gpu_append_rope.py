@@ -53,7 +53,8 @@ class Call:
         self.pos0 = pos0
         self.steps_t = _device_steps(steps)
         self.rope = abi.rope(layout, d, axis_pairs, self.steps_t, factor)
-        self.angle, self.factor, self.half = ol.angles(self.pos, pos0, axis_pairs, steps), factor, layout == abi.ISPA_ROPE_HALF
+        self.angle, self.factor = ol.angles(self.pos, pos0, axis_pairs, steps), factor
+        self.half = layout == abi.ISPA_ROPE_HALF
         self.w = [_weight(seed + i, h, d, m) for i, (h, m) in enumerate(zip((hq, H), norms))]
         self.wt = [None if w is None else torch.from_numpy(w).cuda() for w in self.w]
         self.ks = ((0.5 + g.random(H)) * 0.02).astype(np.float32)      # some keys are cut off
@@ -71,7 +72,8 @@ class Call:
             q = abi.rope_rows(self.x, self.x if self.in_place else self.q_out, hq, W, W if self.in_place else hq * d,
                               self.norms[0], self.wt[0], EPS)
         abi.ispa_kv_append_rope(self.ring.c, self.rope, k, q, self.x[:, (hq + H) * d:], W, self.pos_t, self.pos0,
-                                self.frames, self.ks_t if self.fmt else None, self.vs_t if self.fmt == 2 else None, stream)
+                                self.frames, self.ks_t if self.fmt else None, self.vs_t if self.fmt == 2 else None,
+                                stream)
         return self
 
     def check(self):
@@ -84,15 +86,16 @@ class Call:
         at = torch.from_numpy(at).cuda()
         # queries
         if hq:
-            want, bound = _expected(self.host[:, :hq * d], hq, d, self.norms[0], self.w[0], self.angle, self.factor, self.half)
+            want, bound = _expected(self.host[:, :hq * d], hq, d, self.norms[0], self.w[0], self.angle, self.factor,
+                                    self.half)
             got = self.x[:, :hq * d].reshape(n, hq, d) if self.in_place else self.q_out[:n]
             lh.assert_within(got.float().cpu().numpy(), want, bound, "q")
             assert (self.q_out[n] == 7.0).all()
         keep = hq * d if self.in_place else 0
         assert torch.equal(self.x[:, keep:], x0[:, keep:])
         # keys
-        want, bound = _expected(self.host[:, hq * d:(hq + H) * d], H, d, self.norms[1], self.w[1], self.angle, self.factor,
-                                self.half)
+        want, bound = _expected(self.host[:, hq * d:(hq + H) * d], H, d, self.norms[1], self.w[1], self.angle,
+                                self.factor, self.half)
         want, bound = want.transpose(1, 0, 2), bound.transpose(1, 0, 2)
         got = self.ring.k[:, at]
         if self.fmt:
@@ -132,7 +135,8 @@ def test_formats_norms_and_sizes(fmt, norms, P, frames):
 
 
 @pytest.mark.parametrize("layout", [abi.ISPA_ROPE_INTERLEAVED, abi.ISPA_ROPE_HALF])
-@pytest.mark.parametrize("hq,H,d,pairs", [(0, 1, 64, [32]), (1, 1, 64, [16]), (8, 2, 128, [24, 20, 20]), (0, 12, 128, [32]),
+@pytest.mark.parametrize("hq,H,d,pairs", [(0, 1, 64, [32]), (1, 1, 64, [16]), (8, 2, 128, [24, 20, 20]),
+                                          (0, 12, 128, [32]),
                                           (5, 5, 128, [4]), (24, 8, 64, [32]), (40, 40, 128, [24, 20, 20])])
 @pytest.mark.parametrize("P", [1, 333])
 def test_shapes(layout, hq, H, d, pairs, P):
@@ -141,7 +145,8 @@ def test_shapes(layout, hq, H, d, pairs, P):
 
 
 @pytest.mark.parametrize("fmt", [0, 1, 2])
-@pytest.mark.parametrize("cap,sinks,written,frames", [(3, 0, 0, 1), (3, 0, 2, 3), (5, 1, 4, 4), (17, 0, 40, 16), (4, 2, 1, 2),
+@pytest.mark.parametrize("cap,sinks,written,frames", [(3, 0, 0, 1), (3, 0, 2, 3), (5, 1, 4, 4), (17, 0, 40, 16),
+                                                      (4, 2, 1, 2),
                                                       (2, 0, 10 ** 12 + 1, 1)])
 def test_ring_positions(fmt, cap, sinks, written, frames):
     Call(20, frames, 2, 2, 128, [64], abi.ISPA_ROPE_HALF, (HEAD, HEAD), fmt, cap, sinks, written).run().check()
@@ -149,8 +154,8 @@ def test_ring_positions(fmt, cap, sinks, written, frames):
 
 def test_far_positions_and_scaling():
     pos = np.array([[2 ** 31 - 1 - i for i in range(40)]])
-    Call(40, 1, 2, 2, 128, [64], abi.ISPA_ROPE_HALF, (NONE, NONE), pos=pos, pos0=2 ** 40, scaling=abi.ISPA_ROPE_SCALE_PARTS,
-         scale=8.0, trained_length=32768.0).run().check()
+    Call(40, 1, 2, 2, 128, [64], abi.ISPA_ROPE_HALF, (NONE, NONE), pos=pos, pos0=2 ** 40,
+         scaling=abi.ISPA_ROPE_SCALE_PARTS, scale=8.0, trained_length=32768.0).run().check()
 
 
 def test_queries_in_place():

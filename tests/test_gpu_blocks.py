@@ -79,7 +79,8 @@ class Cache:
 
 # ---------------------------------------------------------------- means
 @pytest.mark.parametrize("H,d,P,block,e4m3", [(1, 64, 1, 64, False), (2, 128, 63, 64, False), (3, 128, 65, 64, False),
-                                              (2, 64, 1000, 192, False), (2, 128, 1560, 64, False), (2, 128, 130, 512, False),
+                                              (2, 64, 1000, 192, False), (2, 128, 1560, 64, False),
+                                              (2, 128, 130, 512, False),
                                               (2, 128, 1, 64, True), (3, 128, 333, 64, True), (1, 128, 1560, 128, True),
                                               (2, 128, 777, 512, True)])
 def test_means(H, d, P, block, e4m3):
@@ -130,7 +131,11 @@ def _select(c, win, block, means, q, top_k, ring=None):
     (1, 1, 64, 64, 64, 3, 3, 0, (0, 0), 1), (1, 12, 128, 1560, 64, 57, 57, 0, (1, 6), 64),
     (129, 2, 128, 100, 64, 9, 14, 1, (1, 2), 5), (300, 3, 64, 333, 128, 20, 45, 0, (0, 3), 17),
     (4680, 2, 128, 1560, 64, 24, 24, 0, (1, 6), 128), (260, 2, 128, 1, 64, 50, 120, 2, (2, 1), 40),
-    (128, 1, 128, 64, 64, 3000, 3000, 0, (0, 0), 100), (200, 2, 64, 640, 64, 5, 5, 0, (0, 0), 49)])
+    (128, 1, 128, 64, 64, 3000, 3000, 0, (0, 0), 100), (200, 2, 64, 640, 64, 5, 5, 0, (0, 0), 49),
+    # 16, 9 and 74 query blocks
+    (2000, 1, 128, 700, 64, 9, 9, 0, (0, 0), 20), (1030, 2, 64, 64, 64, 129, 129, 0, (0, 0), 90),
+    (9400, 1, 128, 64, 64, 70, 200, 0, (0, 5), 7), (100, 1, 64, 64, 64, 2000, 2000, 1, (1, 3), 1900),
+    (300, 1, 64, 64, 64, 7001, 7001, 0, (0, 0), 333), (1, 2, 128, 128, 64, 3000, 9999, 0, (0, 2), 5999)])
 def test_selection(n, H, d, P, block, cap, written, sinks, win, top_k):
     c = Cache(n + P, H, d, P if P * cap < 20000 else 1, 1)
     ring = abi.KVRing(H, d, P, cap, sinks, 0, written, 16, 16)     # no key is read
@@ -155,11 +160,14 @@ def test_fewer_candidates_than_asked_for(cand, top_k):
     assert (got == np.array(want)).all()
 
 
-@pytest.mark.parametrize("values,top_k", [("same", 10), ("zero", 10), ("few", 33), ("few", 100), ("pairs", 7), ("nan", 30),
+@pytest.mark.parametrize("frames", [20, 80, 1400])
+@pytest.mark.parametrize("values,top_k", [("same", 10), ("zero", 10), ("few", 33), ("few", 100), ("pairs", 7),
+                                          ("nan", 30),
                                           ("inf", 30), ("nan", 310), ("huge", 40), ("tiny", 40), ("close", 50)])
-def test_equal_close_and_extreme_scores(values, top_k):
+def test_equal_close_and_extreme_scores(values, top_k, frames):
     """Small whole numbers, whose scores are exact in any order, and values at the ends of the range."""
-    H, d, P, cap, n = 2, 64, 64 * 4, 80, 200
+    H, d, P, cap, n = 2, 64, 64 * 4, frames, 200
+    top_k = min(top_k, 4 * cap - 1)
     c = Cache(9, H, d, 1, 1)
     ring = abi.KVRing(H, d, P, cap, 0, 0, cap, 16, 16)
     g = np.random.default_rng(4)
@@ -292,6 +300,25 @@ def test_frame_causal(d, P, frames):
     Step(5, c, n).check(c, (0, 1), 64, _lists(8, c, (0, 1), 64, n, 4, True), causal=True)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n,H,win,top_k", [(500, 40, (0, 2), 40), (640, 1, (0, 0), 60), (1, 2, (0, 4), 60)])
+def test_long_items_split_over_clusters(n, H, win, top_k, e4m3):
+    """More items than SMs whose last wave is split, few items, one query: lists and dense tiles over several CTAs."""
+    c = Cache(3, H, 128, 1560, 5, e4m3=e4m3)
+    s = Step(6, c, n)
+    lists = _lists(2, c, win, 64, n, top_k)
+    out, lse = s.run(c, win, 64, lists)
+    _ok()
+    rows = {0, n // 2, n - 1}
+    nb = ob.per_frame(c.P, 64)
+    want = ob.attend(s.q, c.k, c.v, c.window(win), lists, c.P, 64, s.kc, s.vc, residents=5 * nb,
+                     queries=rows)
+    b_out, b_lse = ob.bounds(*want, 128)
+    at = sorted(rows)
+    lh.assert_within(to_f32(out[:n])[at], want[0][at], b_out[at], "out")
+    lh.assert_within(lse[:-1].view(H, n).cpu().numpy()[:, at], want[1][:, at], b_lse[:, at], "lse")
+
+
 def test_rows_that_see_nothing():
     for n, d, e4m3 in ((1, 128, False), (129, 64, False), (300, 128, True)):
         c = Cache(n, 2, d, 80, 5, e4m3=e4m3)
@@ -408,8 +435,8 @@ def test_a_rollout(e4m3):
         pos = torch.arange(step * n, step * n + n, device="cuda", dtype=torch.int32)
         W = 3 * H * d
         # the chunk's queries and keys for the attention; then the keys into the ring
-        abi.ispa_rope_apply(rope, [abi.rope_rows(x, q, H, W, H * d), abi.rope_rows(x[:, H * d:], turned, H, W, H * d)], pos,
-                            0, n)
+        both = [abi.rope_rows(x, q, H, W, H * d), abi.rope_rows(x[:, H * d:], turned, H, W, H * d)]
+        abi.ispa_rope_apply(rope, both, pos, 0, n)
         v = x[:, 2 * H * d:].reshape(n, H, d).contiguous()
         abi.ispa_select_blocks(c.ring.c, Window(*win), block, means, q, n, top_k, blocks, ws, size)
         out = torch.empty(n, H * d, dtype=torch.bfloat16, device="cuda")
@@ -417,8 +444,8 @@ def test_a_rollout(e4m3):
         if e4m3:
             abi.ispa_quantize_q_e4m3(q, n, H, d, q8, qs)
             abi.ispa_quantize_k_e4m3(turned, n, H, d, c.ks_t, kc8)
-            abi.ispa_attn_blocks_qk8(c.ring.c, c.ks_t, Window(*win), block, blocks, top_k, q8, qs, kc8, c.ks_t, v, n, 0.0,
-                                     out, lse)
+            abi.ispa_attn_blocks_qk8(c.ring.c, c.ks_t, Window(*win), block, blocks, top_k, q8, qs, kc8, c.ks_t, v, n,
+                                     0.0, out, lse)
         else:
             abi.ispa_attn_blocks(c.ring.c, Window(*win), block, blocks, top_k, q, turned, v, n, 0.0, 0, out, lse)
         _ok()
@@ -437,15 +464,15 @@ def test_a_rollout(e4m3):
         assert np.array_equal(blocks.cpu().numpy(), want_b)
         qd, kd = qh, to_f32(turned)
         if e4m3:
-            qd = oq.decode(q8.cpu().numpy()) * np.repeat(qs.cpu().numpy(), 128, 1)[:, :n].T[:, :, None].astype(np.float64)
+            qd = oq.dequantize_query_blocks(q8.cpu().numpy(), qs.cpu().numpy())
             kd = oq.decode(kc8.cpu().numpy()) * c.k_scale.astype(np.float64)[None, :, None]
         want = ob.attend(qd, c.k, c.v, c.window(win), want_b, P, block, kd, to_f32(v), None, False,
                          min(c.written, cap) * nb)
         b_out, b_lse = ob.bounds(*want, d)
         lh.assert_within(to_f32(out).reshape(n, H, d), want[0], b_out, f"step {step}")
         lh.assert_within(lse.cpu().numpy(), want[1], b_lse, f"step {step}")
-        abi.ispa_kv_append_rope(c.ring.c, rope, abi.rope_rows(x[:, H * d:], None, H, W, 0), None, x[:, 2 * H * d:], W, pos,
-                                0, chunk, c.ks_t if e4m3 else None)
+        abi.ispa_kv_append_rope(c.ring.c, rope, abi.rope_rows(x[:, H * d:], None, H, W, 0), None, x[:, 2 * H * d:], W,
+                                pos, 0, chunk, c.ks_t if e4m3 else None)
         abi.ispa_key_means(c.ring.c, c.ks_t if e4m3 else None, c.ring.frames_written - chunk, chunk, block, means)
     _ok()
 
@@ -466,7 +493,8 @@ def test_captured_run_of_all_and_two_streams():
 
     def calls(c, s, stream):
         abi.ispa_key_means(c.ring.c, None, 0, 6, block, c.means, stream)
-        abi.ispa_select_blocks(c.ring.c, Window(*win), block, c.means, s.q_t, n, top_k, c.blocks, c.ws, c.ws.numel(), stream)
+        abi.ispa_select_blocks(c.ring.c, Window(*win), block, c.means, s.q_t, n, top_k, c.blocks, c.ws, c.ws.numel(),
+                               stream)
         out, lse = torch.empty(n, H * d, dtype=torch.bfloat16, device="cuda"), torch.empty(H, n, device="cuda")
         abi.ispa_attn_blocks(c.ring.c, Window(*win), block, c.blocks, top_k, s.q_t, s.kc_t, s.vc_t, n, 0.0, 0, out, lse,
                              stream)
@@ -499,7 +527,8 @@ def test_captured_run_of_all_and_two_streams():
         graph.replay()
         _ok()
         assert all(torch.equal(a, b) for a, b in zip(got, eager[seed]))
-        for x, y in ((c.ring.k, other.ring.k), (c.ring.v, other.ring.v), (s.q_t, t.q_t), (s.kc_t, t.kc_t), (s.vc_t, t.vc_t)):
+        for x, y in ((c.ring.k, other.ring.k), (c.ring.v, other.ring.v), (s.q_t, t.q_t), (s.kc_t, t.kc_t),
+                     (s.vc_t, t.vc_t)):
             keep = x.clone()
             x.copy_(y), y.copy_(keep)
 
