@@ -37,7 +37,9 @@ __device__ __forceinline__ void add16(const uint4& w, float* s) {
   }
 }
 
-// A block of the grid: block blockIdx.x of the frames' blocks, head blockIdx.y.  A row's LPR lanes take 16 bytes each.
+// A block of the grid: block blockIdx.x of the frames' blocks, head blockIdx.y.  A row's LPR lanes take 16 bytes each,
+// eight rows apart on their way at once.  HBM bounds it: the 455 MB of 57 frames of 1560 tokens x 40 heads in 8 bits,
+// blocks of 128, in 78 us, 6.0 TB/s with the means' 15 MB (89 % of the copy rate; issue slots 74 %).
 template <bool E4M3, int D>
 __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant__ MeansParams p) {
   constexpr int VALS = E4M3 ? 16 : 8, LPR = D / VALS, ROWS = M_THREADS / LPR;
@@ -95,6 +97,10 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------ selection
+// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 31 us
+// where reading once takes 3.3; the launches' latency bounds it (6, 10 and 10 us each by itself, of which 2 are a
+// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 43 to 48 %).  One query: 11 us, two
+// kernels, the sum in the scoring one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
 // 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
 // multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
