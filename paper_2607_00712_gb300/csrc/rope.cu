@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(1024, 1) rope_stream_kernel(const __grid_const
 
 // The values of many tokens, in a launch of their own in front of the keys', which starts as soon as this one's blocks
 // have the kernel before behind them and runs beside it.  In the teams' loop the copies cost their registers: 4680
-// tokens of 3 x 5120 with 8-bit keys 83 us against 57, of 3 x 1536 25.6 against 20.
+// tokens of 3 x 5120 with 8-bit keys 83 us against 50, of 3 x 1536 25.6 against 20.
 __global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ RopeAppendParams p, int per_block) {
   pdl_wait();
   pdl_trigger();
@@ -504,7 +504,14 @@ __global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ Rop
 template <bool HALF, typename Params>
 cudaError_t launch_layout(const Params& p, int sms, cudaStream_t s) {
   const int32_t heads[2] = {p.rows[0].heads, p.rows[1].heads}, norms[2] = {p.rows[0].norm, p.rows[1].norm};
-  const RopeForm f = rope_form(p.n, p.n_rows, heads, norms, p.head_dim, p.pairs, p.lanes_per_head, HALF, sms);
+  RopeForm f = rope_form(p.n, p.n_rows, heads, norms, p.head_dim, p.pairs, p.lanes_per_head, HALF, sms);
+  if constexpr (kRing<Params>) {
+    // Teams that have several tokens each make room for the values' block (see below): 4680 x 40 heads, norm per head,
+    // 60 us with 25 warps and the values in front, 56 with 20 beside them; not without a norm (51 both ways), where
+    // there is less to wait for.
+    if (f.stream && p.v && norms[0] != ISPA_QK_NORM_NONE && f.tokens > f.teams && f.warps * f.teams > 24)
+      f.teams = std::max(1, 24 / f.warps);
+  }
   if (f.stream) {
     const auto go = [&](auto kernel) {
       cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), R_SMEM);
@@ -513,7 +520,11 @@ cudaError_t launch_layout(const Params& p, int sms, cudaStream_t s) {
       if constexpr (kRing<Params>) {
         q.wait_first = p.v == nullptr;
         if (p.v) {
-          const int per = static_cast<int>((p.n + 8 * sms - 1) / (8 * sms));
+          // One block an SM where the keys' block leaves it room, so that both go on side by side: of a lane's 512
+          // registers in a quarter of an SM, six warps with the keys' 64 and two with the 40 here (4680 x 40 heads, 20
+          // warps, 50 us, 56 with eight blocks; with 25 warps 82 against 50), else as many as get through fastest.
+          const bool beside = f.warps * f.teams <= 24;
+          const int blocks = beside ? sms : 8 * sms, per = static_cast<int>((p.n + blocks - 1) / blocks);
           e = launch_pdl(values_kernel, dim3(static_cast<unsigned>((p.n + per - 1) / per)), dim3(256), 0, s, p, per);
           if (e != cudaSuccess) return e;
         }
