@@ -1132,10 +1132,11 @@ ispa_status ispa_select_blocks(const ispa_kv_ring* ring, ispa_window win, int32_
   if (n_q <= 0 || top_k <= 0 || block <= 0 || !aligned16(means) || !aligned16(q) || !aligned4(blocks))
     return ISPA_ERR_INVALID_ARG;
   if ((st = check_blocks(ring, block)) != ISPA_OK) return st;
+  const size_t need = ispa_select_blocks_workspace_size(ring, block, n_q);
+  if (need == 0) return ISPA_ERR_UNSUPPORTED;
+  if (!aligned16(workspace) || ws_bytes < need) return ISPA_ERR_WORKSPACE;
   ispa_key_sets ks;
   if ((st = resolve(ring, win, &ks)) != ISPA_OK) return st;
-  if (!aligned16(workspace) || ws_bytes < ispa_select_blocks_workspace_size(ring, block, n_q))
-    return ISPA_ERR_WORKSPACE;
   SelectParams p = {};
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.means = means;

@@ -706,6 +706,7 @@ cudaError_t launch_key_means(const MeansParams& p, cudaStream_t s) {
 }
 
 size_t select_ws_bytes(int64_t H, int64_t n_qt, int64_t d, int64_t ids) {
+  if (static_cast<double>(H) * n_qt * (ids + d) > 1e17) return 0;   // far past any memory, and no overflow below
   return static_cast<size_t>(H) * (n_qt * ids * 12 + n_qt * d * 8 + n_qt * 4 + (ids + S_CAND - 1) / S_CAND * 4);
 }
 

@@ -99,6 +99,9 @@ def test_select_workspace():
     size = abi.ispa_select_blocks_workspace_size
     assert size(ring, 64, 1) > 0 and size(ring, 64, 128) == size(ring, 64, 1) < size(ring, 64, 129)
     assert size(ring, 128, 1) < size(ring, 64, 1)
+    huge = _ring(H=65535, P=1, cap=2 ** 31 - 1, F=1)
+    assert size(huge, 64, 2 ** 31 - 1) == 0
+    assert _status(lambda: abi.ispa_select_blocks(huge, Window(0, 1), 64, 16, 16, 2 ** 31 - 1, 4, 16, 16, 2 ** 62)) == UNSUP
     assert size(ring, 63, 1) == 0 and size(ring, 64, 0) == 0 and size(_ring(d=1), 64, 1) == 0
 
 
