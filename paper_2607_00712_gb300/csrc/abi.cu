@@ -410,11 +410,7 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
   ispa_status st = check_ring(ring);
   if (st != ISPA_OK) return st;
   const bool has_chunk = !blocks || k_cur || v_cur;
-  if (!has_chunk) {   // stands in for the chunk's maps, which no tile uses
-    k_cur = ring->k;
-    v_cur = ring->v;
-    if (flags) return ISPA_ERR_INVALID_ARG;
-  }
+  if (!has_chunk && flags) return ISPA_ERR_INVALID_ARG;
   if ((ring->k_format != ISPA_KV_BF16) != (qk8 != nullptr)) return ISPA_ERR_INVALID_ARG;
   if (qk8 && (!qk8->q || (!qk8->k_cur && has_chunk) || !qk8->k_ring)) return ISPA_ERR_INVALID_ARG;
   const bool kv8 = ring->k_format == ISPA_KV_KV_E4M3;
@@ -422,7 +418,7 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
   if (!kv8 && qk8 && qk8->v) return ISPA_ERR_INVALID_ARG;   // 8-bit P V needs a ring with e4m3 values
   if (flags & ~static_cast<uint32_t>(ISPA_ATTN_FRAME_CAUSAL)) return ISPA_ERR_INVALID_ARG;
   if ((flags & ISPA_ATTN_FRAME_CAUSAL) && n_q % ring->tokens_per_frame != 0) return ISPA_ERR_INVALID_ARG;
-  if (n_q <= 0 || !aligned16(q) || !aligned16(k_cur) || !aligned16(v_cur) || !aligned16(out) ||
+  if (n_q <= 0 || !aligned16(q) || (has_chunk && (!aligned16(k_cur) || !aligned16(v_cur))) || !aligned16(out) ||
       !aligned16(ring->k) || !aligned16(ring->v))
     return ISPA_ERR_INVALID_ARG;
   if (mode == MODE_DUAL && (!aligned16(out_loc) || !disc_part)) return ISPA_ERR_INVALID_ARG;
@@ -522,6 +518,7 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
   const uint32_t box_q[4] = {64, static_cast<uint32_t>(kAttnBM), nb, 1};
   const uint32_t box_k[4] = {64, static_cast<uint32_t>(bn), nb, 1};
   CUtensorMap tq, tkr, tvr, tkc, tvc;
+  const bool has_ring = !blocks || ks.n_local > 0;   // dense tiles of it; a map that no tile uses isn't made
   bool ok;
   if (kv8) {
     // d-major e4m3 values [H][128][keys]: boxes of 128 keys x 128 rows, 128-byte swizzle (the
@@ -533,7 +530,8 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
                            1);
     p.v_scale = qk8->v;
   } else {
-    ok = encode_tmap_4d(&tvc, v_cur, dims_c, str_c, box_k) && encode_tmap_4d(&tvr, ring->v, dims_r, str_r, box_k);
+    ok = (!has_chunk || encode_tmap_4d(&tvc, v_cur, dims_c, str_c, box_k)) &&
+         (!has_ring || encode_tmap_4d(&tvr, ring->v, dims_r, str_r, box_k));
   }
   if (qk8) {
     // e4m3 Q and K: a token's 128 features are one 128-byte row, so the column-block
@@ -545,14 +543,15 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
     const uint32_t box_q8[4] = {128, static_cast<uint32_t>(kAttnBM), 1, 1};
     const uint32_t box_k8[4] = {128, static_cast<uint32_t>(kAttnBN), 1, 1};
     ok = ok && encode_tmap_4d(&tq, q, dims_c8, str_c8, box_q8, true) &&
-         encode_tmap_4d(&tkc, k_cur, dims_c8, str_c8, box_k8, true) &&
-         encode_tmap_4d(&tkr, ring->k, dims_r8, str_r8, box_k8, true);
+         (!has_chunk || encode_tmap_4d(&tkc, k_cur, dims_c8, str_c8, box_k8, true)) &&
+         (!has_ring || encode_tmap_4d(&tkr, ring->k, dims_r8, str_r8, box_k8, true));
     p.q_scale = qk8->q;
     p.kc_scale = has_chunk ? qk8->k_cur : qk8->k_ring;
     p.kr_scale = qk8->k_ring;
   } else {
-    ok = ok && encode_tmap_4d(&tq, q, dims_c, str_c, box_q) && encode_tmap_4d(&tkc, k_cur, dims_c, str_c, box_k) &&
-         encode_tmap_4d(&tkr, ring->k, dims_r, str_r, box_k);
+    ok = ok && encode_tmap_4d(&tq, q, dims_c, str_c, box_q) &&
+         (!has_chunk || encode_tmap_4d(&tkc, k_cur, dims_c, str_c, box_k)) &&
+         (!has_ring || encode_tmap_4d(&tkr, ring->k, dims_r, str_r, box_k));
   }
   if (ok && blocks) {
     const auto frames = [&](CUtensorMap* m, const void* base, uint64_t row, bool u8) {
@@ -563,6 +562,8 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
       return encode_tmap_4d(m, base, dims, str, box, u8);
     };
     ok = frames(&lists.k, ring->k, qk8 ? 128 : row_b, qk8 != nullptr) && frames(&lists.v, ring->v, row_b, false);
+    if (!has_ring) tkr = lists.k, tvr = lists.v;   // the kernel prefetches all of them
+    if (!has_chunk) tkc = tkr, tvc = tvr;
   }
   if (!ok) return ISPA_ERR_CUDA;
   if (launch_attention(HD, &tq, &tkr, &tvr, &tkc, &tvc, p, stream, blocks ? &lists : nullptr) != cudaSuccess)
