@@ -496,6 +496,18 @@ ispa_status attn_common(Mode mode, const ispa_kv_ring* ring, ispa_window win, co
   p.lse = lse;
   p.lse_loc = lse_loc;
   p.disc_part = disc_part;
+  if (blocks && n_q <= kFewQueries && p.causal_p == 0) {
+    if (qk8) {
+      p.q_scale = qk8->q;
+      p.kr_scale = qk8->k_ring;
+      p.kc_scale = has_chunk ? qk8->k_cur : qk8->k_ring;
+    }
+    return launch_attention_few(HD, p, lists, q, ring->k, ring->v, k_cur, v_cur,
+                                static_cast<int64_t>(ring->capacity_frames) * P, stream) == cudaSuccess
+               ? ISPA_OK
+               : ISPA_ERR_CUDA;
+  }
+
   p.status = device_status_ptr();
   if (!p.status) return ISPA_ERR_CUDA;
   p.heartbeat = next_heartbeat_slot(1);

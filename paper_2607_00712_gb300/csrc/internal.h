@@ -105,6 +105,11 @@ cudaError_t launch_attention(int head_dim, const CUtensorMap* tm_q, const CUtens
                              const CUtensorMap* tm_vr, const CUtensorMap* tm_kc,
                              const CUtensorMap* tm_vc, const AttnParams& p, cudaStream_t s,
                              const AttnLists* lists = nullptr);
+// The same over segments and lists for up to kFewQueries queries, chunk not causal, without tensor maps (few.cu).
+constexpr int kFewQueries = 2;
+cudaError_t launch_attention_few(int head_dim, const AttnParams& a, const AttnLists& lists, const void* q,
+                                 const void* k_ring, const void* v_ring, const void* k_cur, const void* v_cur,
+                                 int64_t ring_tok, cudaStream_t s);
 // disc[t] = sqrt(sum_h part[h][t]); *disc_sq_sum += sum_t sum_h part[h][t]
 cudaError_t launch_disc_reduce(const float* part, int32_t H, int32_t n_q, float* disc,
                                float* disc_sq_sum, cudaStream_t s);
