@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "pdl.cuh"
@@ -97,10 +98,10 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------ selection
-// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 31 us
-// where reading once takes 3.3; the launches' latency bounds it (6, 10 and 10 us each by itself, of which 2 are a
-// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 43 to 48 %).  One query: 11 us, two
-// kernels, the sum in the scoring one.
+// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 27 us
+// where reading once takes 3.3; the launches' latency bounds it (6, 8 and 9 us each by itself, of which 2 are a
+// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 43 to 48 %).  One query block: one
+// kernel, one query 8.4 us (select_one_kernel); few heads with many candidates two, the sum in the scoring one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
 // 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
 // multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
@@ -175,6 +176,7 @@ struct QSum {
     if (threadIdx.x < D) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
+        if (r >= n) break;
         const float2 v = part[r][threadIdx.x];
         two_sum(a, b, v.x);
         b += v.y;
@@ -230,11 +232,17 @@ __global__ void __launch_bounds__(S_THREADS) score_kernel(const __grid_constant_
   if constexpr (OWN) pdl_wait();
   const uint32_t m_at = smem_u32(m), q_at = smem_u32(q);
   const float4* const means = reinterpret_cast<const float4*>(p.means) + h * p.ids * VPR;
+  {
+    constexpr int ROWS = S_THREADS / VPR, N = S_CAND / ROWS;   // rows at a time; one lane looks up one number
+    const int r0 = threadIdx.x / VPR, c = threadIdx.x % VPR, lane = threadIdx.x & 31;
+    const int id = id_of(p, min(c0 + r0 + lane % N * ROWS, p.n_cand - 1));
 #pragma unroll
-  for (int i = threadIdx.x; i < S_CAND * VPR; i += S_THREADS) {
-    const int r = i / VPR, c = i % VPR;
-    const bool here = c0 + r < p.n_cand;
-    copy16(m_at + (r * LD + 4 * c) * 4, means + (here ? static_cast<int64_t>(id_of(p, c0 + r)) * VPR + c : 0), here);
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + i * ROWS;
+      const bool here = c0 + r < p.n_cand;
+      const int64_t row = __shfl_sync(0xffffffffu, id, lane / VPR * VPR + i);
+      copy16(m_at + (r * LD + 4 * c) * 4, means + (here ? row * VPR + c : 0), here);
+    }
   }
   if constexpr (!OWN) pdl_wait();
   pdl_trigger();
@@ -419,27 +427,21 @@ __device__ uint64_t kth_largest(int n, int k, Get&& key, Live&& live, int* hist,
 // One block of W warps a list.  Warp w takes the candidates from w 32 steps on, a step of 32 neighbours at a time.
 // PER: the steps, with their keys in registers; 0: any number, read again for each pass.  Latency bounds it (the passes
 // over the keys, with a barrier each): 1250 candidates in two warps 3 us longer than in eight.
-template <int D, int W, int PER>
-__global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ SelectParams p) {
-  constexpr int THREADS = 32 * W;
-  __shared__ PickShared<W> sh;
-  const int qt = blockIdx.x, h = blockIdx.y, n = p.n_cand, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int64_t list = static_cast<int64_t>(h) * p.n_qt + qt;
-  int32_t* const out = p.blocks + list * p.top_k;
+template <int W>
+__device__ __forceinline__ void pick_begin(PickShared<W>& sh) {   // a barrier follows before pick
 #pragma unroll
-  for (int i = threadIdx.x; i < 128; i += THREADS) sh.hist[i / 64][i % 64] = make_int4(0, 0, 0, 0);
+  for (int i = threadIdx.x; i < 128; i += 32 * W) sh.hist[i / 64][i % 64] = make_int4(0, 0, 0, 0);
   if (threadIdx.x == 0) sh.n_list = sh.n_few = 0;
-  pdl_wait();
-  pdl_trigger();
-  if (n <= p.top_k) {   // everything there is
-    for (int i = threadIdx.x; i < p.top_k; i += THREADS) out[i] = i < n ? id_of(p, i) : -1;
-    return;
-  }
+}
+template <int D, int W, int PER>
+__device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, int h, int64_t list, int tiles) {
+  constexpr int THREADS = 32 * W;
+  const int n = p.n_cand, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  int32_t* const out = p.blocks + list * p.top_k;
   const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, n);
   const float* score = ws.score + list * n;
   double* exact = ws.exact + list * n;
   const int steps = PER ? PER : (n + THREADS - 1) / THREADS, first = warp * 32 * steps + lane;
-  const int tiles = (n + S_CAND - 1) / S_CAND;
   float f[PER ? PER : 1];
   if constexpr (PER != 0) {
 #pragma unroll
@@ -458,9 +460,19 @@ __global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ Se
 #pragma unroll
       for (int j = 0; j < PER; ++j) f(first + 32 * j, keys[j], first + 32 * j < n);
     } else {
-      for (int j = 0; j < steps; ++j) {
-        const int i = first + 32 * j;
-        f(i, i < n ? order_key(__ldcg(score + i)) : 0, i < n);
+#pragma unroll 1
+      for (int j = 0; j < steps; j += 8) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = first + 32 * (j + u);
+          x[u] = j + u < steps && i < n ? __ldcg(score + i) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = first + 32 * (j + u);
+          f(i, order_key(x[u]), j + u < steps && i < n);
+        }
       }
     }
   };
@@ -669,8 +681,128 @@ __global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ Se
   });
 }
 
+template <int D, int W, int PER>
+__global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ SelectParams p) {
+  __shared__ PickShared<W> sh;
+  const int h = blockIdx.y, n = p.n_cand;
+  const int64_t list = static_cast<int64_t>(h) * p.n_qt + blockIdx.x;
+  pick_begin(sh);
+  pdl_wait();
+  pdl_trigger();
+  if (n <= p.top_k) {   // everything there is
+    int32_t* const out = p.blocks + list * p.top_k;
+    for (int i = threadIdx.x; i < p.top_k; i += 32 * W) out[i] = i < n ? id_of(p, i) : -1;
+    return;
+  }
+  pick<D, W, PER>(p, sh, h, list, (n + S_CAND - 1) / S_CAND);
+}
+
+// One query block, all in one launch: a cluster a head, every CTA with the queries' sum and its share of the
+// candidates, a warp eight means at a time and as many on their way; then the first CTA chooses.  Latency bounds it
+// (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.4 us where two
+// launches took 10.9, 128 queries 10.1 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not by all:
+// 9.8 -> 8.4.
+constexpr int O_WARPS = 8, O_THREADS = 32 * O_WARPS, O_BATCH = 8;
+template <int D, int PER>
+__global__ void __launch_bounds__(O_THREADS) select_one_kernel(const __grid_constant__ SelectParams p) {
+  constexpr int V = D / 32;   // features of a lane
+  using Vec = std::conditional_t<V == 4, float4, float2>;
+  __shared__ PickShared<O_WARPS> sh;
+  __shared__ QSum<D, O_THREADS> sum;
+  __shared__ __align__(16) float q_sum[D];
+  __shared__ float red[2][32];
+  const int rank = static_cast<int>(cluster_ctarank()), c = static_cast<int>(gridDim.x), h = blockIdx.y;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, n = p.n_cand;
+  pick_begin(sh);
+  pdl_wait();
+  pdl_trigger();
+  const SelectWs ws = ws_of(p.ws, p.H, 1, D, n);
+  const Vec* const means = reinterpret_cast<const Vec*>(p.means) + h * p.ids * 32 + lane;
+  const int step = c * O_WARPS * O_BATCH;
+  Vec here[O_BATCH], next[O_BATCH];   // two batches on their way
+  const auto load = [&](Vec (&m)[O_BATCH], int c0) {
+    const int id = id_of(p, min(c0 + lane % O_BATCH, n - 1));
+#pragma unroll
+    for (int i = 0; i < O_BATCH; ++i) {
+      const int64_t row = __shfl_sync(0xffffffffu, id, i);
+      m[i] = c0 + i < n ? __ldg(means + row * 32) : Vec{};
+    }
+  };
+  int c0 = (rank * O_WARPS + warp) * O_BATCH;
+  load(here, c0);
+  load(next, c0 + step);
+  const float2 v = sum.of(p, h, 0);
+  if (threadIdx.x < D) q_sum[threadIdx.x] = v.x;
+  if (rank == 0) keep_sum<D>(ws, h, v, red, O_WARPS);
+  __syncthreads();
+  const Vec qv = reinterpret_cast<const Vec*>(q_sum)[lane];
+  float largest = 0.f;
+  const auto batch = [&](Vec (&m)[O_BATCH]) {
+    float s[2 * O_BATCH];   // products, then squares
+#pragma unroll
+    for (int i = 0; i < O_BATCH; ++i) {
+      if constexpr (V == 4) {
+        s[i] = fmaf(m[i].x, qv.x, fmaf(m[i].y, qv.y, fmaf(m[i].z, qv.z, m[i].w * qv.w)));
+        s[O_BATCH + i] = fmaf(m[i].x, m[i].x, fmaf(m[i].y, m[i].y, fmaf(m[i].z, m[i].z, m[i].w * m[i].w)));
+      } else {
+        s[i] = fmaf(m[i].x, qv.x, m[i].y * qv.y);
+        s[O_BATCH + i] = fmaf(m[i].x, m[i].x, m[i].y * m[i].y);
+      }
+    }
+    load(m, c0 + 2 * step);
+    // each lane sends half of its sums on at every step and keeps the others: lanes 2 i and 2 i + 1 end with sum i
+#pragma unroll
+    for (int half = O_BATCH; half > 0; half /= 2) {
+      const bool up = lane & (2 * half);
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const float give = up ? s[i] : s[i + half], keep = up ? s[i + half] : s[i];
+        s[i] = keep + __shfl_xor_sync(0xffffffffu, give, 2 * half);
+      }
+    }
+    s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
+    const int i = lane / 2;
+    if (i < O_BATCH) {
+      if (lane % 2 == 0 && c0 + i < n) ws.score[static_cast<int64_t>(h) * n + c0 + i] = s[0];
+    } else {
+      largest = max_nan(largest, s[0]);
+    }
+    c0 += step;
+  };
+#pragma unroll 1
+  while (c0 < n) {
+    batch(here);
+    if (c0 < n) batch(next);
+  }
+  largest = block_reduce<MaxOp>(largest, O_WARPS, red, 1);
+  if (threadIdx.x == 0) ws.largest[h * c + rank] = sqrtf(largest);
+  cluster_sync();   // the scores are there
+  if (rank == 0) pick<D, O_WARPS, PER>(p, sh, h, h, c);
+}
+
+int sm_count() {
+  int dev = 0, sms = 152;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms;
+}
+
 template <int D>
 cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
+  const int n = p.n_cand;
+  // Few heads are few SMs for the means: 4825 candidates of one head 16.3 us so, 12.2 in two launches, of six
+  // heads 16.4 (17.2); 1250 of one head 7.1 (7.2).
+  const int sms = sm_count(), wanted = (n + O_WARPS * O_BATCH - 1) / (O_WARPS * O_BATCH);
+  const int c = std::max(1, std::min({8, sms / p.H, wanted}));
+  if (p.n_qt == 1 && n > p.top_k && (n <= 192 * c || 3 * p.H * c >= sms)) {
+    const auto one = [&](auto kernel) {
+      return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(c), static_cast<unsigned>(p.H)), dim3(O_THREADS), 0,
+                                c, s, p);
+    };
+    return n <= 256 ? one(select_one_kernel<D, 1>) : n <= 1280 ? one(select_one_kernel<D, 5>)
+         : n <= 2560 ? one(select_one_kernel<D, 10>) : n <= 5120 ? one(select_one_kernel<D, 20>)
+         : one(select_one_kernel<D, 0>);
+  }
   const dim3 lists(static_cast<unsigned>(p.n_qt), static_cast<unsigned>(p.H));
   if (p.n_cand > p.top_k) {
     const dim3 tiles(static_cast<unsigned>((p.n_cand + S_CAND - 1) / S_CAND), static_cast<unsigned>(p.H));
@@ -687,7 +819,6 @@ cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   const auto pick = [&](auto kernel, int warps) { return launch_pdl(kernel, lists, dim3(32 * warps), 0, s, p); };
-  const int n = p.n_cand;
   return n <= 128    ? pick(pick_kernel<D, 1, 4>, 1)
          : n <= 768  ? pick(pick_kernel<D, 4, 6>, 4)
          : n <= 1280 ? pick(pick_kernel<D, 8, 5>, 8)
