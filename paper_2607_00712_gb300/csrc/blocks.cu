@@ -99,9 +99,9 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 
 // ------------------------------------------------------------ selection
 // Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 27 us
-// where reading once takes 3.3; the launches' latency bounds it (6, 8 and 9 us each by itself, of which 2 are a
-// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 43 to 48 %).  One query block: one
-// kernel, one query 8.4 us (select_one_kernel); few heads with many candidates two, the sum in the scoring one.
+// where reading once takes 3.3; the launches' latency bounds it (6 to 10 us each by itself, of which 2 are a
+// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 50 to 60 %).  One query block: one
+// kernel, one query 8.2 us (select_one_kernel); few heads with many candidates two, the sum in the scoring one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
 // 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
 // multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
@@ -140,13 +140,21 @@ __device__ __forceinline__ void two_sum(float& hi, float& lo, float x) {
   hi = s;
 }
 
+// The same of 2^-7 x, whose products are exact.
+__device__ __forceinline__ void two_sum_7(float& hi, float& lo, float x) {
+  constexpr float C = 0.0078125f;
+  const float s = __fmaf_rn(C, x, hi), t = __fsub_rn(s, hi);
+  lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fmaf_rn(C, x, -t)));
+  hi = s;
+}
+
 // Sum of a query block's queries of one head, by THREADS threads: rows over the threads, then over the block.  Of 2^-7
 // of the queries, exact for every bf16 value, so that the sum of finite ones stays finite; the order of the scores is
 // the same.  Feature c's sum (hi, lo) to thread c < D; a barrier has passed since the last use of `part` by others.
 template <int D, int THREADS>
 struct QSum {
   static constexpr int LPR = D / 8, ROWS = THREADS / LPR;
-  float2 part[ROWS][D];
+  float2 part[ROWS][LPR * 9];   // a lane's eight 9 apart: 16 lanes to as many pairs of banks
   __device__ __forceinline__ float2 of(const SelectParams& p, int h, int qt) {
     const int lane = threadIdx.x % LPR, r0 = threadIdx.x / LPR;
     const int n = min(kSelectQueries, p.n_q - qt * kSelectQueries);
@@ -166,18 +174,18 @@ struct QSum {
         float f[8];
         unpack8(w[u], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) two_sum(hi[e], lo[e], 0.0078125f * f[e]);
+        for (int e = 0; e < 8; ++e) two_sum_7(hi[e], lo[e], f[e]);
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part[r0][lane * 8 + e] = make_float2(hi[e], lo[e]);
+    for (int e = 0; e < 8; ++e) part[r0][lane * 9 + e] = make_float2(hi[e], lo[e]);
     __syncthreads();
     float a = 0.f, b = 0.f;
     if (threadIdx.x < D) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
         if (r >= n) break;
-        const float2 v = part[r][threadIdx.x];
+        const float2 v = part[r][threadIdx.x + threadIdx.x / 8];
         two_sum(a, b, v.x);
         b += v.y;
       }
@@ -699,8 +707,8 @@ __global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ Se
 
 // One query block, all in one launch: a cluster a head, every CTA with the queries' sum and its share of the
 // candidates, a warp eight means at a time and as many on their way; then the first CTA chooses.  Latency bounds it
-// (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.4 us where two
-// launches took 10.9, 128 queries 10.1 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not by all:
+// (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.2 us where two
+// launches took 10.9, 128 queries 9.9 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not by all:
 // 9.8 -> 8.4.
 constexpr int O_WARPS = 8, O_THREADS = 32 * O_WARPS, O_BATCH = 8;
 template <int D, int PER>
