@@ -100,8 +100,9 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 // ------------------------------------------------------------ selection
 // Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 27 us
 // where reading once takes 3.3; the launches' latency bounds it (6 to 10 us each by itself, of which 2 are a
-// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 50 to 60 %).  One query block: one
-// kernel, one query 8.2 us (select_one_kernel); few heads with many candidates two, the sum in the scoring one.
+// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 50 to 60 %).  Few candidates or one
+// query block: one kernel, one query 8.2 us (select_kernel); one query block and few heads: two, the sum in the scoring
+// one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
 // 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
 // multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
@@ -442,7 +443,8 @@ __device__ __forceinline__ void pick_begin(PickShared<W>& sh) {   // a barrier f
   if (threadIdx.x == 0) sh.n_list = sh.n_few = 0;
 }
 template <int D, int W, int PER>
-__device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, int h, int64_t list, int tiles) {
+__device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, int h, int64_t list, const float* norms,
+                                     int n_norms) {
   constexpr int THREADS = 32 * W;
   const int n = p.n_cand, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   int32_t* const out = p.blocks + list * p.top_k;
@@ -457,7 +459,7 @@ __device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, i
   }
   const float q_norm = __ldcg(ws.norm + list);
   float m_norm = 0.f;
-  for (int i = threadIdx.x; i < tiles; i += THREADS) m_norm = max_nan(m_norm, __ldcg(ws.largest + h * tiles + i));
+  for (int i = threadIdx.x; i < n_norms; i += THREADS) m_norm = max_nan(m_norm, __ldcg(norms + i));
   uint32_t keys[PER ? PER : 1];
   if constexpr (PER != 0) {
 #pragma unroll
@@ -702,29 +704,33 @@ __global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ Se
     for (int i = threadIdx.x; i < p.top_k; i += 32 * W) out[i] = i < n ? id_of(p, i) : -1;
     return;
   }
-  pick<D, W, PER>(p, sh, h, list, (n + S_CAND - 1) / S_CAND);
+  const int tiles = (n + S_CAND - 1) / S_CAND;
+  pick<D, W, PER>(p, sh, h, list, ws_of(p.ws, p.H, p.n_qt, D, n).largest + h * tiles, tiles);
 }
 
-// One query block, all in one launch: a cluster a head, every CTA with the queries' sum and its share of the
-// candidates, a warp eight means at a time and as many on their way; then the first CTA chooses.  Latency bounds it
-// (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.2 us where two
-// launches took 10.9, 128 queries 9.9 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not by all:
-// 9.8 -> 8.4.
+// All in one launch, for few candidates or one query block: a cluster a list, every CTA with the queries' sum and its
+// share of the candidates, a warp eight means at a time and as many on their way; then the first CTA chooses.  Latency
+// bounds it (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.2 us
+// where two launches took 10.9, 128 queries 9.9 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not
+// by all: 9.8 -> 8.4.
 constexpr int O_WARPS = 8, O_THREADS = 32 * O_WARPS, O_BATCH = 8;
 template <int D, int PER>
-__global__ void __launch_bounds__(O_THREADS) select_one_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(O_THREADS) select_kernel(const __grid_constant__ SelectParams p) {
   constexpr int V = D / 32;   // features of a lane
   using Vec = std::conditional_t<V == 4, float4, float2>;
   __shared__ PickShared<O_WARPS> sh;
   __shared__ QSum<D, O_THREADS> sum;
   __shared__ __align__(16) float q_sum[D];
   __shared__ float red[2][32];
-  const int rank = static_cast<int>(cluster_ctarank()), c = static_cast<int>(gridDim.x), h = blockIdx.y;
+  const int rank = static_cast<int>(cluster_ctarank()), c = static_cast<int>(gridDim.x);
+  const int h = blockIdx.y / p.n_qt, qt = blockIdx.y % p.n_qt;
+  const int64_t list = blockIdx.y;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, n = p.n_cand;
   pick_begin(sh);
   pdl_wait();
   pdl_trigger();
-  const SelectWs ws = ws_of(p.ws, p.H, 1, D, n);
+  const SelectWs ws = ws_of(p.ws, p.H, p.n_qt, D, n);
+  float* const norms = reinterpret_cast<float*>(ws.exact + list * n);   // [c], read before exact is written
   const Vec* const means = reinterpret_cast<const Vec*>(p.means) + h * p.ids * 32 + lane;
   const int step = c * O_WARPS * O_BATCH;
   Vec here[O_BATCH], next[O_BATCH];   // two batches on their way
@@ -739,9 +745,9 @@ __global__ void __launch_bounds__(O_THREADS) select_one_kernel(const __grid_cons
   int c0 = (rank * O_WARPS + warp) * O_BATCH;
   load(here, c0);
   load(next, c0 + step);
-  const float2 v = sum.of(p, h, 0);
+  const float2 v = sum.of(p, h, qt);
   if (threadIdx.x < D) q_sum[threadIdx.x] = v.x;
-  if (rank == 0) keep_sum<D>(ws, h, v, red, O_WARPS);
+  if (rank == 0) keep_sum<D>(ws, list, v, red, O_WARPS);
   __syncthreads();
   const Vec qv = reinterpret_cast<const Vec*>(q_sum)[lane];
   float largest = 0.f;
@@ -771,7 +777,7 @@ __global__ void __launch_bounds__(O_THREADS) select_one_kernel(const __grid_cons
     s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
     const int i = lane / 2;
     if (i < O_BATCH) {
-      if (lane % 2 == 0 && c0 + i < n) ws.score[static_cast<int64_t>(h) * n + c0 + i] = s[0];
+      if (lane % 2 == 0 && c0 + i < n) ws.score[list * n + c0 + i] = s[0];
     } else {
       largest = max_nan(largest, s[0]);
     }
@@ -783,9 +789,9 @@ __global__ void __launch_bounds__(O_THREADS) select_one_kernel(const __grid_cons
     if (c0 < n) batch(next);
   }
   largest = block_reduce<MaxOp>(largest, O_WARPS, red, 1);
-  if (threadIdx.x == 0) ws.largest[h * c + rank] = sqrtf(largest);
+  if (threadIdx.x == 0) norms[rank] = sqrtf(largest);
   cluster_sync();   // the scores are there
-  if (rank == 0) pick<D, O_WARPS, PER>(p, sh, h, h, c);
+  if (rank == 0) pick<D, O_WARPS, PER>(p, sh, h, list, norms, c);
 }
 
 int sm_count() {
@@ -798,18 +804,23 @@ int sm_count() {
 template <int D>
 cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   const int n = p.n_cand;
-  // Few heads are few SMs for the means: 4825 candidates of one head 16.3 us so, 12.2 in two launches, of six
-  // heads 16.4 (17.2); 1250 of one head 7.1 (7.2).
+  // One launch where an SM's share of the means is small: 12 heads x 125 candidates, 1024 queries 6.5 us (three launches
+  // 10.2); 40 heads x 225, 512 queries 10.7 (19.6); 12 heads x 325, 4680 queries, a share of 950, 22.1 (22.7); 3 heads x
+  // 4825, 512 queries, 965, 15.6 (13.9); 64 features: 12 heads x 125, 1024 queries 6.8 (9.2); x 325, a share of as many,
+  // 10.8 (10.0).  One query block, which all of the scoring kernel's blocks would add up: but for few heads, too; 12
+  // heads x 4825 21 (24), one head 16.3 (12.2).
   const int sms = sm_count(), wanted = (n + O_WARPS * O_BATCH - 1) / (O_WARPS * O_BATCH);
-  const int c = std::max(1, std::min({8, sms / p.H, wanted}));
-  if (p.n_qt == 1 && n > p.top_k && (n <= 192 * c || 3 * p.H * c >= sms)) {
+  const int64_t items = static_cast<int64_t>(p.H) * p.n_qt;
+  const int c = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, sms / items, wanted})));
+  const int64_t share = std::max<int64_t>(n / c, n * items / sms);   // n >= 2: it keeps the grid's y below 65536
+  if (n > p.top_k && (share <= (D == 128 ? 450 : 200) || (p.n_qt == 1 && 3 * items * c >= sms))) {
     const auto one = [&](auto kernel) {
-      return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(c), static_cast<unsigned>(p.H)), dim3(O_THREADS), 0,
+      return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(c), static_cast<unsigned>(items)), dim3(O_THREADS), 0,
                                 c, s, p);
     };
-    return n <= 256 ? one(select_one_kernel<D, 1>) : n <= 1280 ? one(select_one_kernel<D, 5>)
-         : n <= 2560 ? one(select_one_kernel<D, 10>) : n <= 5120 ? one(select_one_kernel<D, 20>)
-         : one(select_one_kernel<D, 0>);
+    return n <= 256 ? one(select_kernel<D, 1>) : n <= 1280 ? one(select_kernel<D, 5>)
+         : n <= 2560 ? one(select_kernel<D, 10>) : n <= 5120 ? one(select_kernel<D, 20>)
+         : one(select_kernel<D, 0>);
   }
   const dim3 lists(static_cast<unsigned>(p.n_qt), static_cast<unsigned>(p.H));
   if (p.n_cand > p.top_k) {

@@ -1,5 +1,5 @@
-"""Selection for one query block (up to 128 queries): the single launch and its border to the two launches that few
-heads with many candidates take.  Exact, as in tests/test_gpu_blocks.py.
+"""Selection in one launch, for one query block (up to 128 queries) or few candidates, and its borders to the two and
+three launches.  Exact, as in tests/test_gpu_blocks.py.
 """
 import numpy as np
 import pytest
@@ -47,6 +47,18 @@ def test_selection(n, H, d, cap, top_k):
     assert np.array_equal(got, ob.select(ob.scores(q, means), list(range(cap)), top_k))
 
 
+# an SM's share of the candidates below and above 450 (64 features: 200), lists of each instance, 2 to 74 query blocks
+@pytest.mark.parametrize("n,H,d,cap,top_k", [
+    (1100, 12, 128, 50, 7), (1100, 12, 128, 1500, 64), (2200, 12, 128, 1300, 64), (5000, 40, 64, 70, 5),
+    (5000, 40, 128, 130, 30), (1000, 3, 64, 1281, 64), (140, 2, 64, 1600, 100), (140, 2, 64, 1601, 100),
+    (256, 1, 128, 3600, 64), (256, 1, 128, 3601, 64), (9400, 2, 128, 460, 100), (9400, 2, 128, 900, 100),
+    (9400, 2, 64, 205, 3), (9400, 2, 64, 201, 3), (4680, 3, 128, 100, 99), (4680, 3, 128, 601, 64),
+    (300, 40, 128, 451, 33), (300, 50, 128, 456, 33), (520, 3, 128, 2561, 40), (1025, 2, 128, 5121, 40),
+    (700, 160, 64, 9, 4)])
+def test_selection_of_more_query_blocks(n, H, d, cap, top_k):
+    test_selection(n, H, d, cap, top_k)
+
+
 @pytest.mark.parametrize("n", [1, 90])
 @pytest.mark.parametrize("P,cap,written,sinks,win", [(700, 20, 20, 0, (0, 3)), (333, 31, 77, 2, (1, 4)),
                                                      (1000, 9, 100, 1, (1, 1)), (64, 700, 5000, 3, (3, 100))])
@@ -67,9 +79,9 @@ def test_selection_around_a_window(P, cap, written, sinks, win, n):
 @pytest.mark.parametrize("cap", [80, 1000, 6000])
 @pytest.mark.parametrize("values,top_k", [("same", 10), ("zero", 10), ("few", 33), ("pairs", 7), ("nan", 30),
                                           ("inf", 30), ("nan", 75), ("huge", 40), ("tiny", 40), ("close", 50)])
-def test_equal_close_and_extreme_scores(values, top_k, cap):
+def test_equal_close_and_extreme_scores(values, top_k, cap, n=100):
     """Small whole numbers, whose scores are exact in any order, and values at the ends of the range."""
-    H, d, n = 7, 128, 100
+    H, d = 7, 128
     c = Cache(9, H, d, 1, 1)
     ring = abi.KVRing(H, d, 64, cap, 0, 0, cap, 16, 16)
     g = np.random.default_rng(4)
@@ -98,6 +110,13 @@ def test_equal_close_and_extreme_scores(values, top_k, cap):
         score = ob.scores(q, m)
     got = _select(c, (0, 0), 64, torch.from_numpy(m).cuda(), bf16_tensor(q), top_k, ring)
     assert np.array_equal(got, ob.select(score, list(range(cap)), top_k))
+
+
+@pytest.mark.parametrize("cap,n", [(80, 300), (1000, 1100), (6000, 300)])   # one launch, three, three
+@pytest.mark.parametrize("values,top_k", [("same", 10), ("few", 33), ("nan", 75), ("inf", 30), ("huge", 40),
+                                          ("close", 50)])
+def test_the_same_of_more_query_blocks(values, top_k, cap, n):
+    test_equal_close_and_extreme_scores(values, top_k, cap, n)
 
 
 def test_calls_in_a_row_over_one_workspace_and_replayed():
