@@ -98,9 +98,9 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------ selection
-// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 27 us
-// where reading once takes 3.3; the launches' latency bounds it (6 to 10 us each by itself, of which 2 are a
-// launch's own and 3 to 5 the chain of loads, passes and barriers; issue slots 50 to 60 %).  Few candidates or one
+// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 22 us
+// where reading once takes 3.3; the launches' latency bounds it (each a launch's own 2 us and a chain of loads, passes
+// and barriers; issue slots 50 to 60 %).  Few candidates or one
 // query block: one kernel, one query 8.2 us (select_kernel); one query block and few heads: two, the sum in the scoring
 // one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
@@ -205,9 +205,11 @@ __device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float
   if (threadIdx.x == 0) ws.norm[list] = sqrtf(s);
 }
 
+// Registers of four blocks an SM, so that a row's eight words are all on their way: 23.5 -> 21.5 us in all for 37 query
+// blocks of 12 heads (46 registers without; of three or five, 20.6 and 22.9, but 40 heads 37.0 and 33.7 for 35.6).
 constexpr int Q_THREADS = 256;
 template <int D>
-__global__ void __launch_bounds__(Q_THREADS) qsum_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(Q_THREADS, 4) qsum_kernel(const __grid_constant__ SelectParams p) {
   __shared__ QSum<D, Q_THREADS> sum;
   __shared__ float red[2][32];
   const int qt = blockIdx.x, h = blockIdx.y;
@@ -219,15 +221,19 @@ __global__ void __launch_bounds__(Q_THREADS) qsum_kernel(const __grid_constant__
 
 // 32-bit scores: a tile of 64 candidates x 8 J query blocks of one head in shared memory, 2 x J a thread.  A warp's
 // lanes read 16 candidates' words and two query blocks' at a time, with J = 5 in 9 cycles of shared memory for 10 of
-// products.  OWN: one query block, whose sum every block of the grid takes for itself.
+// products; J = 3 for 17 to 24 query blocks, where 5 takes 3 to 4 us more for 12 heads x 1250.  OWN: one query block,
+// whose sum every block of the grid takes for itself.  BLOCKS: that an SM is to hold; with the registers of two (108
+// where three leave 80) the rows are read further ahead: 37 query blocks, 12 heads x 1250 23.3 us in all (26.1), but 40
+// heads x 650, three blocks an SM, 37.3 (35.3).  Without a bound the compiler leaves 34 to 78 registers and
+// reads no row ahead: 28.9 and 38.9.
 constexpr int S_CAND = 64, S_THREADS = 256;
 template <int D, int J>
 constexpr int kScoreSmem = (S_CAND + 8 * J) * (D + 4) * 4;
 __device__ __forceinline__ void copy16(uint32_t dst, const float4* src, bool here) {   // else zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(here ? 16 : 0) : "memory");
 }
-template <int D, int J, bool OWN>
-__global__ void __launch_bounds__(S_THREADS) score_kernel(const __grid_constant__ SelectParams p) {
+template <int D, int J, bool OWN, int BLOCKS>
+__global__ void __launch_bounds__(S_THREADS, BLOCKS) score_kernel(const __grid_constant__ SelectParams p) {
   static_assert(!OWN || J == 1, "one query block");
   constexpr int LD = D + 4, QT = 8 * J, VPR = D / 4;   // rows 4 banks apart; a row's float4
   extern __shared__ float4 tile[];
@@ -265,11 +271,11 @@ __global__ void __launch_bounds__(S_THREADS) score_kernel(const __grid_constant_
   }
   // candidates tc + 32 i, query blocks tq + 8 j: a warp has 16 of the one and two of the other
   const int tc = threadIdx.x % 16 + 16 * (threadIdx.x / 128), tq = threadIdx.x / 16 % 8;
-  for (int q0 = 0; q0 < p.n_qt; q0 += QT) {
+  for (int q0 = blockIdx.z * QT; q0 < p.n_qt; q0 += gridDim.z * QT) {
     const int rows = min(QT, p.n_qt - q0);
     if constexpr (!OWN) {
       const float4* from = reinterpret_cast<const float4*>(ws.hi + (static_cast<int64_t>(h) * p.n_qt + q0) * D);
-      if (q0 > 0) __syncthreads();
+      if (q0 > static_cast<int>(blockIdx.z) * QT) __syncthreads();
 #pragma unroll
       for (int i = threadIdx.x; i < QT * VPR; i += S_THREADS) {
         const bool here = i < rows * VPR;
@@ -299,6 +305,7 @@ __global__ void __launch_bounds__(S_THREADS) score_kernel(const __grid_constant_
         if (c0 + tc + 32 * i < p.n_cand && tq + 8 * j < rows)
           ws.score[(static_cast<int64_t>(h) * p.n_qt + q0 + tq + 8 * j) * p.n_cand + c0 + tc + 32 * i] = acc[i][j];
   }
+  if (blockIdx.z > 0) return;
   // the largest of the tile's norms: four threads a mean
   float s = 0.f;
 #pragma unroll
@@ -804,19 +811,19 @@ int sm_count() {
 template <int D>
 cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   const int n = p.n_cand;
-  // One launch where an SM's share of the means is small: 12 heads x 125 candidates, 1024 queries 6.5 us (three launches
-  // 10.2); 40 heads x 225, 512 queries 10.7 (19.6); 12 heads x 325, 4680 queries, a share of 950, 22.1 (22.7); 3 heads x
-  // 4825, 512 queries, 965, 15.6 (13.9); 64 features: 12 heads x 125, 1024 queries 6.8 (9.2); x 325, a share of as many,
-  // 10.8 (10.0).  One query block, which all of the scoring kernel's blocks would add up: but for few heads, too; 12
-  // heads x 4825 21 (24), one head 16.3 (12.2).
+  // One launch where an SM's share of the means is small: 12 heads x 125 candidates, 1024 queries 6.5 us (three
+  // launches 10.2); 40 heads x 225, 512 queries 10.7 (19.6); 12 heads x 325, 4680 queries, a share of 950, 22.1 (22.7);
+  // 3 heads x 4825, 512 queries, 965, 15.6 (13.9); 64 features: 12 heads x 125, 1024 queries 6.8 (9.2); x 325, a share
+  // of as many, 10.8 (10.0).  One query block, which all of the scoring kernel's blocks would add up: but for few
+  // heads, too; 12 heads x 4825 21 (24), one head 16.3 (12.2).
   const int sms = sm_count(), wanted = (n + O_WARPS * O_BATCH - 1) / (O_WARPS * O_BATCH);
   const int64_t items = static_cast<int64_t>(p.H) * p.n_qt;
   const int c = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, sms / items, wanted})));
   const int64_t share = std::max<int64_t>(n / c, n * items / sms);   // n >= 2: it keeps the grid's y below 65536
   if (n > p.top_k && (share <= (D == 128 ? 450 : 200) || (p.n_qt == 1 && 3 * items * c >= sms))) {
     const auto one = [&](auto kernel) {
-      return launch_pdl_cluster(kernel, dim3(static_cast<unsigned>(c), static_cast<unsigned>(items)), dim3(O_THREADS), 0,
-                                c, s, p);
+      const dim3 grid(static_cast<unsigned>(c), static_cast<unsigned>(items));
+      return launch_pdl_cluster(kernel, grid, dim3(O_THREADS), 0, c, s, p);
     };
     return n <= 256 ? one(select_kernel<D, 1>) : n <= 1280 ? one(select_kernel<D, 5>)
          : n <= 2560 ? one(select_kernel<D, 10>) : n <= 5120 ? one(select_kernel<D, 20>)
@@ -824,17 +831,31 @@ cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   }
   const dim3 lists(static_cast<unsigned>(p.n_qt), static_cast<unsigned>(p.H));
   if (p.n_cand > p.top_k) {
-    const dim3 tiles(static_cast<unsigned>((p.n_cand + S_CAND - 1) / S_CAND), static_cast<unsigned>(p.H));
-    const auto score = [&](auto kernel, int smem) {
-      const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), smem);
-      return e != cudaSuccess ? e : launch_pdl(kernel, tiles, dim3(S_THREADS), smem, s, p);
+    const int64_t tiles = (n + S_CAND - 1) / S_CAND;
+    // Query blocks by groups of 8 J: one after the other in a block of the grid, or side by side where that leaves the
+    // blocks that the SMs hold: 9344 queries x 12 heads x 1250 candidates 36 us in all, else 46.
+    const auto score = [&](auto j, auto own) {
+      constexpr int J = decltype(j)::value;
+      const int64_t groups = (p.n_qt + 8 * J - 1) / (8 * J);
+      const int64_t z = std::max<int64_t>(1, std::min<int64_t>(groups, 4 * sms / (tiles * p.H)));
+      const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(p.H), static_cast<unsigned>(z));
+      const auto with = [&](auto kernel) {
+        const cudaError_t e = set_smem_limit_once(reinterpret_cast<const void*>(kernel), kScoreSmem<D, J>);
+        return e != cudaSuccess ? e : launch_pdl(kernel, grid, dim3(S_THREADS), kScoreSmem<D, J>, s, p);
+      };
+      if constexpr (J >= 3)
+        if (tiles * p.H * z <= 2 * sms) return with(score_kernel<D, J, false, 2>);
+      return with(score_kernel<D, J, decltype(own)::value, 3>);
     };
     cudaError_t e = p.n_qt == 1 ? cudaSuccess : launch_pdl(qsum_kernel<D>, lists, dim3(Q_THREADS), 0, s, p);
     if (e != cudaSuccess) return e;
-    e = p.n_qt == 1    ? score(score_kernel<D, 1, true>, kScoreSmem<D, 1>)
-        : p.n_qt <= 8  ? score(score_kernel<D, 1, false>, kScoreSmem<D, 1>)
-        : p.n_qt <= 16 ? score(score_kernel<D, 2, false>, kScoreSmem<D, 2>)
-                       : score(score_kernel<D, 5, false>, kScoreSmem<D, 5>);
+    using std::integral_constant;
+    e = p.n_qt == 1    ? score(integral_constant<int, 1>(), std::true_type())
+        : p.n_qt <= 8  ? score(integral_constant<int, 1>(), std::false_type())
+        : p.n_qt <= 16 ? score(integral_constant<int, 2>(), std::false_type())
+        : p.n_qt <= 24 ? score(integral_constant<int, 3>(), std::false_type())
+        : p.n_qt <= 32 ? score(integral_constant<int, 4>(), std::false_type())
+                       : score(integral_constant<int, 5>(), std::false_type());
     if (e != cudaSuccess) return e;
   }
   const auto pick = [&](auto kernel, int warps) { return launch_pdl(kernel, lists, dim3(32 * warps), 0, s, p); };

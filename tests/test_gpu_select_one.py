@@ -54,7 +54,9 @@ def test_selection(n, H, d, cap, top_k):
     (256, 1, 128, 3600, 64), (256, 1, 128, 3601, 64), (9400, 2, 128, 460, 100), (9400, 2, 128, 900, 100),
     (9400, 2, 64, 205, 3), (9400, 2, 64, 201, 3), (4680, 3, 128, 100, 99), (4680, 3, 128, 601, 64),
     (300, 40, 128, 451, 33), (300, 50, 128, 456, 33), (520, 3, 128, 2561, 40), (1025, 2, 128, 5121, 40),
-    (700, 160, 64, 9, 4)])
+    (700, 160, 64, 9, 4),
+    # 32, 25, 24 and 74 query blocks in three launches
+    (4000, 12, 128, 1300, 64), (3200, 12, 64, 700, 30), (3000, 3, 128, 1400, 70), (9400, 12, 128, 1300, 128)])
 def test_selection_of_more_query_blocks(n, H, d, cap, top_k):
     test_selection(n, H, d, cap, top_k)
 
