@@ -141,11 +141,11 @@ __device__ __forceinline__ void two_sum(float& hi, float& lo, float x) {
   hi = s;
 }
 
-// The same of 2^-7 x, whose products are exact.
-__device__ __forceinline__ void two_sum_7(float& hi, float& lo, float x) {
-  constexpr float C = 0.0078125f;
-  const float s = __fmaf_rn(C, x, hi), t = __fsub_rn(s, hi);
-  lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fmaf_rn(C, x, -t)));
+// The same of 2^-7 x, whose products are exact, two at a time.
+__device__ __forceinline__ void two_sum_7(float2& hi, float2& lo, float2 x) {
+  const float2 c = make_float2(0.0078125f, 0.0078125f), minus = make_float2(-1.f, -1.f);
+  const float2 s = fma2(c, x, hi), t = fma2(minus, s, hi);   // t: -2^-7 x, as far as s has it
+  lo = add2(lo, add2(fma2(minus, add2(s, t), hi), fma2(c, x, t)));
   hi = s;
 }
 
@@ -162,7 +162,7 @@ struct QSum {
     const int64_t row = static_cast<int64_t>(p.H) * LPR;
     const uint4* from = reinterpret_cast<const uint4*>(p.q) + (static_cast<int64_t>(qt) * kSelectQueries) * row +
                         h * LPR + lane;
-    float hi[8] = {}, lo[8] = {};
+    float2 hi[4] = {}, lo[4] = {};
     for (int u0 = 0; u0 * ROWS < n; u0 += 8) {
       uint4 w[8];
 #pragma unroll
@@ -175,11 +175,14 @@ struct QSum {
         float f[8];
         unpack8(w[u], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) two_sum_7(hi[e], lo[e], f[e]);
+        for (int e = 0; e < 4; ++e) two_sum_7(hi[e], lo[e], make_float2(f[2 * e], f[2 * e + 1]));
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part[r0][lane * 9 + e] = make_float2(hi[e], lo[e]);
+    for (int e = 0; e < 4; ++e) {
+      part[r0][lane * 9 + 2 * e] = make_float2(hi[e].x, lo[e].x);
+      part[r0][lane * 9 + 2 * e + 1] = make_float2(hi[e].y, lo[e].y);
+    }
     __syncthreads();
     float a = 0.f, b = 0.f;
     if (threadIdx.x < D) {
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(S_THREADS, BLOCKS) score_kernel(const __grid_c
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    float acc[2][J] = {};
+    float2 acc[2][J] = {};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
       float4 a[2], b[J];
@@ -296,14 +299,16 @@ __global__ void __launch_bounds__(S_THREADS, BLOCKS) score_kernel(const __grid_c
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j)
-          acc[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, acc[i][j]))));
+          acc[i][j] = fma2(make_float2(a[i].z, a[i].w), make_float2(b[j].z, b[j].w),
+                           fma2(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), acc[i][j]));
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < J; ++j)
         if (c0 + tc + 32 * i < p.n_cand && tq + 8 * j < rows)
-          ws.score[(static_cast<int64_t>(h) * p.n_qt + q0 + tq + 8 * j) * p.n_cand + c0 + tc + 32 * i] = acc[i][j];
+          ws.score[(static_cast<int64_t>(h) * p.n_qt + q0 + tq + 8 * j) * p.n_cand + c0 + tc + 32 * i] =
+              acc[i][j].x + acc[i][j].y;
   }
   if (blockIdx.z > 0) return;
   // the largest of the tile's norms: four threads a mean

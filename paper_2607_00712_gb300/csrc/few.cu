@@ -70,14 +70,6 @@ __device__ __forceinline__ Unit unit_at(const FewParams& p, const int32_t* list,
   return Unit{static_cast<int64_t>(frame) * p.lists.P + at + first, max(0, min(F_KEYS, n)), false};
 }
 
-// Two fp32 operations an instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<uint64_t&>(r))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
-  return r;
-}
 // Sixteen bytes as fp32: eight bf16 values, or sixteen codes.
 __device__ __forceinline__ void unpack(const uint4& w, float2 (&f)[4]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
