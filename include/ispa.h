@@ -30,7 +30,8 @@
  *     error, which ispa_last_device_error() reports as ISPA_ERR_TIMEOUT.
  *   - The attention kernels launch one CTA per (query tile, head); the CTAs
  *     that start first take the items of CTAs that have not started yet
- *     (cluster launch control), so each SM works through a run of items.
+ *     (cluster launch control), so each SM works through a run of items.  (One
+ *     or two queries of ispa_attn_blocks: up to eight CTAs a head.)
  *   - Head dims supported: 64 and 128.  Tokens per frame P >= 1.
  *   - Counts (queries n_q, tokens T, frames n_frames, rows) must be at least
  *     1: an empty call is an argument error (ISPA_ERR_INVALID_ARG) and
