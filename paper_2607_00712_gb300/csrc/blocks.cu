@@ -104,14 +104,16 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 // query block: one kernel, one query 8.2 us (select_kernel); one query block and few heads: two, the sum in the scoring
 // one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
-// 32-bit scores, and the sum's norm; per head and tile of candidates the largest norm of a mean.  hi and lo are
-// multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on its 8 and 4.
+// 32-bit scores, the sum's norm, and a bound on what hi + lo is off by; per head and tile of candidates the largest norm
+// of a mean.  hi and lo are multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on
+// its 8 and 4.
 struct SelectWs {
   float* hi;          // [H][n_qt][d]
   float* lo;
   double* exact;      // [H][n_qt][n_cand]
   float* score;       // [H][n_qt][n_cand]
   float* norm;        // [H][n_qt]
+  float* lost;        // [H][n_qt]
   float* largest;     // [H][tiles]
 };
 __host__ __device__ __forceinline__ SelectWs ws_of(void* ws, int64_t H, int64_t n_qt, int64_t d, int64_t n_cand) {
@@ -121,7 +123,8 @@ __host__ __device__ __forceinline__ SelectWs ws_of(void* ws, int64_t H, int64_t 
   w.exact = reinterpret_cast<double*>(w.lo + H * n_qt * d);
   w.score = reinterpret_cast<float*>(w.exact + H * n_qt * n_cand);
   w.norm = w.score + H * n_qt * n_cand;
-  w.largest = w.norm + H * n_qt;
+  w.lost = w.norm + H * n_qt;
+  w.largest = w.lost + H * n_qt;
   return w;
 }
 
@@ -149,35 +152,64 @@ __device__ __forceinline__ void two_sum_7(float2& hi, float2& lo, float2 x) {
   hi = s;
 }
 
+// Of two bf16 values each the larger magnitude; its sign has no meaning.
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // Sum of a query block's queries of one head, by THREADS threads: rows over the threads, then over the block.  Of 2^-7
 // of the queries, exact for every bf16 value, so that the sum of finite ones stays finite; the order of the scores is
-// the same.  Feature c's sum (hi, lo) to thread c < D; a barrier has passed since the last use of `part` by others.
+// the same.  Feature c's sum (hi, lo) to thread c < D, hi the rounded sum of both whatever cancelled on the way; a
+// barrier has passed since the last use of `part` by others.
+//
+// TwoSum is exact, so hi + lo is off by the roundings of lo alone.  With Y the largest |2^-7 q| and steps of 2^-24 Y:
+// the k-th sum of a thread's N rows is at most k Y, and its lo takes a residue of k steps; the block's k-th sum is at
+// most N k Y, and its lo takes a residue of N k steps and then a thread's lo of N (N + 1) / 2.  So the lo's stay below
+// (N k (k + 1) + N (N + 1) k) / 2 steps, and both additions round to 2^-24 of that: over k <= ROWS, with the threads'
+// own, 2^-33.4 Y for N = 8 and 2^-32.1 Y for N = 4.  lost_of: 2^-32 sqrt(D) Y for all features, twice, for the roundings
+// of 64-bit scores (below 2^-37 sqrt(D) Y |m|).
+template <int D>
+__device__ __forceinline__ float lost_of(float y) {
+  return (D == 128 ? 11.5f : 8.f) * 4.6566129e-10f * y;
+}
 template <int D, int THREADS>
 struct QSum {
   static constexpr int LPR = D / 8, ROWS = THREADS / LPR;
+  static constexpr int N = kSelectQueries / ROWS;   // rows of a thread, all on their way at once
+  static_assert(ROWS >= 16 && ROWS <= 32, "lost_of's partial sums");
   float2 part[ROWS][LPR * 9];   // a lane's eight 9 apart: 16 lanes to as many pairs of banks
+  float top[THREADS / 32];      // the largest magnitude that a warp read (NaN aside, with which the sum is NaN)
   __device__ __forceinline__ float2 of(const SelectParams& p, int h, int qt) {
     const int lane = threadIdx.x % LPR, r0 = threadIdx.x / LPR;
     const int n = min(kSelectQueries, p.n_q - qt * kSelectQueries);
     const int64_t row = static_cast<int64_t>(p.H) * LPR;
     const uint4* from = reinterpret_cast<const uint4*>(p.q) + (static_cast<int64_t>(qt) * kSelectQueries) * row +
                         h * LPR + lane;
-    float2 hi[4] = {}, lo[4] = {};
-    for (int u0 = 0; u0 * ROWS < n; u0 += 8) {
-      uint4 w[8];
+    uint4 w[N];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int r = r0 + (u0 + u) * ROWS;
-        w[u] = r < n ? __ldg(from + r * row) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        float f[8];
-        unpack8(w[u], f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) two_sum_7(hi[e], lo[e], make_float2(f[2 * e], f[2 * e + 1]));
-      }
+    for (int u = 0; u < N; ++u) {
+      const int r = r0 + u * ROWS;
+      w[u] = r < n ? __ldg(from + r * row) : make_uint4(0, 0, 0, 0);
     }
+    float2 hi[4], lo[4] = {};
+    uint32_t most = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      float f[8];
+      unpack8(w[u], f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 x = make_float2(f[2 * e], f[2 * e + 1]);
+        if (u == 0) hi[e] = make_float2(0.0078125f * x.x, 0.0078125f * x.y);
+        else two_sum_7(hi[e], lo[e], x);
+      }
+      most = larger2(larger2(most, w[u].x), larger2(w[u].y, larger2(w[u].z, w[u].w)));
+    }
+    const float own = fmaxf(fabsf(__uint_as_float(most << 16)), fabsf(__uint_as_float(most & 0xffff0000u)));
+    const float of_warp = warp_max(own);
+    if ((threadIdx.x & 31) == 0) top[threadIdx.x / 32] = of_warp;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       part[r0][lane * 9 + 2 * e] = make_float2(hi[e].x, lo[e].x);
@@ -194,32 +226,41 @@ struct QSum {
         b += v.y;
       }
     }
-    return make_float2(a, fabsf(a) < INFINITY ? b : 0.f);
+    float rest = 0.f;
+    if (fabsf(a) < INFINITY) two_sum(a, rest, b);
+    return make_float2(a, rest);
   }
 };
-// The sum to the workspace, with its norm; all threads of the block.
-template <int D>
-__device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float2 v, float (*red)[32], int warps) {
+// The sum to the workspace, with its norm and lost_of; all threads of the block.
+template <int D, int THREADS>
+__device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float2 v, const QSum<D, THREADS>& sum,
+                                         float (*red)[32]) {
   if (threadIdx.x < D) {
     ws.hi[list * D + threadIdx.x] = v.x;
     ws.lo[list * D + threadIdx.x] = v.y;
   }
-  const float s = block_reduce<SumOp>(threadIdx.x < D ? v.x * v.x : 0.f, warps, red, 0);
-  if (threadIdx.x == 0) ws.norm[list] = sqrtf(s);
+  const float s = block_reduce<SumOp>(threadIdx.x < D ? v.x * v.x : 0.f, THREADS / 32, red, 0);
+  if (threadIdx.x == 0) {
+    ws.norm[list] = sqrtf(s);
+    float y = sum.top[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) y = fmaxf(y, sum.top[i]);
+    ws.lost[list] = lost_of<D>(0.0078125f * y);
+  }
 }
 
-// Registers of four blocks an SM, so that a row's eight words are all on their way: 23.5 -> 21.5 us in all for 37 query
-// blocks of 12 heads (46 registers without; of three or five, 20.6 and 22.9, but 40 heads 37.0 and 33.7 for 35.6).
+// Registers of three blocks an SM, so that a row's eight words are all on their way: 37 query blocks of 12 heads over
+// 1250 candidates 21.0 us in all, of 40 heads over 650 32.5; of four 22.1 and 33.8.
 constexpr int Q_THREADS = 256;
 template <int D>
-__global__ void __launch_bounds__(Q_THREADS, 4) qsum_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(Q_THREADS, 3) qsum_kernel(const __grid_constant__ SelectParams p) {
   __shared__ QSum<D, Q_THREADS> sum;
   __shared__ float red[2][32];
   const int qt = blockIdx.x, h = blockIdx.y;
   pdl_wait();
   pdl_trigger();
-  keep_sum<D>(ws_of(p.ws, p.H, p.n_qt, D, p.n_cand), static_cast<int64_t>(h) * p.n_qt + qt, sum.of(p, h, qt), red,
-              Q_THREADS / 32);
+  const float2 v = sum.of(p, h, qt);
+  keep_sum(ws_of(p.ws, p.H, p.n_qt, D, p.n_cand), static_cast<int64_t>(h) * p.n_qt + qt, v, sum, red);
 }
 
 // 32-bit scores: a tile of 64 candidates x 8 J query blocks of one head in shared memory, 2 x J a thread.  A warp's
@@ -270,7 +311,7 @@ __global__ void __launch_bounds__(S_THREADS, BLOCKS) score_kernel(const __grid_c
     if (threadIdx.x < D) q[threadIdx.x] = v.x;
 #pragma unroll
     for (int i = threadIdx.x; i < 7 * D; i += S_THREADS) q[(1 + i / D) * LD + i % D] = 0.f;
-    if (blockIdx.x == 0) keep_sum<D>(ws, h, v, red, S_THREADS / 32);
+    if (blockIdx.x == 0) keep_sum(ws, h, v, sum, red);
   }
   // candidates tc + 32 i, query blocks tq + 8 j: a warp has 16 of the one and two of the other
   const int tc = threadIdx.x % 16 + 16 * (threadIdx.x / 128), tq = threadIdx.x / 16 % 8;
@@ -336,6 +377,9 @@ __device__ __forceinline__ uint64_t order_key(double f) {
 __device__ __forceinline__ float score_of(uint32_t key) {   // of any key but NaN's
   return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
 }
+__device__ __forceinline__ double score_of(uint64_t key) {
+  return __longlong_as_double(static_cast<long long>(key >> 63 ? key & ~(uint64_t{1} << 63) : ~key));
+}
 
 constexpr int kFew = 64;   // candidates that are ranked one against one
 
@@ -347,9 +391,10 @@ struct PickShared {
   float norms[W];
   uint64_t counts[2][W];
   int few[kFew];
-  uint64_t few_key[kFew], few_least;
-  int n_list, n_few, few_ties;
+  uint64_t few_key[3][kFew], few_least;   // of the score, and of where scores near it begin and end
+  int n_list, n_few, few_ties, few_close;
   int wide[258];
+  double sum[128];            // of the queries, in 64 bits
 };
 
 // Two counts in a word: their sum over the warps before this one, and over all.
@@ -445,6 +490,27 @@ __device__ uint64_t kth_largest(int n, int k, Get&& key, Live&& live, int* hist,
   return known;
 }
 
+// The sum that QSum takes, a feature a thread, as three floats, whose sum has all 53 bits of a double.  Not inlined and
+// short: almost no list needs it, and what it takes (20 us where a list does) is less than its registers and code would
+// cost the others.
+template <int D, int THREADS>
+__device__ __noinline__ void sum_again(const SelectParams& p, int h, int qt, double* sum) {
+  const int n = min(kSelectQueries, p.n_q - qt * kSelectQueries);
+  const int64_t row = static_cast<int64_t>(p.H) * D;
+  for (int c = threadIdx.x; c < D; c += THREADS) {
+    const __nv_bfloat16* from = p.q + static_cast<int64_t>(qt) * kSelectQueries * row + h * D + c;
+    float hi = 0.f, mid = 0.f, lo = 0.f;
+#pragma unroll 4
+    for (int r = 0; r < n; ++r) {
+      float x = 0.f, y = 0.f;
+      two_sum(hi, x, 0.0078125f * __bfloat162float(from[r * row]));
+      two_sum(mid, y, x);
+      lo += y;
+    }
+    sum[c] = fabsf(hi) < INFINITY ? static_cast<double>(hi) + (static_cast<double>(mid) + static_cast<double>(lo)) : hi;
+  }
+}
+
 // One block of W warps a list.  Warp w takes the candidates from w 32 steps on, a step of 32 neighbours at a time.
 // PER: the steps, with their keys in registers; 0: any number, read again for each pass.  Latency bounds it (the passes
 // over the keys, with a barrier each): 1250 candidates in two warps 3 us longer than in eight.
@@ -469,7 +535,7 @@ __device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, i
 #pragma unroll
     for (int j = 0; j < PER; ++j) f[j] = first + 32 * j < n ? __ldcg(score + first + 32 * j) : 0.f;
   }
-  const float q_norm = __ldcg(ws.norm + list);
+  const float q_norm = __ldcg(ws.norm + list), lost = __ldcg(ws.lost + list);
   float m_norm = 0.f;
   for (int i = threadIdx.x; i < n_norms; i += THREADS) m_norm = max_nan(m_norm, __ldcg(norms + i));
   uint32_t keys[PER ? PER : 1];
@@ -592,9 +658,9 @@ __device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, i
     t_key = __shfl_sync(0xffffffffu, a_is ? a : b, __ffs(found) - 1);
   }
   // The bound: a product's sum in 32 bits over d terms is off by at most (d + 1) 2^-24 |q| |m| (Cauchy-Schwarz; q's
-  // rounding to 32 bits among it), besides what underflows, 2^-150 a product; the other 23 steps are for the roundings
-  // of |q|, |m| and of T +- 2 E.
-  const float E = (D + 24) * 5.9604645e-8f * q_norm * m_norm + 1.1754944e-38f;
+  // rounding to 32 bits among it), besides what the sum of the queries has lost and what underflows, 2^-150 a product;
+  // the other 23 steps are for the roundings of |q|, |m| and of T +- 2 E.
+  const float E = ((D + 24) * 5.9604645e-8f * q_norm + lost) * m_norm + 1.1754944e-38f;
   const float T = t_key ? score_of(t_key) : INFINITY;
   // without a finite bound everything is scored again
   const bool bounded = E < INFINITY && fabsf(T) < INFINITY;
@@ -621,7 +687,9 @@ __device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, i
     });
     return;
   }
-  // 64-bit scores, a warp a candidate, every one's terms in the same order
+  // 64-bit scores, a warp a candidate, every one's terms in the same order.  First of hi + lo: where another score lies
+  // so near the last one taken that what the sum has lost could turn them round, then of the queries' sum in 64 bits
+  // (at once where no bound holds or many are open).
   uint64_t least;   // open candidates are taken above this key, `ties` of those at it
   int ties;
   double q[D / 32];
@@ -639,43 +707,59 @@ __device__ __forceinline__ void pick(const SelectParams& p, PickShared<W>& sh, i
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     return s;
   };
+  const double apart = 2.0 * static_cast<double>(lost) * m_norm;
   if (n_open <= kFew) {
     each([&](int i, uint32_t x, bool here) {
       if (here && x >= low_key && x <= high_key) sh.few[atomicAdd(&sh.n_few, 1)] = i;
     });
+  }
+#pragma unroll 1
+  for (bool in64 = !bounded || n_open > kFew;; in64 = true) {
+    if (in64) sum_again<D, THREADS>(p, h, static_cast<int>(list - static_cast<int64_t>(h) * p.n_qt), sh.sum);
     __syncthreads();
+    if (in64) {
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) q[j] = sh.sum[lane + 32 * j];
+    }
+    if (n_open > kFew) {
+      const auto open = [&](int i) {
+        const uint32_t x = order_key(__ldcg(score + i));
+        return x >= low_key && x <= high_key;
+      };
+      for (int i = warp; i < n; i += W)
+        if (open(i)) {
+          const double s = score64(i);
+          if (lane == 0) exact[i] = s;
+        }
+      __syncthreads();
+      least = kth_largest<THREADS>(n, need, [&](int i) { return order_key(exact[i]); }, open, sh.wide, ties);
+      break;
+    }
     for (int i = warp; i < n_open; i += W) {
       const double s = score64(sh.few[i]);
-      if (lane == 0) sh.few_key[i] = order_key(s), exact[sh.few[i]] = s;
+      if (lane < 3) sh.few_key[lane][i] = order_key(s + (lane == 0 ? 0.0 : lane == 1 ? -apart : apart));
+      if (lane == 0) exact[sh.few[i]] = s;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n_open; i += THREADS) {   // those that less than `need` are above of, and so on
-      const uint64_t x = sh.few_key[i];
-      int ahead = 0, equal = 0;
+      const uint64_t x = sh.few_key[0][i], from = sh.few_key[1][i], to = sh.few_key[2][i];
+      int ahead = 0, equal = 0, near = 0;
       for (int j = 0; j < n_open; ++j) {
-        ahead += sh.few_key[j] > x;
-        equal += sh.few_key[j] == x;
+        const uint64_t y = sh.few_key[0][j];
+        ahead += y > x;
+        equal += y == x;
+        near += y >= from && y <= to;
       }
       if (ahead < need && ahead + equal >= need) {   // equal ones write the same
         sh.few_least = x;
         sh.few_ties = need - ahead;
+        sh.few_close = near > 1;
       }
     }
     __syncthreads();
     least = sh.few_least;
     ties = sh.few_ties;
-  } else {
-    const auto open = [&](int i) {
-      const uint32_t x = order_key(__ldcg(score + i));
-      return x >= low_key && x <= high_key;
-    };
-    for (int i = warp; i < n; i += W)
-      if (open(i)) {
-        const double s = score64(i);
-        if (lane == 0) exact[i] = s;
-      }
-    __syncthreads();
-    least = kth_largest<THREADS>(n, need, [&](int i) { return order_key(exact[i]); }, open, sh.wide, ties);
+    if (in64 || !sh.few_close) break;   // the next turn's first barrier is behind these reads
   }
   // In the order of their numbers: the sure ones, the open ones above `least` and the first `ties` of those at it.
   const auto key64 = [&](int i, uint32_t x, bool here) {   // 0: not in question (a NaN's, too, where `least` is more)
@@ -759,7 +843,7 @@ __global__ void __launch_bounds__(O_THREADS) select_kernel(const __grid_constant
   load(next, c0 + step);
   const float2 v = sum.of(p, h, qt);
   if (threadIdx.x < D) q_sum[threadIdx.x] = v.x;
-  if (rank == 0) keep_sum<D>(ws, list, v, red, O_WARPS);
+  if (rank == 0) keep_sum(ws, list, v, sum, red);
   __syncthreads();
   const Vec qv = reinterpret_cast<const Vec*>(q_sum)[lane];
   float largest = 0.f;
@@ -883,7 +967,7 @@ cudaError_t launch_key_means(const MeansParams& p, cudaStream_t s) {
 
 size_t select_ws_bytes(int64_t H, int64_t n_qt, int64_t d, int64_t ids) {
   if (static_cast<double>(H) * n_qt * (ids + d) > 1e17) return 0;   // far past any memory, and no overflow below
-  return static_cast<size_t>(H) * (n_qt * ids * 12 + n_qt * d * 8 + n_qt * 4 + (ids + S_CAND - 1) / S_CAND * 4);
+  return static_cast<size_t>(H) * (n_qt * ids * 12 + n_qt * d * 8 + n_qt * 8 + (ids + S_CAND - 1) / S_CAND * 4);
 }
 
 cudaError_t launch_select(const SelectParams& p, cudaStream_t s) {
