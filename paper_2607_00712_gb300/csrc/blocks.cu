@@ -231,6 +231,10 @@ struct QSum {
     return make_float2(a, rest);
   }
 };
+// A norm for the bound from a sum of at most 128 squares: what those lose below fp32's normal range, 2^-150 each and as
+// much in their additions, is at most 2^-142, and the root of a sum at most the sum of the roots.
+__device__ __forceinline__ float norm_of(float squares) { return sqrtf(squares) + 4.2351647e-22f; }   // 2^-71
+
 // The sum to the workspace, with its norm and lost_of; all threads of the block.
 template <int D, int THREADS>
 __device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float2 v, const QSum<D, THREADS>& sum,
@@ -241,7 +245,7 @@ __device__ __forceinline__ void keep_sum(const SelectWs& ws, int64_t list, float
   }
   const float s = block_reduce<SumOp>(threadIdx.x < D ? v.x * v.x : 0.f, THREADS / 32, red, 0);
   if (threadIdx.x == 0) {
-    ws.norm[list] = sqrtf(s);
+    ws.norm[list] = norm_of(s);
     float y = sum.top[0];
 #pragma unroll
     for (int i = 1; i < THREADS / 32; ++i) y = fmaxf(y, sum.top[i]);
@@ -360,7 +364,7 @@ __global__ void __launch_bounds__(S_THREADS, BLOCKS) score_kernel(const __grid_c
     s = fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, fmaf(v.w, v.w, s))));
   }
   s = block_reduce<MaxOp>(group_reduce<SumOp>(s, 4), S_THREADS / 32, red, 1);
-  if (threadIdx.x == 0) ws.largest[h * gridDim.x + blockIdx.x] = sqrtf(s);
+  if (threadIdx.x == 0) ws.largest[h * gridDim.x + blockIdx.x] = norm_of(s);
 }
 
 // Keys whose order as integers is that of the scores; both zeros alike, NaN below all.
@@ -885,7 +889,7 @@ __global__ void __launch_bounds__(O_THREADS) select_kernel(const __grid_constant
     if (c0 < n) batch(next);
   }
   largest = block_reduce<MaxOp>(largest, O_WARPS, red, 1);
-  if (threadIdx.x == 0) norms[rank] = sqrtf(largest);
+  if (threadIdx.x == 0) norms[rank] = norm_of(largest);
   cluster_sync();   // the scores are there
   if (rank == 0) pick<D, O_WARPS, PER>(p, sh, h, list, norms, c);
 }

@@ -1,6 +1,6 @@
-"""Selections whose scores in 32 bits are far off: queries that cancel in their sum.  Exact against the oracle: the
-queries are whole multiples of a power of two and their sums have less than 53 bits, so the oracle's sums are exact in
-any order.
+"""Selections whose scores in 32 bits are far off: queries that cancel in their sum, and values whose squares leave
+fp32's range at its lower end.  Exact against the oracle: the queries are whole multiples of a power of two and their
+sums have less than 53 bits, so the oracle's sums are exact in any order.
 """
 import numpy as np
 import pytest
@@ -73,3 +73,14 @@ def test_all_queries_but_one_cancel(x, n, H, d, cap, top_k):
         q[rows[0]] = _queries(g, 1, H, d, x * 2.0 ** -12, 14)[0]
     means = g.standard_normal((H, cap, d)).astype(np.float32)
     _check(q, means, top_k)
+
+
+@pytest.mark.parametrize("n,H,d,cap,top_k", FORMS)
+@pytest.mark.parametrize("q_bits,m_bits", [(-80, 0), (-110, 0), (0, -80), (0, -100), (-75, -30), (-30, -75), (-120, 30),
+                                           (60, -100)])
+def test_values_whose_squares_underflow(q_bits, m_bits, n, H, d, cap, top_k):
+    """Means of random signs that differ by some units of their last place."""
+    g = np.random.default_rng(n + d)
+    q = _queries(g, n, H, d, 1.0, 14) * np.float32(2.0 ** q_bits)
+    means = g.choice([-1.0, 1.0], (H, 1, d)) * (1 + g.integers(0, 256, (H, cap, d)) * 2.0 ** -23)
+    _check(q, (means * 2.0 ** m_bits).astype(np.float32), top_k)
