@@ -444,8 +444,12 @@ __global__ void __launch_bounds__(NTHREADS, 1)
         mbar_arrive_expect_tx(b.v_full0 + 8 * vs, C::V_TILE);
         const uint32_t sV = sbase + C::OFF_V + vs * C::V_TILE;
         const int vhead = vk == kk ? kh : prev_h;
-        if (BLOCKS && vj >= n_dense) {
-          if constexpr (BLOCKS) {
+        // The dense tiles' loads behind a condition of their own: as the other branch of one with the listed tiles' the
+        // instances without lists took 0.3 to 0.6 % longer (4680 queries x 12 heads x 32760 keys 586.4 us, so 584.4).
+        bool listed = false;
+        if constexpr (BLOCKS) {
+          listed = vj >= n_dense;
+          if (listed) {
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
               const int2 w = tv == t - 1 ? last[i] : before[i];
@@ -455,13 +459,16 @@ __global__ void __launch_bounds__(NTHREADS, 1)
                             vhead);
             }
           }
-        } else if constexpr (PV8) {
-          // d-major e4m3 V: the tile's first key is a multiple of 16 (segments start aligned)
-          const int x0 = p.seg[vseg].start + voff;
-          tma_load_3d(sV, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, x0, 0, vhead);
-          tma_load_3d(sV + C::V_BOX8, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, x0 + 128, 0, vhead);
-        } else {
-          tma_load_4d(sV, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, 0, p.seg[vseg].start + voff, 0, vhead);
+        }
+        if (!listed) {
+          if constexpr (PV8) {
+            // d-major e4m3 V: the tile's first key is a multiple of 16 (segments start aligned)
+            const int x0 = p.seg[vseg].start + voff;
+            tma_load_3d(sV, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, x0, 0, vhead);
+            tma_load_3d(sV + C::V_BOX8, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, x0 + 128, 0, vhead);
+          } else {
+            tma_load_4d(sV, chunk ? &tm_vc : &tm_vr, b.v_full0 + 8 * vs, 0, p.seg[vseg].start + voff, 0, vhead);
+          }
         }
         tr(tv, 7);
         ++tv;
