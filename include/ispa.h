@@ -909,7 +909,8 @@ ISPA_API ispa_status ispa_kv_append_rope(ispa_kv_ring* ring, const ispa_rope* ro
  * it in all that follows; capacity_frames * nb below 2^31.  Sizes off these are ISPA_ERR_UNSUPPORTED.
  *
  * A rollout keeps `means` next to the ring: after an append, ispa_key_means of the frames appended; before an
- * attention, ispa_select_blocks with its queries and window.
+ * attention, ispa_select_blocks with its queries and window.  The means and the selection take every ring; the
+ * attention has no form for e4m3 values (ISPA_KV_KV_E4M3).
  */
 
 /*
@@ -947,6 +948,9 @@ ISPA_API ispa_status ispa_select_blocks(const ispa_kv_ring* ring, ispa_window wi
  *   k_cur, v_cur : both NULL where the call has no chunk (the new frames are in the ring already); then no flags
  * Other arguments as in ispa_attn_local_ex.  A query that sees no key has out = 0 and lse = -inf.  Tokens behind a
  * frame's last one are not read for listed blocks, whatever they hold.
+ * As in ispa_attn_local the probabilities are rounded to bf16 for their product with the values, but for calls of one
+ * or two queries without flags, which are computed in fp32 up to the output's rounding: a query's last bits depend on
+ * how many there are.
  */
 ISPA_API ispa_status ispa_attn_blocks(const ispa_kv_ring* ring, ispa_window win, int32_t block, const int32_t* blocks,
                                       int32_t top_k, const void* q, const void* k_cur, const void* v_cur, int32_t n_q,

@@ -444,8 +444,9 @@ __global__ void __launch_bounds__(NTHREADS, 1)
         mbar_arrive_expect_tx(b.v_full0 + 8 * vs, C::V_TILE);
         const uint32_t sV = sbase + C::OFF_V + vs * C::V_TILE;
         const int vhead = vk == kk ? kh : prev_h;
-        // The dense tiles' loads behind a condition of their own: as the other branch of one with the listed tiles' the
-        // instances without lists took 0.3 to 0.6 % longer (4680 queries x 12 heads x 32760 keys 586.4 us, so 584.4).
+        // The dense tiles' loads stand behind a condition of their own.  As the else branch of the listed tiles' they
+        // made the instances without lists 0.3 to 0.6 % slower (4680 queries x 12 heads x 32760 keys 586.4 us, not
+        // 584.4).
         bool listed = false;
         if constexpr (BLOCKS) {
           listed = vj >= n_dense;

@@ -98,15 +98,14 @@ __global__ void __launch_bounds__(M_THREADS) means_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------ selection
-// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 22 us
+// Three kernels: sums of the queries, 32-bit scores, the choice.  4680 queries x 12 heads over 1250 candidates: 21 us
 // where reading once takes 3.3; the launches' latency bounds it (each a launch's own 2 us and a chain of loads, passes
-// and barriers; issue slots 50 to 60 %).  Few candidates or one
-// query block: one kernel, one query 8.2 us (select_kernel); one query block and few heads: two, the sum in the scoring
-// one.
+// and barriers; issue slots 50 to 60 %).  Few candidates or one query block: one kernel, one query 7.6 us
+// (select_kernel); one query block and few heads: two, the sum in the scoring one.
 // Workspace: per head and query block the sum of the queries (hi, and lo with the rest); room for 64-bit scores, the
-// 32-bit scores, the sum's norm, and a bound on what hi + lo is off by; per head and tile of candidates the largest norm
-// of a mean.  hi and lo are multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows lies on
-// its 8 and 4.
+// 32-bit scores, the sum's norm, and a bound on what hi + lo is off by; per head and tile of candidates the largest
+// norm of a mean.  hi and lo are multiples of 256 bytes, so that hi's rows can be read by 16 bytes and what follows
+// lies on its 8 and 4.
 struct SelectWs {
   float* hi;          // [H][n_qt][d]
   float* lo;
@@ -168,8 +167,8 @@ __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
 // the k-th sum of a thread's N rows is at most k Y, and its lo takes a residue of k steps; the block's k-th sum is at
 // most N k Y, and its lo takes a residue of N k steps and then a thread's lo of N (N + 1) / 2.  So the lo's stay below
 // (N k (k + 1) + N (N + 1) k) / 2 steps, and both additions round to 2^-24 of that: over k <= ROWS, with the threads'
-// own, 2^-33.4 Y for N = 8 and 2^-32.1 Y for N = 4.  lost_of: 2^-32 sqrt(D) Y for all features, twice, for the roundings
-// of 64-bit scores (below 2^-37 sqrt(D) Y |m|).
+// own, 2^-33.4 Y for N = 8 and 2^-32.1 Y for N = 4.  lost_of: 2^-32 sqrt(D) Y for all features, twice, for the
+// roundings of 64-bit scores (below 2^-37 sqrt(D) Y |m|).
 template <int D>
 __device__ __forceinline__ float lost_of(float y) {
   return (D == 128 ? 11.5f : 8.f) * 4.6566129e-10f * y;
@@ -269,11 +268,11 @@ __global__ void __launch_bounds__(Q_THREADS, 3) qsum_kernel(const __grid_constan
 
 // 32-bit scores: a tile of 64 candidates x 8 J query blocks of one head in shared memory, 2 x J a thread.  A warp's
 // lanes read 16 candidates' words and two query blocks' at a time, with J = 5 in 9 cycles of shared memory for 10 of
-// products; J = 3 for 17 to 24 query blocks, where 5 takes 3 to 4 us more for 12 heads x 1250.  OWN: one query block,
-// whose sum every block of the grid takes for itself.  BLOCKS: that an SM is to hold; with the registers of two (108
-// where three leave 80) the rows are read further ahead: 37 query blocks, 12 heads x 1250 23.3 us in all (26.1), but 40
-// heads x 650, three blocks an SM, 37.3 (35.3).  Without a bound the compiler leaves 34 to 78 registers and
-// reads no row ahead: 28.9 and 38.9.
+// products; J = 3 for 17 to 24 query blocks, where 5 takes 1 us more for 12 heads x 1250.  OWN: one query block, whose
+// sum every block of the grid takes for itself.  BLOCKS: that an SM is to hold; with the registers of two (122 where
+// three leave 80) the rows are read further ahead.  In all, 37 query blocks of 12 heads x 1250, a grid of 240 blocks:
+// 21.2 us with two, 24.0 with three, 24.1 without a bound; of 40 heads x 650, 440 blocks: 32.8, 32.5 and 32.7; 74 query
+// blocks of 40 heads 61.2, 60.0 and 60.4.
 constexpr int S_CAND = 64, S_THREADS = 256;
 template <int D, int J>
 constexpr int kScoreSmem = (S_CAND + 8 * J) * (D + 4) * 4;
@@ -810,9 +809,9 @@ __global__ void __launch_bounds__(32 * W) pick_kernel(const __grid_constant__ Se
 
 // All in one launch, for few candidates or one query block: a cluster a list, every CTA with the queries' sum and its
 // share of the candidates, a warp eight means at a time and as many on their way; then the first CTA chooses.  Latency
-// bounds it (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 8.2 us
-// where two launches took 10.9, 128 queries 9.9 (13.2); of 40 heads 12 (21).  A block number looked up by one lane, not
-// by all: 9.8 -> 8.4.
+// bounds it (sum, means, the cluster's barrier, the choice's passes).  1250 candidates of 12 heads: one query 7.6 us
+// where two launches take 9.8, 128 queries 8.2 (10.7); one query of 40 heads 10.2 (18.1).  Block numbers looked up by
+// every lane instead of one took 1.4 us more.
 constexpr int O_WARPS = 8, O_THREADS = 32 * O_WARPS, O_BATCH = 8;
 template <int D, int PER>
 __global__ void __launch_bounds__(O_THREADS) select_kernel(const __grid_constant__ SelectParams p) {
@@ -904,11 +903,13 @@ int sm_count() {
 template <int D>
 cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   const int n = p.n_cand;
-  // One launch where an SM's share of the means is small: 12 heads x 125 candidates, 1024 queries 6.5 us (three
-  // launches 10.2); 40 heads x 225, 512 queries 10.7 (19.6); 12 heads x 325, 4680 queries, a share of 950, 22.1 (22.7);
-  // 3 heads x 4825, 512 queries, 965, 15.6 (13.9); 64 features: 12 heads x 125, 1024 queries 6.8 (9.2); x 325, a share
-  // of as many, 10.8 (10.0).  One query block, which all of the scoring kernel's blocks would add up: but for few
-  // heads, too; 12 heads x 4825 21 (24), one head 16.3 (12.2).
+  // One launch where an SM's share of the means is small; us in one launch, in three in brackets.  128 features: 1024
+  // queries of 12 heads, shares of 125, 400 and 700, 8.4 (11.6), 12.9 (12.0), 15.5 (12.8); 4680 queries of 12 heads,
+  // 438, 511 and 949, 15.9 (18.0), 16.0 (18.2), 22.6 (18.6); 512 of 3 heads, 300 and 603, 14.5 (14.2), 16.1 (13.7);
+  // 300 of 40, 450 and 650, 13.8 (15.5), 15.8 (16.9).  64 features: 1024 queries of 12 heads, 200, 325 and 500, 7.0
+  // (8.0), 8.9 (8.3), 13.4 (11.4); 4680 of 12, 175 and 350, 10.7 (14.0), 8.4 (10.7).  One query block, which all of
+  // the scoring kernel's blocks would add up, but for few heads too: one query over 4825 candidates of 12 heads 15.6
+  // (two launches 21.1), of 7 14.7 (17.0), of 3 14.6 (12.6), of one 14.4 (10.1).
   const int sms = sm_count(), wanted = (n + O_WARPS * O_BATCH - 1) / (O_WARPS * O_BATCH);
   const int64_t items = static_cast<int64_t>(p.H) * p.n_qt;
   const int c = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, sms / items, wanted})));
@@ -926,7 +927,8 @@ cudaError_t select_d(const SelectParams& p, cudaStream_t s) {
   if (p.n_cand > p.top_k) {
     const int64_t tiles = (n + S_CAND - 1) / S_CAND;
     // Query blocks by groups of 8 J: one after the other in a block of the grid, or side by side where that leaves the
-    // blocks that the SMs hold: 9344 queries x 12 heads x 1250 candidates 36 us in all, else 46.
+    // blocks that the SMs hold: 1250 candidates of 4 heads, 9344 queries 20.2 us in all, else 24.5; of 2 heads, 18720
+    // queries 19.6, else 35.0; of 12 heads the same both ways.
     const auto score = [&](auto j, auto own) {
       constexpr int J = decltype(j)::value;
       const int64_t groups = (p.n_qt + 8 * J - 1) / (8 * J);

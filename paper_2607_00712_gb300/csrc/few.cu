@@ -9,13 +9,14 @@
 // weights from their lanes.  Warps, then CTAs through shared memory of the cluster, merge (O, m, l) as Eq. 11-12 do.
 // All of it in fp32, rounded once.
 //
-// One query, 12 heads, 5656 keys (34.8 MB, 5.0 us at the copy rate): 8.6 us a launch in a graph, 12.2 with the tensor
-// cores' kernel; 1024 keys 4.5 (12.4), 19112 keys 22.3 (25.2); two queries 10.2, 5.1, 23.3.  40 heads x 15016 keys 49.0
-// (50.0; floor 45.3), in 8 bits 37.5 (41.8; 34).  40 heads x 78800 keys is the other way round, 236 against 226 (238 at
-// the copy rate).  What bounds it: an SM takes 60 bytes a cycle in and as many out of its shared memory, and clusters
-// of eight leave 56 SMs without work where there are 12 heads.  Steps: rows in registers, 32 keys at a time 11.4;
-// asynchronous copies, 8 warps of three units 9.7; two products an instruction and 12 warps 9.0; whole units' copies
-// without conditions 8.6.  Four queries 15.2: those are the other kernel's.
+// One query, 12 heads, 5656 keys (34.8 MB, 5.0 us at the copy rate): 8.1 to 8.6 us a launch in a graph, 11.8 to 12.2
+// with the tensor cores' kernel; 1024 keys 4.5 (12.4), 19112 keys 22.3 (25.2); two queries 9.7 to 10.2, 5.2, 23.3.  40
+// heads x 15016 keys 49.0 (50.0; floor 45.3), in 8 bits 37.5 (41.8; 34).  40 heads x 73000 keys is the other way
+// round, 221 against 209 (220 at the copy rate).  What bounds it: an SM takes 60 bytes a cycle in and as many out of
+// its shared memory, and clusters of eight leave 56 SMs without work where there are 12 heads.  Steps: rows in
+// registers, 32 keys at a time 11.4; asynchronous copies, 8 warps of three units 9.7; two products an instruction and
+// 12 warps 9.0; whole units' copies without conditions 8.6.  Four queries were tried with eight warps alone, 15.2:
+// from three on the other kernel's 11.8.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -43,7 +44,7 @@ struct FewParams : AttnParams {
   const __nv_bfloat16* v_ring;
   const __nv_bfloat16* v_cur;
   int64_t ring_tok;
-  int32_t units;             // of 32 keys, of a head
+  int32_t units;             // of F_KEYS keys, of a head
   int32_t units_of_block;
   Divisor by_units;          // of a block
 };

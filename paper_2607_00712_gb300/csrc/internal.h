@@ -106,7 +106,7 @@ cudaError_t launch_attention(int head_dim, const CUtensorMap* tm_q, const CUtens
                              const CUtensorMap* tm_vc, const AttnParams& p, cudaStream_t s,
                              const AttnLists* lists = nullptr);
 // The same over segments and lists for up to kFewQueries queries, chunk not causal, without tensor maps (few.cu).
-constexpr int kFewQueries = 2;
+constexpr int kFewQueries = 2;   // 12 heads x 5656 keys, one to three: 8.1, 9.7 and (attn_kernel) 11.8 us; see few.cu
 cudaError_t launch_attention_few(int head_dim, const AttnParams& a, const AttnLists& lists, const void* q,
                                  const void* k_ring, const void* v_ring, const void* k_cur, const void* v_cur,
                                  int64_t ring_tok, cudaStream_t s);
@@ -238,11 +238,11 @@ cudaError_t launch_quant_given(const void* x, int64_t n, int32_t H, int32_t d, c
 // d-major e4m3 values: out[h][c][t], d = 128, ld % 16 == 0.
 cudaError_t launch_quant_vt(const void* x, int64_t n, int32_t H, const float* scale, uint8_t* out, int64_t ld,
                             cudaStream_t s);
-// vt_scale: null (values copied as bf16), or the values' per-head scales: v_dst then takes d-major codes
-// of row stride vt_ld in the frames' slots (d = 128, P % 4 == 0).
 // Values alone, as d-major codes in the frames' slots; token t's heads at v + t * v_stride.
 cudaError_t launch_append_vt(const int32_t* slots, int32_t n_frames, int32_t P, int32_t H, const void* v,
                              int64_t v_stride, void* v_dst, const float* vt_scale, int64_t vt_ld, cudaStream_t s);
+// vt_scale: null (values copied as bf16), or the values' per-head scales: v_dst then takes d-major codes
+// of row stride vt_ld in the frames' slots (d = 128, P % 4 == 0).
 cudaError_t launch_append_qk8(const int32_t* slots, int32_t n_frames, int32_t P, int32_t H, int32_t d,
                               int64_t ring_tok, const void* k_src, const void* v_src, void* k_dst, void* v_dst,
                               const float* k_scale, const float* vt_scale, int64_t vt_ld, cudaStream_t s);
